@@ -82,6 +82,9 @@ extern "C" {
 #define WISV_ST_BAD_WINDOW    16   /* k_off gave this request a window outside 0..WISV_MAX_K tokens: only its first
                                       WISV_MAX_K positions (or none) were verified.  k_off lives on the device, so
                                       wisv_verify cannot check it; wisv_verify_host does and returns WISV_ESHAPE */
+#define WISV_ST_NO_PAGES      32   /* wisv_cache_extend: the pool or the block-table row cannot hold the request */
+#define WISV_ST_NO_MASS       64   /* wisv_verify_residual: the distribution to draw from has no weight */
+#define WISV_ST_BAD_LENGTH   128   /* wisv_cache_extend / wisv_cache_commit: a length that is negative or out of reach: clamped */
 
 /* element type of a hidden-state array (wisv_batch.target_hidden_dtype / draft_hidden_dtype) */
 #define WISV_DT_F32  0      /* fp32: rounded to bf16 (nearest even) by the library */
@@ -408,6 +411,174 @@ int wisv_debug_wait_probe(wisv_ctx* ctx, uint64_t limit_cycles, void* cuda_strea
  */
 int wisv_debug_poison(wisv_ctx* ctx, void* cuda_stream);
 int wisv_debug_poison_static(void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Paged key/value cache of the target model.
+ *
+ * The hidden states that wisv_verify takes come out of the target's layers, each of which attends from the K_b + 1 window
+ * rows of a request (or from a chunk of its prompt) to everything cached before them.  The cache is cut into pages of
+ * page_size tokens; request b is row b of a block table whose entries name its pages in order.  One round is
+ *
+ *     wisv_cache_extend    pages, slots, positions and lengths for the round's new tokens      (once per round)
+ *     wisv_cache_append    the new keys and values of one layer into their slots               (per layer)
+ *     wisv_cache_attend    attention of the new tokens over the cache, themselves included     (per layer)
+ *     wisv_verify / wisv_verify_residual                                                       (once)
+ *     wisv_cache_commit    the lengths the verdict leaves; the pages behind them go back       (once)
+ *
+ * Lengths stay on the device throughout: nothing here reads them back or synchronises, and every call can be captured
+ * in a CUDA graph.  The page pools (one pair of K and V arrays per layer) and the bookkeeping arrays belong to the caller.
+ * Calls on one wisv_cache must be stream-ordered: they share its workspace.
+ */
+#define WISV_MAX_REQUESTS 4096
+#define WISV_MAX_GROUP    64        /* query heads per key head */
+
+typedef struct wisv_cache wisv_cache;
+
+typedef struct {
+    int32_t n_heads;        /* query heads, a multiple of n_kv_heads, at most WISV_MAX_GROUP per key head */
+    int32_t n_kv_heads;     /* key / value heads */
+    int32_t head_dim;       /* 64 or 128 */
+    int32_t page_size;      /* tokens per page: 16, 32, 64, 128 or 256 */
+    int32_t n_pages;        /* pages in the pool */
+    int32_t max_requests;   /* rows of the block table, 1..WISV_MAX_REQUESTS */
+    int32_t max_blocks;     /* columns of the block table: a request holds at most max_blocks * page_size tokens */
+    int32_t dtype;          /* WISV_DT_BF16 or WISV_DT_F16: keys, values, queries and outputs */
+} wisv_cache_config;
+
+/* bookkeeping arrays, all device memory of the caller */
+typedef struct {
+    int32_t* free_list;     /* dev [n_pages]: the first n_free entries are the free pages */
+    int32_t* n_free;        /* dev [1] */
+    int32_t* block_table;   /* dev [max_requests, max_blocks]: entries past n_blocks[b] are -1 */
+    int32_t* n_blocks;      /* dev [max_requests]: pages that request b holds */
+    int32_t* seq_len;       /* dev [max_requests]: tokens of request b that are kept (committed) */
+} wisv_pages;
+
+/* what wisv_cache_extend writes for the round's T_total new tokens; token t of request b is row q_off[b] + i */
+typedef struct {
+    int32_t* q_off;         /* dev [B+1]: prefix sums of the new tokens */
+    int32_t* kv_len;        /* dev [B]: seq_len[b] + new tokens; 0 for a request that got no pages */
+    int64_t* slot_map;      /* dev [T_total]: page * page_size + offset in the page; -1: not cached */
+    int32_t* positions;     /* dev [T_total]: position of the token in its request; -1 for rows past the last request */
+    int32_t* status;        /* dev [B], optional: WISV_ST_NO_PAGES, WISV_ST_BAD_LENGTH */
+} wisv_layout;
+
+/*
+ * Create a cache context on the current device: checks the configuration and allocates the workspace of
+ * wisv_cache_attend (partial results of the blocks; 2 * SMs * 256 rows).  *out is NULL on failure.
+ */
+int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out);
+int wisv_cache_destroy(wisv_cache* cache);          /* the caller must have synchronised */
+int64_t wisv_cache_launch_count(const wisv_cache* cache);
+/* Read (and clear) the device error word: non-zero if a bounded wait inside a kernel gave up.  Synchronises the stream. */
+int wisv_cache_error(wisv_cache* cache, void* cuda_stream, int32_t* flags);
+
+/*
+ * Room for a round: request b (row b of the table, 0 <= b < B) gets new tokens n_new[b] (dev [B]), or n_uniform each
+ * where n_new is NULL, on top of seq_len[b].  Pages it lacks come from the end of the free list, in request order: with N pages
+ * taken in all, the j-th of them (requests ascending, blocks ascending) is free_list[n_free - N + j].  Requests are served
+ * in order: one whose pages, added to those of all requests before it, exceed the free ones gets none, and neither do
+ * later ones that need any; nor does one whose row of the table is too short.  Such a request is flagged WISV_ST_NO_PAGES; its
+ * slots are -1 and its kv_len is 0 (its rows of wisv_cache_attend become zero).  T_total is the sum of n_new, which the
+ * host knows: rows past it are not written, rows past the sum get slot and position -1.
+ * block_table, n_blocks, free_list and n_free are updated; seq_len is not (the tokens are kept by wisv_cache_commit).
+ */
+int wisv_cache_extend(wisv_cache* cache, const wisv_pages* pages, int32_t B, int32_t T_total, const int32_t* n_new,
+                      int32_t n_uniform, const wisv_layout* out, void* cuda_stream);
+
+/*
+ * The lengths that the verdict leaves: seq_len[b] = new_len[b] (dev [B]), for instance seq_len + accept_len + 1, or 0 for
+ * a finished request.  Pages behind the new length go back to the end of the free list, requests ascending, blocks
+ * ascending, so that a round that is withdrawn entirely leaves the free list as it was.  A length that is negative or
+ * longer than the pages held is clamped and flagged WISV_ST_BAD_LENGTH in status (dev [B], optional).
+ */
+int wisv_cache_commit(wisv_cache* cache, const wisv_pages* pages, int32_t B, const int32_t* new_len, int32_t* status,
+                      void* cuda_stream);
+
+/*
+ * Keys and values of one layer into their slots.  Strides are in elements and multiples of 8, bases 16-byte aligned, a
+ * head's head_dim elements contiguous: k and v may be slices of a fused projection, pages may be [page, token, head, dim] or
+ * [page, head, token, dim].  Slots outside [0, n_pages * page_size) are skipped.  Two tokens must not share a slot.
+ */
+typedef struct {
+    int32_t T;                                                            /* rows */
+    const void *k, *v;                                                    /* dev [T, n_kv_heads, head_dim] */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    void *k_pages, *v_pages;                                              /* dev pools */
+    int64_t kp_page_stride, kp_token_stride, kp_head_stride, vp_page_stride, vp_token_stride, vp_head_stride;
+    const int64_t* slot_map;                                              /* dev [T] */
+} wisv_append;
+int wisv_cache_append(wisv_cache* cache, const wisv_append* a, void* cuda_stream);
+
+/*
+ * Attention of each request's new tokens over its cache.  Row i of request b (n_b = q_off[b+1] - q_off[b] rows, i from 0) sees
+ * keys 0 .. kv_len[b] - n_b + i of the request: all that was cached before, and the new tokens up to itself (which
+ * wisv_cache_append has written).  out = softmax(scale * q k^T) v per head; query head h reads key head h / (n_heads /
+ * n_kv_heads).  A row that sees no key gives zero, and -inf in lse.  Scores, maxima, sums and products are accumulated in fp32; the
+ * probabilities are rounded to the cache's 16-bit type for the second product.
+ * Keys and values past kv_len[b] (and whole pages that the table does not reach) may hold anything, NaN included; table entries
+ * outside the pool read as zeros.
+ */
+typedef struct {
+    int32_t B;
+    int32_t T;                           /* rows of q */
+    int32_t max_new;                     /* largest n_b expected: a hint for the layout of the work, not a limit */
+    const int32_t* q_off;                /* dev [B+1], or NULL: max_new rows per request */
+    const int32_t* kv_len;               /* dev [B]: cached tokens, the new ones included */
+    const int32_t* block_table;          /* dev */
+    int64_t table_stride;                /* entries per row of the table */
+    int32_t max_blocks;                  /* entries of a row that may be read */
+    const void* q;                       /* dev [T, n_heads, head_dim] */
+    int64_t q_token_stride, q_head_stride;
+    const void *k_pages, *v_pages;       /* strides as in wisv_append; page strides are multiples of 8 token strides */
+    int64_t kp_page_stride, kp_token_stride, kp_head_stride, vp_page_stride, vp_token_stride, vp_head_stride;
+    void* out;                           /* dev [T, n_heads, head_dim] */
+    int64_t o_token_stride, o_head_stride;
+    float* lse;                          /* dev [T, n_heads], optional: natural log of the sum of exp(scale * q k^T) */
+    float scale;                         /* 0: 1 / sqrt(head_dim) */
+} wisv_attend;
+int wisv_cache_attend(wisv_cache* cache, const wisv_attend* a, void* cuda_stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Verification against the target's probabilities with a draw from the residual (Eqs. 1 and 2).
+ *
+ * Request b has a window of K_b <= WISV_MAX_K drafts, rows and tokens indexed as in wisv_verify.  With P = target_probs of
+ * row k_off[b] + b + i and Q = the drafter's distribution at token t = k_off[b] + i, draft y is accepted iff
+ * u_t < min(1, P(y) / Q(y)) (Q(y) = 0: iff P(y) > 0), the quotient in fp32.  accept_len = A is the first position that fails, or K_b;
+ * given accept_in (a verdict of wisv_verify, whose decision head may accept a failing position), A = accept_in[b] instead.
+ * The emitted token is drawn from max(P - Q, 0) at position A, or from P itself at A = K_b (the bonus token) and where the
+ * residual has no weight at all.
+ *
+ * The draw is exact and independent of the order of summation: with w(v) = floor(2^44 max(P(v) - Q(v), 0)) (the
+ * difference in fp32), W = sum w and m = floor(2^31 u_draw[b]), the token is the lowest v with
+ * w(0) + ... + w(v) > floor(W m / 2^31).  P and Q are used as given (they need not sum to 1), clamped to [0, 1], NaN as 0.
+ */
+typedef struct {
+    int32_t B, K;                        /* requests; uniform window, or 0 with k_off */
+    const int32_t* k_off;                /* dev [B+1] or NULL */
+    int32_t T_total;                     /* drafts in all */
+    int32_t V;                           /* vocabulary, at most WISV_STATIC_MAX_V */
+    const void* target_probs;            /* dev [T_total + B, V] */
+    int64_t target_stride;               /* elements per row */
+    int32_t target_dtype;                /* WISV_DT_* */
+    const int32_t* draft_tokens;         /* dev [T_total]; ids outside [0, V) are clamped and flagged WISV_ST_BAD_TOKEN */
+    const void* draft_probs;             /* dev: [T_total, V] with draft_ids NULL; fp32 [T_total, n_top] with draft_ids (what a
+                                            device uploads of its distribution: ids and probabilities; tokens not named have 0,
+                                            a token named twice has the sum); NULL: the drafter was deterministic, Q(y) = 1 */
+    int64_t draft_stride;                /* elements per row of draft_probs */
+    int32_t draft_dtype;                 /* of dense draft_probs */
+    const int32_t* draft_ids;            /* dev [T_total, n_top] contiguous; ids outside [0, V) are ignored */
+    int32_t n_top;                       /* at most WISV_MAX_TOP */
+    const float* uniforms;               /* dev [T_total], u in [0, 1); may be NULL with accept_in */
+    const float* u_draw;                 /* dev [B], u in [0, 1) */
+    const int32_t* accept_in;            /* dev [B], optional */
+    int32_t* accept_len;                 /* dev [B], required */
+    int32_t* token;                      /* dev [B], required; -1 where P has no weight either (WISV_ST_NO_MASS) */
+    float* mass;                         /* dev [B], optional: W / 2^44, the mass that the token was drawn from */
+    int32_t* status;                     /* dev [B], optional */
+} wisv_residual;
+#define WISV_MAX_TOP 256
+int wisv_verify_residual(const wisv_residual* r, void* cuda_stream);
 
 const char* wisv_strerror(int code);
 int wisv_version(void);

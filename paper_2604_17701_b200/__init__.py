@@ -10,3 +10,4 @@ from .binding import (  # noqa: F401
     LinkParams, link_cost_round, choose_protocol, plan_host,
     ACT_RELU, ACT_GELU, MODE_FH, MODE_SH, ACCEPT_GREEDY, ACCEPT_STOCHASTIC, DT_F32, DT_BF16, DT_F16,
 )
+from .paged import PagedCache, WindowLayout, ResidualOutput, verify_residual  # noqa: F401
