@@ -13,13 +13,23 @@
 
 using namespace wisv;
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct wisv_cache {
     wisv_cache_config cfg;
     int device = 0;
     int sm_count = 0;
     int page_shift = 0;
     int64_t launches = 0;
+    // one allocation: [error word | merge descriptors | partial maxima and sums | partial outputs]
+    void* work = nullptr;
     int32_t* err = nullptr;
+    int4* desc = nullptr;
+    float2* part_ml = nullptr;
+    float* part_o = nullptr;
+    EncodeTiledFn encode = nullptr;
 };
 
 namespace {
@@ -60,6 +70,34 @@ int launch(void (*kernel)(P), int grid, int block, size_t smem, int cluster, cud
     return WISV_OK;
 }
 
+// Five-dimensional map of 16-bit elements with the 128-byte swizzle; strides[i] in bytes for dimensions 1..4.
+int encode_5d(const wisv_cache* c, CUtensorMap* out, const void* base, const cuuint64_t (&dims)[5],
+              const cuuint64_t (&strides)[4], const cuuint32_t (&box)[5])
+{
+    const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+    const CUresult r = c->encode(out, c->cfg.dtype == WISV_DT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                                 5, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? WISV_OK : WISV_EINVAL;
+}
+
+// A pool of pages as (64 columns, 8 tokens, column halves, key head, 8-token group): one box is one page (or 128 tokens of
+// a larger one) of one head, in shared memory [group][half][token][64].
+int encode_pool(const wisv_cache* c, CUtensorMap* out, const void* base, int64_t page, int64_t token, int64_t head,
+                int32_t* page_groups, int32_t* groups)
+{
+    const int64_t step = c->cfg.n_pages > 1 ? page / (8 * token) : 0;
+    const int64_t n = (c->cfg.n_pages - 1) * step + c->cfg.page_size / 8;
+    if (n > 0x7fffffffLL) return WISV_ESHAPE;
+    *page_groups = (int32_t)step;
+    *groups = (int32_t)n;
+    const cuuint64_t dims[5] = {64, 8, (cuuint64_t)c->cfg.head_dim / 64, (cuuint64_t)c->cfg.n_kv_heads, (cuuint64_t)n};
+    const cuuint64_t strides[4] = {(cuuint64_t)token * 2, 128, (cuuint64_t)(c->cfg.n_kv_heads > 1 ? head : 64) * 2, (cuuint64_t)token * 16};
+    const cuuint32_t box[5] = {64, 8, (cuuint32_t)c->cfg.head_dim / 64, 1, (cuuint32_t)(c->cfg.page_size < kAttnTile ? c->cfg.page_size : kAttnTile) / 8};
+    return encode_5d(c, out, base, dims, strides, box);
+}
+
 int check_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B)
 {
     if (!c || !pg || !pg->free_list || !pg->n_free || !pg->block_table || !pg->n_blocks || !pg->seq_len) return WISV_EINVAL;
@@ -85,6 +123,34 @@ void fill_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B, PagesParam
 // rounds with more rows than this are laid out by a cluster of eight blocks
 constexpr int kExtendOneBlockRows = 4096;
 constexpr int kCommitOneBlockRequests = 64;
+
+// the smallest stretch of key tiles worth a block of its own: two run at the same time, one per warpgroup
+constexpr int kAttnMinUnits = 2;
+constexpr int kMergeRowBlocks = 8;
+
+// the attention kernel and, behind it with programmatic dependent launch, the merge of what its blocks share
+template <typename E, int D>
+int launch_attn(const wisv_cache* c, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const AttnParams& p,
+                const AttnMerge& m, cudaStream_t st)
+{
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof cfg);
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)c->sm_count);
+    cfg.blockDim = dim3(kAttnThreads);
+    cfg.dynamicSmemBytes = kAttnSmem;
+    WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn_kernel<E, D>, tmQ, tmK, tmV, p));
+    cfg.gridDim = dim3((unsigned)c->sm_count, kMergeRowBlocks);
+    cfg.blockDim = dim3(kMergeThreads);
+    cfg.dynamicSmemBytes = 0;
+    WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn_merge_kernel<E, D>, m));
+    return WISV_OK;
+}
 
 }  // namespace
 
@@ -121,10 +187,27 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
         delete c;
         return WISV_ECUDA;
     }
-    if (cudaMalloc(&c->err, 256) != cudaSuccess) { (void)cudaGetLastError(); delete c; return WISV_ENOMEM; }
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ready =
+        cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) == cudaSuccess && fn &&
+        cudaFuncSetAttribute(attn_kernel<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+        cudaFuncSetAttribute(attn_kernel<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+        cudaFuncSetAttribute(attn_kernel<__half, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+        cudaFuncSetAttribute(attn_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
+    if (!ready) { (void)cudaGetLastError(); delete c; return WISV_ECUDA; }
+    c->encode = reinterpret_cast<EncodeTiledFn>(fn);
+    const size_t n_ml = (size_t)sms * 2 * 256, off_desc = 256, off_ml = off_desc + (size_t)sms * 32,
+                 off_o = (off_ml + n_ml * 8 + 255) / 256 * 256;
+    if (cudaMalloc(&c->work, off_o + n_ml * cfg->head_dim * 4) != cudaSuccess) { (void)cudaGetLastError(); delete c; return WISV_ENOMEM; }
+    char* w = static_cast<char*>(c->work);
+    c->err = reinterpret_cast<int32_t*>(w);
+    c->desc = reinterpret_cast<int4*>(w + off_desc);
+    c->part_ml = reinterpret_cast<float2*>(w + off_ml);
+    c->part_o = reinterpret_cast<float*>(w + off_o);
     if (cudaMemset(c->err, 0, 256) != cudaSuccess || cudaStreamSynchronize(0) != cudaSuccess) {
         (void)cudaGetLastError();
-        cudaFree(c->err);
+        cudaFree(c->work);
         delete c;
         return WISV_ECUDA;
     }
@@ -135,7 +218,7 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
 int wisv_cache_destroy(wisv_cache* c)
 {
     if (!c) return WISV_EINVAL;
-    cudaFree(c->err);
+    cudaFree(c->work);
     delete c;
     return WISV_OK;
 }
@@ -243,27 +326,39 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     const int64_t s[] = {a->q_token_stride, a->q_head_stride, a->o_token_stride, a->o_head_stride, a->kp_page_stride,
                          a->kp_token_stride, a->kp_head_stride, a->vp_page_stride, a->vp_token_stride, a->vp_head_stride};
     for (int64_t x : s) if (x % 8 || x < 0) return WISV_EALIGN;
-    if (a->kp_page_stride % (8 * a->kp_token_stride) || a->vp_page_stride % (8 * a->vp_token_stride)) return WISV_EALIGN;
+    if (!a->kp_token_stride || !a->vp_token_stride || a->kp_page_stride % (8 * a->kp_token_stride) || a->vp_page_stride % (8 * a->vp_token_stride)) return WISV_EALIGN;
+    const int group = c->cfg.n_heads / c->cfg.n_kv_heads, D = c->cfg.head_dim;
     AttnParams p;
-    p.B = a->B; p.T = a->T; p.max_new = a->max_new;
-    p.n_heads = c->cfg.n_heads; p.group = c->cfg.n_heads / c->cfg.n_kv_heads;
-    p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
-    p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table; p.table_stride = a->table_stride;
-    p.q = a->q; p.qt = s[0]; p.qh = s[1]; p.out = a->out; p.ot = s[2]; p.oh = s[3];
-    p.kp = a->k_pages; p.vp = a->v_pages; p.kpp = s[4]; p.kpt = s[5]; p.kph = s[6]; p.vpp = s[7]; p.vpt = s[8]; p.vph = s[9];
-    p.lse = a->lse;
-    p.scale = a->scale > 0.0f ? a->scale : 1.0f / sqrtf((float)c->cfg.head_dim);
-    const int64_t n = (int64_t)a->T * p.n_heads;
-    const int grid = (int)((n + 3) / 4);
+    memset(&p, 0, sizeof p);
+    CUtensorMap tmQ, tmK, tmV;
+    int r = encode_pool(c, &tmK, a->k_pages, s[4], s[5], s[6], &p.page_groups_k, &p.groups_k);
+    if (r == WISV_OK) r = encode_pool(c, &tmV, a->v_pages, s[7], s[8], s[9], &p.page_groups_v, &p.groups_v);
+    if (r != WISV_OK) return r;
+    p.tpt = kAttnTile / group < a->max_new ? kAttnTile / group : a->max_new;
+    {
+        // (64 columns, head of the group, token, column halves, key head): a box is a row tile of one key head
+        const cuuint64_t dims[5] = {64, (cuuint64_t)group, (cuuint64_t)a->T, (cuuint64_t)D / 64, (cuuint64_t)c->cfg.n_kv_heads};
+        const cuuint64_t strides[4] = {(cuuint64_t)(c->cfg.n_heads > 1 ? s[1] : 64) * 2, (cuuint64_t)(a->T > 1 ? s[0] : 64) * 2, 128,
+                                       (cuuint64_t)(c->cfg.n_heads > 1 ? s[1] : 64) * 2 * group};
+        const cuuint32_t box[5] = {64, (cuuint32_t)group, (cuuint32_t)p.tpt, 1, 1};
+        r = encode_5d(c, &tmQ, a->q, dims, strides, box);
+        if (r != WISV_OK) return r;
+    }
+    p.B = a->B; p.T = a->T; p.max_new = a->max_new; p.n_kv = c->cfg.n_kv_heads; p.group = group;
+    p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks; p.min_units = kAttnMinUnits;
+    p.uniform = a->max_new; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
+    p.table_stride = a->table_stride;
+    p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;
+    p.scale_log2 = (a->scale > 0.0f ? a->scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+    p.err = c->err; p.part_o = c->part_o; p.part_ml = c->part_ml; p.desc = c->desc;
+    AttnMerge m;
+    m.part_o = p.part_o; m.part_ml = p.part_ml; m.desc = p.desc;
+    m.out = p.out; m.ot = p.ot; m.oh = p.oh; m.lse = p.lse; m.group = group; m.n_heads = c->cfg.n_heads;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    int r;
-    if (c->cfg.dtype == WISV_DT_BF16)
-        r = c->cfg.head_dim == 128 ? launch(attn_simple_kernel<__nv_bfloat16, 128>, grid, 128, 0, 1, st, p)
-                                   : launch(attn_simple_kernel<__nv_bfloat16, 64>, grid, 128, 0, 1, st, p);
-    else
-        r = c->cfg.head_dim == 128 ? launch(attn_simple_kernel<__half, 128>, grid, 128, 0, 1, st, p)
-                                   : launch(attn_simple_kernel<__half, 64>, grid, 128, 0, 1, st, p);
-    if (r == WISV_OK) ++c->launches;
+    const bool bf = c->cfg.dtype == WISV_DT_BF16;
+    if (D == 128) r = bf ? launch_attn<__nv_bfloat16, 128>(c, tmQ, tmK, tmV, p, m, st) : launch_attn<__half, 128>(c, tmQ, tmK, tmV, p, m, st);
+    else r = bf ? launch_attn<__nv_bfloat16, 64>(c, tmQ, tmK, tmV, p, m, st) : launch_attn<__half, 64>(c, tmQ, tmK, tmV, p, m, st);
+    if (r == WISV_OK) c->launches += 2;
     return r;
 }
 
