@@ -3,15 +3,17 @@
 //
 // One cluster of thread blocks per request, one launch, no workspace.  Every block of the cluster makes the acceptance
 // test of the whole window (at most 64 pairs of gathered probabilities); that gives the ONE row of P, and of Q, which
-// has to be read.  The row is cut into contiguous slices, one per warp of the cluster; a warp adds the weights of its
-// slice, the blocks exchange their sums through distributed shared memory, and the one warp whose slice holds the goal reads its
-// slice again (from L2) to find the token.  So the row crosses HBM once, and that is the bound: V (size(P) + size(Q))
-// bytes per request.
+// has to be read.  The row is cut into chunks of 512 tokens; a warp adds up the weights of a chunk and keeps the sum in shared
+// memory, the blocks exchange their totals through distributed shared memory, and the block whose chunks hold the
+// goal scans its sums and reads that one chunk again (from L2) to find the token.  So the row crosses HBM once, and that
+// is the bound: V (size(P) + size(Q)) bytes per request.
 //
-// Weights are integers (2^-44 units, 64-bit sums): addition is exact in any order, so the token depends neither on the number
-// of blocks nor on how the row was cut, and a row whose mass is spread over 2^18 tokens still leaves each token with
+// Weights are integers (2^-44 units): addition is exact in any order, so the token depends neither on the number of
+// blocks nor on how the row was cut, and a row whose mass is spread over 2^18 tokens still leaves each token with
 // the 24 bits that an fp32 probability of 2^-20 or more has.  A residual below 2^-44 has no weight; 2^18 of those would
-// be 1.5e-8 of the mass, less than the rounding of one fp32 probability.
+// be 1.5e-8 of the mass, less than the rounding of one fp32 probability.  In the inner loop a weight is a pair of integers below
+// 2^22 and 2^23 that two fused multiply-adds with rounding towards zero leave in the low bits of a float (adding 2^23
+// makes the spacing of floats 1): six full-rate instructions, where a conversion to 64 bits runs at an eighth of that rate.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -27,9 +29,13 @@ namespace {
 
 typedef unsigned long long u64;
 
-constexpr int kResThreads = 512;
+constexpr int kResThreads = 256;
 constexpr int kResWarps = kResThreads / 32;
-constexpr int kResMaxCluster = 8;
+constexpr int kResMaxCluster = 16;
+constexpr int kChunk = 512;                        // tokens whose weights a warp adds into one sum: 512 (2^23 - 1) < 2^32
+constexpr int kMaxChunks = WISV_STATIC_MAX_V / kChunk;
+constexpr int kChunksPerThread = kMaxChunks / kResThreads;
+constexpr int kResResident = 592;                  // blocks that run at once: four on each of 148 SMs
 constexpr float kFix = 17592186044416.0f;          // 2^44
 constexpr int kQuiet = 0, kDense = 1, kTop = 2;    // the drafter's distribution: one token, dense, a list
 
@@ -49,45 +55,81 @@ __device__ __forceinline__ float as_f(float x) { return x; }
 __device__ __forceinline__ float as_f(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float as_f(__half x) { return __half2float(x); }
 // a probability as the draw sees it: NaN and negative values 0, at most 1
-__device__ __forceinline__ float unit(float x) { return fminf(fmaxf(x, 0.0f), 1.0f); }
-__device__ __forceinline__ u64 fix(float x) { return __float2ull_rz(x * kFix); }
+__device__ __forceinline__ float unit(float x) { return __saturatef(x); }
 
-// E consecutive elements from v on; E = 8 needs 16-byte aligned rows.  Elements past V are 0.
-template <typename T, int E>
-__device__ __forceinline__ void load_probs(const T* row, int v, int V, float (&x)[E])
+// floor(2^44 x) of 0 <= x <= 1 as hi 2^23 + lo, both with a constant on top that the caller takes off: kHiBias and kLoBias
+constexpr unsigned kBias = 0x4B000000u;            // the bits of 2^23
+__device__ __forceinline__ void fix_parts(float x, unsigned& hi, unsigned& lo)
 {
-    if (E == 8 && v + 8 <= V) {
-        uint4 w[sizeof(T) / 2];
+    const float t = __fmaf_rz(x, 2097152.0f, 8388608.0f);                     // 2^23 + floor(2^21 x)
+    const float r = __fmaf_rn(x, 2097152.0f, 8388608.0f - t);                 // the rest, exact: 0 <= r < 1
+    hi = __float_as_uint(t);
+    lo = __float_as_uint(__fmaf_rz(r, 8388608.0f, 8388608.0f));               // 2^23 + floor(2^23 r)
+}
+__device__ __forceinline__ u64 fix(float x)
+{
+    unsigned hi, lo;
+    fix_parts(x, hi, lo);
+    return (static_cast<u64>(hi - kBias) << 23) + (lo - kBias);
+}
+
+// 16 of a chunk's 512 elements per lane, as they lie in memory.  kWide: two runs of 8 consecutive ones (16-byte aligned
+// rows), at 8 lane and 256 + 8 lane; otherwise every 32nd.  Elements past V are 0.
+template <typename T, bool kWide>
+struct Piece {
+    union { uint4 w[sizeof(T)]; unsigned raw[4 * sizeof(T)]; };               // 16 elements
+
+    __device__ __forceinline__ void load(const T* row, int v, int V, int lane)
+    {
 #pragma unroll
-        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(row + v) + i);
-        const T* e = reinterpret_cast<const T*>(w);
+        for (int h = 0; h < 2; ++h) {
+            constexpr int n = sizeof(T) / 2;                                  // 16-byte loads per run
+            const int at = v + h * 256 + lane * 8;
+            if (kWide && at + 8 <= V) {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = unit(as_f(e[i]));
-    } else {
+                for (int i = 0; i < n; ++i) w[h * n + i] = __ldg(reinterpret_cast<const uint4*>(row + at) + i);
+            } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = v + i < V ? unit(as_f(row[v + i])) : 0.0f;
+                for (int i = 0; i < 8; ++i) {
+                    const int x = kWide ? at + i : v + (8 * h + i) * 32 + lane;
+                    put(8 * h + i, x < V ? bits(row[x]) : 0u);
+                }
+            }
+        }
     }
-}
-
-__device__ __forceinline__ u64 warp_sum(u64 x)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-    return x;
-}
+    static __device__ __forceinline__ unsigned bits(float x) { return __float_as_uint(x); }
+    static __device__ __forceinline__ unsigned bits(__nv_bfloat16 x) { return __bfloat16_as_ushort(x); }
+    static __device__ __forceinline__ unsigned bits(__half x) { return __half_as_ushort(x); }
+    __device__ __forceinline__ void put(int i, unsigned x)
+    {
+        if (sizeof(T) == 4) raw[i] = x;
+        else raw[i / 2] = (i & 1) ? raw[i / 2] | (x << 16) : x;
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if (sizeof(T) == 4) return __uint_as_float(raw[i]);
+        const unsigned x = raw[i / 2];
+        if (is_bf16(static_cast<T*>(nullptr))) return __uint_as_float((i & 1) ? x & 0xffff0000u : x << 16);
+        return __half2float(__ushort_as_half(static_cast<unsigned short>((i & 1) ? x >> 16 : x & 0xffffu)));
+    }
+    static __device__ __forceinline__ bool is_bf16(const __nv_bfloat16*) { return true; }
+    static __device__ __forceinline__ bool is_bf16(const void*) { return false; }
+};
 
 __device__ __forceinline__ void st_cluster_u64(uint32_t addr, u64 x)
 {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(x) : "memory");
 }
 
-template <typename TP, typename TQ, int kForm, int E>
-__global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualParams p)
+template <typename TP, typename TQ, int kForm, bool kWide>
+__global__ void __launch_bounds__(kResThreads, 4) residual_kernel(const ResidualParams p)
 {
+    __shared__ u64 chunk_mass[kMaxChunks];
     __shared__ u64 warp_mass[kResWarps];
     __shared__ u64 block_mass[2][kResMaxCluster];          // written by every block of the cluster
     __shared__ unsigned ok_bits[2];
-    __shared__ int flag;
+    __shared__ int flag, found;
+    __shared__ u64 found_before;
     __shared__ int list_v[kForm == kTop ? WISV_MAX_TOP : 1];
     __shared__ float list_q[kForm == kTop ? WISV_MAX_TOP : 1];
     __shared__ long long list_d[kForm == kTop ? WISV_MAX_TOP : 1];
@@ -95,7 +137,7 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = static_cast<int>(cluster_ctarank());
     const int b = blockIdx.x / p.cluster;
-    if (tid == 0) { ok_bits[0] = ok_bits[1] = 0; flag = 0; }
+    if (tid == 0) { ok_bits[0] = ok_bits[1] = 0; flag = 0; found = -1; }
     cluster_arrive();                                      // waited for before the first store to another block
 
     // ---- the window: offsets come from the device, so every index made of them is clamped
@@ -103,11 +145,11 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
     if (p.k_off) {
         t0 = min(max(p.k_off[b], 0), p.T);
         K = min(max(p.k_off[b + 1], 0), p.T) - t0;
-        if (tid == 0 && (K < 0 || K > WISV_MAX_K)) flag = WISV_ST_BAD_WINDOW;
-        K = min(max(K, 0), WISV_MAX_K);
     } else {
         K = p.K; t0 = b * K;
     }
+    const bool bad_window = K < 0 || K > WISV_MAX_K;
+    K = min(max(K, 0), WISV_MAX_K);
     const TP* P0 = static_cast<const TP*>(p.P) + static_cast<int64_t>(t0 + b) * p.p_stride;
     auto draft_at = [&](int i) {
         const int y = p.tokens[t0 + i];
@@ -121,19 +163,21 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
         A = min(max(p.accept_in[b], 0), K);
     } else {
         if (kForm == kTop) {
-            for (int i = warp; i < K; i += kResWarps) {    // a warp looks one token up in its list
-                const int y = draft_at(i);
+            // eight lanes look one token up in its list
+            for (int i = tid >> 3; i < ((K + 3) & ~3); i += kResThreads / 8) {
+                const int k = min(i, K - 1);               // (whole warps take part in the shuffles)
+                const int y = draft_at(k);
+                const int64_t at = static_cast<int64_t>(t0 + k) * p.n_top, aq = static_cast<int64_t>(t0 + k) * p.q_stride;
+                const float a = unit(as_f(P0[static_cast<int64_t>(k) * p.p_stride + y]));
+                const float u = p.u[t0 + k];
                 float q = 0.0f;
-                for (int j = lane; j < p.n_top; j += 32) {
-                    const int64_t at = static_cast<int64_t>(t0 + i) * p.n_top + j;
-                    if (p.ids[at] == y) q += static_cast<const float*>(p.Q)[static_cast<int64_t>(t0 + i) * p.q_stride + j];
-                }
+#pragma unroll 4
+                for (int j = lane & 7; j < p.n_top; j += 8) q += p.ids[at + j] == y ? static_cast<const float*>(p.Q)[aq + j] : 0.0f;
 #pragma unroll
-                for (int o = 16; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
+                for (int o = 4; o; o >>= 1) q += __shfl_xor_sync(0xffffffffu, q, o);
                 q = unit(q);
-                const float a = unit(as_f(P0[static_cast<int64_t>(i) * p.p_stride + y]));
-                const bool ok = p.u[t0 + i] < (q > 0.0f ? fminf(a / q, 1.0f) : (a > 0.0f ? 1.0f : 0.0f));
-                if (lane == 0 && ok) atomicOr(&ok_bits[i >> 5], 1u << (i & 31));
+                if ((lane & 7) == 0 && i < K && u < (q > 0.0f ? fminf(a / q, 1.0f) : (a > 0.0f ? 1.0f : 0.0f)))
+                    atomicOr(&ok_bits[i >> 5], 1u << (i & 31));
             }
         } else if (tid < K) {
             const int y = draft_at(tid);
@@ -152,59 +196,60 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
     const TP* P = P0 + static_cast<int64_t>(A) * p.p_stride;
     const TQ* Q = kForm == kDense ? static_cast<const TQ*>(p.Q) + static_cast<int64_t>(t0 + A) * p.q_stride : nullptr;
     const int y = A < K ? draft_at(A) : -1;
-    const int m = static_cast<int>(fminf(unit(p.u_draw[b]) * 2147483648.0f, 2147483520.0f));
+    const unsigned m = static_cast<unsigned>(fminf(unit(p.u_draw[b]) * 2147483648.0f, 2147483520.0f));
+    if (kForm == kTop && A < K) {
+        for (int j = tid; j < p.n_top; j += kResThreads) {
+            const int v = p.ids[static_cast<int64_t>(t0 + A) * p.n_top + j];
+            list_v[j] = v >= 0 && v < p.V ? v : -1;
+            list_q[j] = static_cast<const float*>(p.Q)[static_cast<int64_t>(t0 + A) * p.q_stride + j];
+        }
+    }
 
-    // ---- slices: a warp owns `per` consecutive elements, a multiple of 32 * E
-    const int warps = p.cluster * kResWarps;
-    const int per = (p.V + warps * 32 * E - 1) / (warps * 32 * E) * (32 * E);
-    const int64_t at0 = static_cast<int64_t>(rank * kResWarps + warp) * per;
-    const int v0 = static_cast<int>(at0 < p.V ? at0 : p.V), v1 = min(v0 + per, p.V);
+    // ---- this block's chunks, a contiguous run of them
+    const int all = (p.V + kChunk - 1) / kChunk, per = (all + p.cluster - 1) / p.cluster;
+    const int first = min(rank * per, all), n_chunks = min(first + per, all) - first;
 
     for (int pass = 0; pass < 2; ++pass) {
         const bool rest = pass == 0 && A < K;              // the residual; then (or at once, for a bonus token) P alone
-        auto weights = [&](int v, u64 (&w)[E]) {
-            float a[E];
-            load_probs<TP, E>(P, v, p.V, a);
-            if (kForm == kDense && rest) {
-                float q[E];
-                load_probs<TQ, E>(Q, v, p.V, q);
-#pragma unroll
-                for (int i = 0; i < E; ++i) a[i] = fmaxf(a[i] - q[i], 0.0f);
-            }
-#pragma unroll
-            for (int i = 0; i < E; ++i) {
-                if (kForm == kQuiet && rest && v + i == y) a[i] = fmaxf(a[i] - 1.0f, 0.0f);
-                w[i] = fix(a[i]);
-            }
-        };
-        u64 sum = 0;
-        constexpr int U = E == 8 ? 2 : 8;
-        for (int v = v0 + lane * E; v < v1; v += 32 * E * U) {
-            u64 w[U][E];
+        auto residual = [&](float a, float q) { return kForm == kDense && rest ? __saturatef(unit(a) - unit(q)) : unit(a); };
+        // chunks whose loads are under way together: some 128 bytes per lane
+        constexpr int kBytes = static_cast<int>(sizeof(TP)) + (kForm == kDense ? static_cast<int>(sizeof(TQ)) : 0);
+        constexpr int U = kBytes <= 2 ? 4 : kBytes <= 4 ? 2 : 1;
+        for (int c0 = warp; c0 < n_chunks; c0 += U * kResWarps) {
+            Piece<TP, kWide> a[U];
+            Piece<TQ, kWide> q[kForm == kDense ? U : 1];
 #pragma unroll
             for (int s = 0; s < U; ++s) {
-                const int x = v + s * 32 * E;
-                if (x < v1) weights(x, w[s]);
-                else {
-#pragma unroll
-                    for (int i = 0; i < E; ++i) w[s][i] = 0;
+                const int c = c0 + s * kResWarps;
+                if (c < n_chunks) {
+                    a[s].load(P, (first + c) * kChunk, p.V, lane);
+                    if (kForm == kDense && rest) q[kForm == kDense ? s : 0].load(Q, (first + c) * kChunk, p.V, lane);
                 }
             }
 #pragma unroll
-            for (int s = 0; s < U; ++s)
+            for (int s = 0; s < U; ++s) {
+                const int c = c0 + s * kResWarps;
+                if (c >= n_chunks) break;
+                unsigned hi = 0, lo = 0;
 #pragma unroll
-                for (int i = 0; i < E; ++i) sum += w[s][i];
+                for (int i = 0; i < 16; ++i) {
+                    float x = residual(a[s].get(i), kForm == kDense ? q[kForm == kDense ? s : 0].get(i) : 0.0f);
+                    if (kForm == kQuiet && rest) {         // Q is 1 at the drafted token: nothing is left there
+                        const int v = (first + c) * kChunk + (kWide ? (i >> 3) * 256 + lane * 8 + (i & 7) : i * 32 + lane);
+                        x = v == y ? 0.0f : x;
+                    }
+                    unsigned h, l;
+                    fix_parts(x, h, l);
+                    hi += h; lo += l;
+                }
+                hi = __reduce_add_sync(0xffffffffu, hi - 16u * kBias);
+                lo = __reduce_add_sync(0xffffffffu, lo - 16u * kBias);
+                if (lane == 0) chunk_mass[c] = (static_cast<u64>(hi) << 23) + lo;
+            }
         }
-        sum = warp_sum(sum);
-        if (lane == 0) warp_mass[warp] = sum;
+        __syncthreads();
         if (kForm == kTop && rest) {
             // the listed tokens' weights, taken with Q = 0 above, are corrected by integers
-            for (int j = tid; j < p.n_top; j += kResThreads) {
-                const int v = p.ids[static_cast<int64_t>(t0 + A) * p.n_top + j];
-                list_v[j] = v >= 0 && v < p.V ? v : -1;
-                list_q[j] = static_cast<const float*>(p.Q)[static_cast<int64_t>(t0 + A) * p.q_stride + j];
-            }
-            __syncthreads();
             for (int j = tid; j < p.n_top; j += kResThreads) {
                 const int v = list_v[j];
                 float q = 0.0f;
@@ -212,23 +257,41 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
                 for (int k = 0; k < p.n_top; ++k)
                     if (list_v[k] == v) { if (k < j) head = false; q += list_q[k]; }
                 long long d = 0;
-                const int64_t slice = head ? v / per : -1;
                 if (head) {
                     const float a = unit(as_f(P[v]));
-                    d = static_cast<long long>(fix(fmaxf(a - unit(q), 0.0f))) - static_cast<long long>(fix(a));
+                    d = static_cast<long long>(fix(__saturatef(a - unit(q)))) - static_cast<long long>(fix(a));
+                    const int c = v / kChunk - first;
+                    if (c >= 0 && c < n_chunks) atomicAdd(&chunk_mass[c], static_cast<u64>(d));
                 }
                 list_d[j] = d;
-                if (slice / kResWarps == rank && head)
-                    atomicAdd(&warp_mass[slice % kResWarps], static_cast<u64>(d));
             }
+            __syncthreads();
         }
+        // ---- exclusive prefix sums over the block's chunks
+        u64 own[kChunksPerThread], sum = 0;
+#pragma unroll
+        for (int i = 0; i < kChunksPerThread; ++i) {
+            const int c = tid * kChunksPerThread + i;
+            own[i] = c < n_chunks ? chunk_mass[c] : 0;
+            sum += own[i];
+        }
+        u64 upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        if (lane == 31) warp_mass[warp] = upto;
         __syncthreads();
-        if (pass == 0) cluster_wait();                     // every block of the cluster is running
-        if (warp == 0) {
-            u64 x = lane < kResWarps ? warp_mass[lane] : 0;
-            x = warp_sum(x);
-            if (lane < p.cluster) st_cluster_u64(mapa_u32(smem_u32(&block_mass[pass][rank]), lane), x);
+        u64 total = 0;
+#pragma unroll
+        for (int w = 0; w < kResWarps; ++w) {
+            if (w < warp) upto += warp_mass[w];
+            total += warp_mass[w];
         }
+        if (pass == 0) cluster_wait();                     // every block of the cluster is running
+        if (tid < p.cluster) st_cluster_u64(mapa_u32(smem_u32(&block_mass[pass][rank]), tid), total);
+        __syncwarp();
         cluster_arrive();
         cluster_wait();
         u64 W = 0, before = 0;
@@ -240,62 +303,73 @@ __global__ void __launch_bounds__(kResThreads) residual_kernel(const ResidualPar
         if (rank == 0 && tid == 0) {
             p.accept_len[b] = A;
             if (p.mass) p.mass[b] = static_cast<float>(W) * (1.0f / kFix);
-            if (p.status) p.status[b] = flag | (W == 0 ? WISV_ST_NO_MASS : 0);
+            if (p.status) p.status[b] = flag | (bad_window ? WISV_ST_BAD_WINDOW : 0) | (W == 0 ? WISV_ST_NO_MASS : 0);
             if (W == 0) p.token[b] = -1;
         }
         if (W == 0) break;
-        const u64 mm = static_cast<u64>(m);
-        const u64 goal = (W >> 31) * mm + (((W & 0x7fffffffull) * mm) >> 31);
-        for (int k = 0; k < warp; ++k) before += warp_mass[k];
-        if (goal < before || goal >= before + warp_mass[warp]) break;
-        // ---- this warp's slice holds the goal: 32 * E elements at a time
-        for (int v = v0; v < v1; v += 32 * E) {
-            u64 w[E];
-            const int mine = v + lane * E;
-            if (mine < v1) weights(mine, w);
-            else {
+        const u64 goal = (W >> 31) * m + (((W & 0x7fffffffull) * m) >> 31);
+        if (goal < before || goal >= before + total) break;                   // another block's
+        u64 at = before + upto - sum;
 #pragma unroll
-                for (int i = 0; i < E; ++i) w[i] = 0;
+        for (int i = 0; i < kChunksPerThread; ++i) {
+            if (goal >= at && goal < at + own[i]) { found = tid * kChunksPerThread + i; found_before = at; }
+            at += own[i];
+        }
+        __syncthreads();
+        if (warp != 0) break;
+        // ---- the chunk that holds the goal: 16 consecutive tokens per lane
+        const int v0 = (first + found) * kChunk + lane * 16;
+        u64 w[16], s = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int v = v0 + i;
+            float x = 0.0f;
+            if (v < p.V) {
+                x = residual(as_f(P[v]), kForm == kDense && rest ? as_f(Q[v]) : 0.0f);
+                if (kForm == kQuiet && rest && v == y) x = 0.0f;
             }
-            if (kForm == kTop && rest) {
-                for (int j = 0; j < p.n_top; ++j) {
-                    const int x = list_v[j] - mine;
+            w[i] = fix(x);
+        }
+        if (kForm == kTop && rest) {
+            for (int j0 = 0; j0 < p.n_top; j0 += 32) {     // listed tokens of this chunk
+                const int x = j0 + lane < p.n_top ? list_v[j0 + lane] : -1;
+                unsigned hit = __ballot_sync(0xffffffffu, x >= 0 && x / kChunk == first + found);
+                while (hit) {
+                    const int j = j0 + __ffs(hit) - 1;
+                    hit &= hit - 1;
+                    const int e = list_v[j] - v0;
 #pragma unroll
-                    for (int i = 0; i < E; ++i) if (x == i) w[i] += static_cast<u64>(list_d[j]);
+                    for (int i = 0; i < 16; ++i) if (e == i) w[i] += static_cast<u64>(list_d[j]);
                 }
             }
-            u64 s = 0;
+        }
 #pragma unroll
-            for (int i = 0; i < E; ++i) s += w[i];
-            u64 upto = s;
+        for (int i = 0; i < 16; ++i) s += w[i];
+        u64 run = s;
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const u64 z = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += z;
+        for (int o = 1; o < 32; o <<= 1) {
+            const u64 x = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += x;
+        }
+        run += found_before;
+        if (goal < run && goal >= run - s) {
+            u64 c = run - s;
+            int tok = -1;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                c += w[i];
+                if (tok < 0 && c > goal) tok = v0 + i;
             }
-            const unsigned past = __ballot_sync(0xffffffffu, before + upto > goal);
-            if (past) {
-                if (lane == __ffs(past) - 1) {
-                    u64 c = before + upto - s;
-                    int tok = -1;
-#pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        c += w[i];
-                        if (tok < 0 && c > goal) tok = mine + i;
-                    }
-                    p.token[b] = tok;
-                }
-                break;
-            }
-            before += __shfl_sync(0xffffffffu, upto, 31);
+            p.token[b] = tok;
         }
         break;
     }
 }
 
-template <typename TP, typename TQ, int kForm, int E>
+template <typename TP, typename TQ, int kForm, bool kWide>
 int go(const ResidualParams& p, cudaStream_t st)
 {
+    auto kernel = residual_kernel<TP, TQ, kForm, kWide>;
     cudaLaunchConfig_t cfg;
     memset(&cfg, 0, sizeof cfg);
     cfg.gridDim = dim3((unsigned)(p.B * p.cluster));
@@ -308,32 +382,33 @@ int go(const ResidualParams& p, cudaStream_t st)
     attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, residual_kernel<TP, TQ, kForm, E>, p) != cudaSuccess) {
+    if ((p.cluster > 8 && cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+        cudaLaunchKernelEx(&cfg, kernel, p) != cudaSuccess) {
         (void)cudaGetLastError();
         return WISV_ECUDA;
     }
     return WISV_OK;
 }
 
-template <typename TP, int E>
+template <typename TP, bool kWide>
 int by_form(const wisv_residual* r, const ResidualParams& p, cudaStream_t st)
 {
-    if (!r->draft_probs) return go<TP, float, kQuiet, E>(p, st);
-    if (r->draft_ids) return go<TP, float, kTop, E>(p, st);
+    if (!r->draft_probs) return go<TP, float, kQuiet, kWide>(p, st);
+    if (r->draft_ids) return go<TP, float, kTop, kWide>(p, st);
     switch (r->draft_dtype) {
-        case WISV_DT_F32: return go<TP, float, kDense, E>(p, st);
-        case WISV_DT_BF16: return go<TP, __nv_bfloat16, kDense, E>(p, st);
-        default: return go<TP, __half, kDense, E>(p, st);
+        case WISV_DT_F32: return go<TP, float, kDense, kWide>(p, st);
+        case WISV_DT_BF16: return go<TP, __nv_bfloat16, kDense, kWide>(p, st);
+        default: return go<TP, __half, kDense, kWide>(p, st);
     }
 }
 
-template <int E>
+template <bool kWide>
 int by_target(const wisv_residual* r, const ResidualParams& p, cudaStream_t st)
 {
     switch (r->target_dtype) {
-        case WISV_DT_F32: return by_form<float, E>(r, p, st);
-        case WISV_DT_BF16: return by_form<__nv_bfloat16, E>(r, p, st);
-        default: return by_form<__half, E>(r, p, st);
+        case WISV_DT_F32: return by_form<float, kWide>(r, p, st);
+        case WISV_DT_BF16: return by_form<__nv_bfloat16, kWide>(r, p, st);
+        default: return by_form<__half, kWide>(r, p, st);
     }
 }
 
@@ -377,12 +452,15 @@ extern "C" int wisv_verify_residual(const wisv_residual* r, void* cuda_stream)
     if (major != 10) return WISV_EARCH;
     ResidualParams p;
     p.B = r->B; p.K = r->K; p.T = r->T_total; p.V = r->V; p.n_top = r->n_top;
+    // blocks per request: as many as can run at once (four per SM), so that a small batch uses the whole chip and a large one
+    // pays for the acceptance test and the exchange once per request
     p.cluster = kResMaxCluster;
+    while (p.cluster > 1 && (int64_t)p.B * p.cluster > kResResident) p.cluster >>= 1;
     p.k_off = r->k_off; p.P = r->target_probs; p.p_stride = r->target_stride;
     p.Q = r->draft_probs; p.q_stride = r->draft_stride; p.ids = r->draft_ids; p.tokens = r->draft_tokens;
     p.u = r->uniforms; p.u_draw = r->u_draw; p.accept_in = r->accept_in;
     p.accept_len = r->accept_len; p.token = r->token; p.status = r->status; p.mass = r->mass;
     const bool wide = rows_aligned(p.P, p.p_stride, ps, 16) && (!dense || rows_aligned(p.Q, p.q_stride, qs, 16));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return wide ? by_target<8>(r, p, st) : by_target<1>(r, p, st);
+    return wide ? by_target<true>(r, p, st) : by_target<false>(r, p, st);
 }

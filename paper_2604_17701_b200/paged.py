@@ -2,10 +2,11 @@
 from __future__ import annotations
 
 import ctypes as C
+import struct
 from dataclasses import dataclass
 from typing import Optional
 
-from .binding import DT_BF16, DT_F16, DT_F32, WisvError, _check, _ptr, load_library
+from .binding import DT_BF16, DT_F16, DT_F32, WisvError, _check, load_library
 
 
 class _CacheConfig(C.Structure):
@@ -50,6 +51,15 @@ class _Residual(C.Structure):
                 ("mass", C.c_void_p), ("status", C.c_void_p)]
 
 
+def _packer(cls):
+    """struct.Struct of a ctypes structure's layout: filling 25 fields takes 0.5 us that way, 4 us through ctypes."""
+    code = {C.c_int32: "i", C.c_int64: "q", C.c_void_p: "P", C.c_float: "f"}
+    s = struct.Struct("@" + "".join(code[t] for _, t in cls._fields_) + "0q")
+    assert s.size == C.sizeof(cls)
+    return s.pack
+
+
+_pack_layout, _pack_append, _pack_attend, _pack_residual = (_packer(c) for c in (_Layout, _Append, _Attend, _Residual))
 _declared = False
 
 
@@ -57,15 +67,12 @@ def _lib():
     global _declared
     lib = load_library()
     if not _declared:
-        P = C.c_void_p
-        for name, args in (("wisv_cache_create", [C.POINTER(_CacheConfig), C.POINTER(P)]),
-                           ("wisv_cache_destroy", [P]),
-                           ("wisv_cache_error", [P, P, C.POINTER(C.c_int32)]),
-                           ("wisv_cache_extend", [P, P, C.c_int32, C.c_int32, P, C.c_int32, C.POINTER(_Layout), P]),
-                           ("wisv_cache_commit", [P, P, C.c_int32, P, P, P]),
-                           ("wisv_cache_append", [P, C.POINTER(_Append), P]),
-                           ("wisv_cache_attend", [P, C.POINTER(_Attend), P]),
-                           ("wisv_verify_residual", [C.POINTER(_Residual), P])):
+        P, I = C.c_void_p, C.c_int32                           # argument blocks go as packed bytes
+        for name, args in (("wisv_cache_create", [C.POINTER(_CacheConfig), C.POINTER(P)]), ("wisv_cache_destroy", [P]),
+                           ("wisv_cache_error", [P, P, C.POINTER(I)]),
+                           ("wisv_cache_extend", [P, P, I, I, P, I, P, P]), ("wisv_cache_commit", [P, P, I, P, P, P]),
+                           ("wisv_cache_append", [P, P, P]), ("wisv_cache_attend", [P, P, P]),
+                           ("wisv_verify_residual", [P, P])):
             f = getattr(lib, name)
             f.restype, f.argtypes = C.c_int, args
         lib.wisv_cache_launch_count.restype = C.c_int64
@@ -74,10 +81,10 @@ def _lib():
     return lib
 
 
-def _ints(torch, device, what, t, dtype, *shape):
-    """A contiguous tensor of the documented type and at least the documented size, or ValueError."""
-    if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() < shape[0]:
-        raise ValueError("%s must be a contiguous %s tensor with %d entries on %s" % (what, dtype, shape[0], device))
+def _array(what, t, dtype, n, index):
+    """Address of a contiguous tensor of the documented type, at least the documented size and on device `index`."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n or t.get_device() != index:
+        raise ValueError("%s must be a contiguous %s tensor with %d entries on cuda:%d" % (what, dtype, n, index))
     return t.data_ptr()
 
 
@@ -86,12 +93,12 @@ def _row_stride(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _empty(torch, stream, *args, **kw):
+def _empty(torch, stream, shape, dtype, device):
     """torch.empty for a result that `stream` (None: the current one) writes."""
     if stream is None:
-        return torch.empty(*args, **kw)
+        return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(*args, **kw)
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 @dataclass
@@ -142,7 +149,11 @@ class PagedCache:
                                                       self.seq_len)))
         # the arrays whose addresses the block above holds
         self._owned = (self.free_list, self.n_free, self.block_table, self.n_blocks, self.seq_len)
-        self._pages_ref = C.byref(self._pages)
+        self._pages_at = C.addressof(self._pages)
+        self._index = self.device.index
+        self._row = (n_kv_heads, head_dim)
+        self._pool = (n_pages, page_size, n_kv_heads, head_dim)
+        self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 
     def close(self):
         if getattr(self, "_h", None):
@@ -157,35 +168,31 @@ class PagedCache:
             pass
 
     # ------------------------------------------------------------------ helpers
-    def _stream(self, stream):
-        return (stream if stream is not None else self._torch.cuda.current_stream(self.device)).cuda_stream
-
-    def _call(self, name, *args):
-        """One library call with this cache's device current."""
-        f = getattr(self.lib, name)
-        torch = self._torch
-        if torch.cuda.current_device() != self.device.index:
-            with torch.cuda.device(self.device):
-                rc = f(self._h, *args)
+    def _call(self, name, stream, *args):
+        """One library call with this cache's device current; the stream goes last."""
+        st = self._raw_stream(self._index) if stream is None else stream.cuda_stream
+        if self._current() != self._index:
+            with self._torch.cuda.device(self.device):
+                rc = getattr(self.lib, name)(self._h, *args, st)
         else:
-            rc = f(self._h, *args)
+            rc = getattr(self.lib, name)(self._h, *args, st)
         if rc:
             raise WisvError(rc, name)
 
-    def _check_rows(self, what, t, heads, rows=None):
+    def _rows(self, what, t, heads, rows=None):
         s = t.shape
-        if t.dtype is not self.dtype or len(s) != 3 or s[1] != heads or s[2] != self.head_dim or t.stride(2) != 1 or \
-                t.device != self.device or (rows is not None and s[0] != rows):
+        if t.dtype is not self.dtype or len(s) != 3 or s[1] != heads or s[2] != self.head_dim or \
+                (rows is not None and s[0] != rows) or t.get_device() != self._index or t.stride(2) != 1:
             raise ValueError("%s must be [%s, %d, %d] %s on %s with a head's elements contiguous" %
                              (what, "T" if rows is None else rows, heads, self.head_dim, self.dtype, self.device))
         return t.data_ptr(), t.stride(0), t.stride(1)
 
-    def _check_pool(self, what, t):
-        if t.dtype is not self.dtype or t.stride(3) != 1 or t.device != self.device or \
-                t.shape != (self.n_pages, self.page_size, self.n_kv_heads, self.head_dim):
-            raise ValueError("%s must be [%d, %d, %d, %d] %s on %s with a head's elements contiguous" %
-                             (what, self.n_pages, self.page_size, self.n_kv_heads, self.head_dim, self.dtype, self.device))
+    def _pages_of(self, what, t):
+        if t.dtype is not self.dtype or t.shape != self._pool or t.get_device() != self._index:
+            raise ValueError("%s must be [%d, %d, %d, %d] %s on %s" % ((what,) + self._pool + (self.dtype, self.device)))
         st = t.stride()
+        if st[3] != 1:
+            raise ValueError("%s must keep a head's elements contiguous" % what)
         return t.data_ptr(), st[0], st[1], st[2]
 
     # ------------------------------------------------------------------ calls
@@ -193,87 +200,81 @@ class PagedCache:
                stream=None) -> WindowLayout:
         """wisv_cache_extend: pages, slots and positions for n_new tokens per request (an int, or int32 [B] on the
         device with their sum T given)."""
-        torch = self._torch
+        torch, dev = self._torch, self._index
+        i32, i64 = torch.int32, torch.int64
         uniform = isinstance(n_new, int)
         if T is None:
             if not uniform:
                 raise ValueError("T, the sum of n_new, must be given where n_new lives on the device")
             T = B * n_new
-        ptr = None if uniform else _ints(torch, self.device, "n_new", n_new, torch.int32, B)
+        ptr = None if uniform else _array("n_new", n_new, i32, B, dev)
         if out is None:
-            # one allocation for the int32 arrays
-            buf = _empty(torch, stream, 3 * B + 1 + T, dtype=torch.int32, device=self.device)
-            out = WindowLayout(buf[:B + 1], buf[B + 1:2 * B + 1],
-                               _empty(torch, stream, T, dtype=torch.int64, device=self.device), buf[3 * B + 1:], buf[2 * B + 1:3 * B + 1])
-        else:
-            i32 = torch.int32
-            _ints(torch, self.device, "out.q_off", out.q_off, i32, B + 1)
-            _ints(torch, self.device, "out.kv_len", out.kv_len, i32, B)
-            _ints(torch, self.device, "out.positions", out.positions, i32, T)
-            _ints(torch, self.device, "out.slot_map", out.slot_map, torch.int64, T)
-            if out.status is not None:
-                _ints(torch, self.device, "out.status", out.status, i32, B)
-        lay = _Layout(out.q_off.data_ptr(), out.kv_len.data_ptr(), out.slot_map.data_ptr(), out.positions.data_ptr(),
-                      _ptr(out.status))
-        self._call("wisv_cache_extend", self._pages_ref, B, T, ptr, n_new if uniform else 0, C.byref(lay),
-                   self._stream(stream))
+            # one allocation for the int32 arrays, one for the slots
+            q_off, kv_len, status, positions = _empty(torch, stream, 3 * B + 1 + T, i32, self.device).split_with_sizes(
+                (B + 1, B, B, T))
+            out = WindowLayout(q_off, kv_len, _empty(torch, stream, T, i64, self.device), positions, status)
+        lay = _pack_layout(_array("out.q_off", out.q_off, i32, B + 1, dev), _array("out.kv_len", out.kv_len, i32, B, dev),
+                           _array("out.slot_map", out.slot_map, i64, T, dev),
+                           _array("out.positions", out.positions, i32, T, dev),
+                           0 if out.status is None else _array("out.status", out.status, i32, B, dev))
+        self._call("wisv_cache_extend", stream, self._pages_at, B, T, ptr, n_new if uniform else 0, lay)
         return out
 
     def commit(self, new_len, *, B: int, status=None, stream=None):
         """wisv_cache_commit: the kept length of each request (int32 [B]); pages behind it go back.  Returns status."""
-        torch = self._torch
-        ptr = _ints(torch, self.device, "new_len", new_len, torch.int32, B)
+        i32 = self._torch.int32
         if status is None:
-            status = _empty(torch, stream, B, dtype=torch.int32, device=self.device)
-        else:
-            _ints(torch, self.device, "status", status, torch.int32, B)
-        self._call("wisv_cache_commit", self._pages_ref, B, ptr, status.data_ptr(), self._stream(stream))
+            status = _empty(self._torch, stream, B, i32, self.device)
+        self._call("wisv_cache_commit", stream, self._pages_at, B, _array("new_len", new_len, i32, B, self._index),
+                   _array("status", status, i32, B, self._index))
         return status
 
     def append(self, k, v, k_pages, v_pages, slot_map, *, stream=None):
         """wisv_cache_append: one layer's new keys and values [T, n_kv_heads, head_dim] into their slots."""
         T = k.shape[0]
-        kp, kt, kh = self._check_rows("k", k, self.n_kv_heads)
-        vp, vt, vh = self._check_rows("v", v, self.n_kv_heads, T)
-        kpool, k0, k1, k2 = self._check_pool("k_pages", k_pages)
-        vpool, v0, v1, v2 = self._check_pool("v_pages", v_pages)
-        a = _Append(T, kp, vp, kt, kh, vt, vh, kpool, vpool, k0, k1, k2, v0, v1, v2,
-                    _ints(self._torch, self.device, "slot_map", slot_map, self._torch.int64, T))
-        self._call("wisv_cache_append", C.byref(a), self._stream(stream))
+        kp, kt, kh = self._rows("k", k, self.n_kv_heads)
+        vp, vt, vh = self._rows("v", v, self.n_kv_heads, T)
+        kpool, k0, k1, k2 = self._pages_of("k_pages", k_pages)
+        vpool, v0, v1, v2 = self._pages_of("v_pages", v_pages)
+        self._call("wisv_cache_append", stream,
+                   _pack_append(T, kp, vp, kt, kh, vt, vh, kpool, vpool, k0, k1, k2, v0, v1, v2,
+                                _array("slot_map", slot_map, self._torch.int64, T, self._index)))
 
     def attend(self, q, k_pages, v_pages, kv_len, *, B: int, max_new: int, q_off=None, out=None, lse=None,
                scale: Optional[float] = None, block_table=None, stream=None):
         """wisv_cache_attend: attention of the new rows q [T, n_heads, head_dim] over the cache, causal among
         themselves.  kv_len: int32 [B], new tokens included; q_off: int32 [B+1], or None for max_new rows each."""
-        torch = self._torch
+        torch, dev = self._torch, self._index
         i32 = torch.int32
-        qp, qt, qh = self._check_rows("q", q, self.n_heads)
+        qp, qt, qh = self._rows("q", q, self.n_heads)
         T = q.shape[0]
-        kpool, k0, k1, k2 = self._check_pool("k_pages", k_pages)
-        vpool, v0, v1, v2 = self._check_pool("v_pages", v_pages)
+        kpool, k0, k1, k2 = self._pages_of("k_pages", k_pages)
+        vpool, v0, v1, v2 = self._pages_of("v_pages", v_pages)
         if out is None:
-            out = _empty(torch, stream, (T, self.n_heads, self.head_dim), dtype=self.dtype, device=self.device)
-        op, ot, oh = self._check_rows("out", out, self.n_heads, T)
+            out = _empty(torch, stream, (T, self.n_heads, self.head_dim), self.dtype, self.device)
+        op, ot, oh = self._rows("out", out, self.n_heads, T)
         if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, self.n_heads) or
-                                not lse.is_contiguous() or lse.device != self.device):
+                                not lse.is_contiguous() or lse.get_device() != dev):
             raise ValueError("lse must be a contiguous float32 [T, n_heads] tensor")
         if scale is not None and not scale > 0:
             raise ValueError("scale must be positive")
-        table = self.block_table if block_table is None else block_table
-        if table is not self.block_table and (table.dtype is not i32 or table.dim() != 2 or table.shape[0] < B or
-                                              table.stride(1) != 1 or table.device != self.device):
-            raise ValueError("block_table must be int32 [B, blocks] on %s" % self.device)
-        a = _Attend(B, T, max_new,
-                    None if q_off is None else _ints(torch, self.device, "q_off", q_off, i32, B + 1),
-                    _ints(torch, self.device, "kv_len", kv_len, i32, B), table.data_ptr(),
-                    _row_stride(table), table.shape[1], qp, qt, qh, kpool, vpool, k0, k1, k2, v0, v1, v2,
-                    op, ot, oh, _ptr(lse), 0.0 if scale is None else scale)
-        self._call("wisv_cache_attend", C.byref(a), self._stream(stream))
+        table, blocks, step = self.block_table, self.max_blocks, self.max_blocks
+        if block_table is not None:
+            table = block_table
+            if table.dtype is not i32 or table.dim() != 2 or table.shape[0] < B or table.stride(1) != 1 or table.get_device() != dev:
+                raise ValueError("block_table must be int32 [B, blocks] on %s" % self.device)
+            blocks, step = table.shape[1], _row_stride(table)
+        self._call("wisv_cache_attend", stream,
+                   _pack_attend(B, T, max_new, 0 if q_off is None else _array("q_off", q_off, i32, B + 1, dev),
+                                _array("kv_len", kv_len, i32, B, dev), table.data_ptr(), step, blocks, qp, qt, qh,
+                                kpool, vpool, k0, k1, k2, v0, v1, v2, op, ot, oh, 0 if lse is None else lse.data_ptr(),
+                                0.0 if scale is None else scale))
         return out
 
     def device_error(self) -> int:
         v = C.c_int32(0)
-        self._call("wisv_cache_error", self._stream(None), C.byref(v))
+        with self._torch.cuda.device(self.device):
+            _check(self.lib.wisv_cache_error(self._h, self._raw_stream(self._index), C.byref(v)), "wisv_cache_error")
         return v.value
 
     def launch_count(self) -> int:
@@ -289,7 +290,8 @@ class ResidualOutput:
 
 
 def _probs_dtype(torch, t) -> int:
-    code = {torch.float32: DT_F32, torch.bfloat16: DT_BF16, torch.float16: DT_F16}.get(t.dtype)
+    dt = t.dtype
+    code = DT_F32 if dt is torch.float32 else DT_BF16 if dt is torch.bfloat16 else DT_F16 if dt is torch.float16 else None
     if code is None or t.dim() != 2 or t.stride(1) != 1:
         raise ValueError("probabilities must be 2-D float32, bfloat16 or float16 tensors with contiguous rows")
     return code
@@ -307,48 +309,47 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
     """
     import torch
     lib = _lib()
-    device = target_probs.device
+    dev, i32, f32 = target_probs.get_device(), torch.int32, torch.float32
+    if dev < 0:
+        raise ValueError("target_probs must be a CUDA tensor")
     if T is None:
         T = B * K if k_off is None else draft_tokens.shape[0]
     tdt = _probs_dtype(torch, target_probs)
-    if target_probs.shape[0] < T + B:
+    rows, V = target_probs.shape
+    if rows < T + B:
         raise ValueError("target_probs must have T + B rows")
-    V = target_probs.shape[1]
-    qp, qs, qdt, n_top, ids = None, 0, DT_F32, 0, None
+    qp, qs, qdt, n_top, ids = 0, 0, DT_F32, 0, 0
     if draft_probs is not None:
         qdt = _probs_dtype(torch, draft_probs)
-        if draft_probs.shape[0] < T or draft_probs.device != device:
+        n, width = draft_probs.shape
+        if n < T or draft_probs.get_device() != dev:
             raise ValueError("draft_probs must have T rows on the target's device")
         qp, qs = draft_probs.data_ptr(), _row_stride(draft_probs)
         if draft_ids is not None:
             if qdt != DT_F32 or draft_ids.shape != draft_probs.shape:
                 raise ValueError("listed draft_probs are float32 and of draft_ids' shape")
-            n_top = draft_ids.shape[1]
-            ids = _ints(torch, device, "draft_ids", draft_ids, torch.int32, T * n_top)
-        elif draft_probs.shape[1] != V:
+            n_top = width
+            ids = _array("draft_ids", draft_ids, i32, T * n_top, dev)
+        elif width != V:
             raise ValueError("dense draft_probs must have the target's vocabulary")
     elif draft_ids is not None:
         raise ValueError("draft_ids without draft_probs")
     if out is None:
-        buf = _empty(torch, stream, 3 * B, dtype=torch.int32, device=device)
-        out = ResidualOutput(buf[:B], buf[B:2 * B], _empty(torch, stream, B, dtype=torch.float32, device=device), buf[2 * B:])
+        a, t, m, st = _empty(torch, stream, (4, B), i32, target_probs.device).unbind()
+        out = ResidualOutput(a, t, m.view(f32), st)
+    r = _pack_residual(B, 0 if k_off is not None else K, 0 if k_off is None else _array("k_off", k_off, i32, B + 1, dev), T, V,
+                       target_probs.data_ptr(), _row_stride(target_probs), tdt,
+                       _array("draft_tokens", draft_tokens, i32, T, dev), qp, qs, qdt, ids, n_top,
+                       0 if uniforms is None else _array("uniforms", uniforms, f32, T, dev),
+                       _array("u_draw", u_draw, f32, B, dev),
+                       0 if accept_len is None else _array("accept_len", accept_len, i32, B, dev),
+                       _array("out.accept_len", out.accept_len, i32, B, dev), _array("out.token", out.token, i32, B, dev),
+                       0 if out.mass is None else _array("out.mass", out.mass, f32, B, dev),
+                       0 if out.status is None else _array("out.status", out.status, i32, B, dev))
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            _check(lib.wisv_verify_residual(r, s), "wisv_verify_residual")
     else:
-        for name, t, dt in (("accept_len", out.accept_len, torch.int32), ("token", out.token, torch.int32),
-                            ("mass", out.mass, torch.float32), ("status", out.status, torch.int32)):
-            if t is not None:
-                _ints(torch, device, "out." + name, t, dt, B)
-    r = _Residual(B, 0 if k_off is not None else K,
-                  None if k_off is None else _ints(torch, device, "k_off", k_off, torch.int32, B + 1), T, V,
-                  target_probs.data_ptr(), _row_stride(target_probs), tdt,
-                  _ints(torch, device, "draft_tokens", draft_tokens, torch.int32, T), qp, qs, qdt,
-                  ids, n_top, None if uniforms is None else _ints(torch, device, "uniforms", uniforms, torch.float32, T),
-                  _ints(torch, device, "u_draw", u_draw, torch.float32, B),
-                  None if accept_len is None else _ints(torch, device, "accept_len", accept_len, torch.int32, B),
-                  out.accept_len.data_ptr(), out.token.data_ptr(), _ptr(out.mass), _ptr(out.status))
-    st = (stream if stream is not None else torch.cuda.current_stream(device)).cuda_stream
-    if torch.cuda.current_device() != device.index:
-        with torch.cuda.device(device):
-            _check(lib.wisv_verify_residual(C.byref(r), st), "wisv_verify_residual")
-    else:
-        _check(lib.wisv_verify_residual(C.byref(r), st), "wisv_verify_residual")
+        _check(lib.wisv_verify_residual(r, s), "wisv_verify_residual")
     return out
