@@ -11,12 +11,12 @@
 // keys at D = 128) is faster than its 64 KB of keys and values (some 2800 clocks at a 148th of the measured copy
 // rate).  Prompt chunks are bound by the MMAs and by the exponentials, 1024 clocks each per 128 x 128 tile.
 //
-// Roles.  One block per SM, persistent: a TMA warp, an MMA warp and two softmax warpgroups, each with its own S and O in
-// TMEM (all 512 columns).  A work item is either "paired" - two row tiles of
-// the same (request, key head), one per warpgroup, sharing each tile of keys - or, where a single row tile is left, "split":
-// the warpgroups take the key tiles in turn and merge at the end.  Either way the jobs (row tile, key tile) alternate
-// between the two warpgroups, and the MMA warp issues S of job j + 2 behind O of job j, so one warpgroup's
-// exponentials run under the other's MMAs.
+// Roles.  One block per SM, persistent: a warp that walks the work and issues the TMA copies, two warps that issue the MMAs,
+// and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
+// "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
+// single row tile is left, "split": the slots take the key tiles in turn and are put together at the end.  Either way
+// the jobs (row tile, key tile) alternate between the slots, and the MMA warp issues S of job j + 2 behind O of job j,
+// so one slot's exponentials run under the other's MMAs.
 //
 // Work split.  The key tiles of all items form one line, cut into equal contiguous ranges, one per block; every block finds
 // its range from the lengths on the device, so the host knows no lengths and a captured graph stays balanced.  An item cut by a
@@ -37,11 +37,12 @@ namespace wisv {
 
 constexpr int kAttnThreads = 384;
 constexpr int kAttnTile = 128;                   // rows of a row tile, keys of a key tile
+constexpr int kAttnSub = 64;                     // keys of a job
 constexpr int kAttnMaxStages = 12;
 constexpr int kAttnItemCost = 1;                 // key tiles that starting and finishing an item is worth
 constexpr int kAttnSmem = 232448;                // all of an SM's shared memory that a block can have
-constexpr int kAttnSmall = 2624;                 // barriers, the warpgroups' exchange of m and l
-constexpr int kAttnSlack = 448;                  // for aligning the tiles to 1024 bytes
+constexpr int kAttnSmall = 2816;                 // barriers, the queue of stretches, the slots' exchange of m and l
+constexpr int kAttnSlack = 256;                  // for aligning the tiles to 1024 bytes
 constexpr uint64_t kAttnWaitClocks = 4000000000ull;
 
 struct AttnParams {
@@ -76,11 +77,89 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
 template <typename E> struct is_bf16 { static constexpr bool value = false; };
 template <> struct is_bf16<__nv_bfloat16> { static constexpr bool value = true; };
 
+// 2^x by the hardware approximation (relative error 2^-22)
 __device__ __forceinline__ float attn_ex2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Bounded wait; `flag` is the shared-memory address of the block's abort flag.  One inline try and everything else out of
+// line: a try that is the condition of an inline loop costs some 370 clocks even where the barrier is complete.
+static __device__ __noinline__ bool attn_wait_slow(uint32_t bar, uint32_t parity, uint32_t flag)
+{
+    const long long t0 = clock64();
+    uint32_t n = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        if ((++n & 0xFFu) == 0) {
+            uint32_t stop;
+            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(stop) : "r"(flag) : "memory");
+            if (stop != 0) return false;
+            if (static_cast<uint64_t>(clock64() - t0) > kAttnWaitClocks) {
+                asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(flag), "r"(1) : "memory");
+                return false;
+            }
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, uint32_t flag)
+{
+    if (mbar_try_wait(bar, parity)) return true;
+    return attn_wait_slow(bar, parity, flag);
+}
+// the same for a warp that acts as one
+__device__ __forceinline__ bool attn_wait_warp(uint32_t bar, uint32_t parity, uint32_t flag)
+{
+    return __all_sync(0xffffffffu, attn_wait(bar, parity, flag));
+}
+
+// ---- pairs of floats: one instruction does two multiply-adds
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float low(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x)); }
+__device__ __forceinline__ float high(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of a pair by multiply-adds, for x <= 8 (below -126 as at -126): the nearest whole number goes to the exponent, the rest
+// r in [-1/2, 1/2] through the degree-4 polynomial with the least relative error there (2.6e-6; fitted by Remez's exchange).
+// The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both
+// matrix products; kAttnPoly of every 8 pairs go this way instead.
+constexpr int kAttnPoly = 0;
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x)
+{
+    const uint64_t magic = pair(12582912.0f, 12582912.0f), unmagic = pair(-12582912.0f, -12582912.0f);
+    x = pair(fmaxf(low(x), -126.0f), fmaxf(high(x), -126.0f));
+    const uint64_t t = add2(x, magic);                       // the whole number in the low bits
+    const uint64_t r = fma2(add2(t, unmagic), pair(-1.0f, -1.0f), x);
+    uint64_t y = fma2(r, pair(9.570102207e-3f, 9.570102207e-3f), pair(5.591785908e-2f, 5.591785908e-2f));
+    y = fma2(y, r, pair(2.402474433e-1f, 2.402474433e-1f));
+    y = fma2(y, r, pair(6.931217909e-1f, 6.931217909e-1f));
+    y = fma2(y, r, pair(9.999992847e-1f, 9.999992847e-1f));
+    const uint32_t a = static_cast<uint32_t>(t) * 0x800000u + static_cast<uint32_t>(y);
+    const uint32_t b = static_cast<uint32_t>(t >> 32) * 0x800000u + static_cast<uint32_t>(y >> 32);
+    return pair(__uint_as_float(a), __uint_as_float(b));
 }
 
 // ---------------------------------------------------------------- instructions that only this kernel needs
@@ -175,15 +254,17 @@ __device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnReq& r,
     return last_key < 0 ? 1 : last_key / kAttnTile + 1;
 }
 
-// A stretch of one item's key tiles that this block works on
-struct AttnSeg {
-    int b, kvh, q0, tok0, lim0, kv;              // first row of the item in q; last key that its first token sees
-    int rows[2];                                 // valid rows of its row tiles (rows[1] = 0: split)
-    int t0, t1, nt;
-    bool paired;
-    __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == nt; }
-    __device__ __forceinline__ int jobs() const { return paired ? 2 * (t1 - t0) : t1 - t0; }
+// A stretch of one item's key tiles that this block works on, as the walking warp queues it for the others: 16 words
+enum {
+    kSegJobs,                                    // 0: the end
+    kSegPaired, kSegT0, kSegT1, kSegTiles,       // key tiles [t0, t1) of the item's kSegTiles
+    kSegKeys,                                    // keys of the request
+    kSegLimit,                                   // last key that the item's first token sees
+    kSegRow, kSegHead,                           // first row of the item in q, key head
+    kSegRows0, kSegRows1,                        // valid rows of its row tiles
+    kSegReq, kSegWords = 16
 };
+constexpr int kSegQueue = 4;
 
 struct AttnWalk {
     int b, kvh, it, pos, units;                  // position on the line of key tiles, and what is left of the range
@@ -194,7 +275,8 @@ struct AttnWalk {
         b = s[0]; kvh = s[1]; it = s[2]; pos = s[3]; units = s[4];
         if (units > 0) r = attn_request(p, b);
     }
-    __device__ __forceinline__ bool next(const AttnParams& p, AttnSeg& s)
+    // The next stretch; false at the end of the range.
+    __device__ __forceinline__ bool next(const AttnParams& p, int (&s)[kSegWords])
     {
         while (units > 0) {
             if (it >= r.items) {                 // (a request without rows)
@@ -203,24 +285,22 @@ struct AttnWalk {
                 r = attn_request(p, b);
                 continue;
             }
-            s.nt = attn_tiles(p, r, it);
-            const int take = min(units, s.nt + kAttnItemCost - pos);
-            s.t0 = pos;
-            s.t1 = min(s.nt, pos + take);
-            const bool some = s.t1 > s.t0;
-            if (some) {
-                s.b = b; s.kvh = kvh; s.kv = r.kv;
-                s.tok0 = it * 2 * p.tpt;
-                s.q0 = r.q0 + s.tok0;
-                s.lim0 = r.kv - r.n + s.tok0;
-                const int left = r.n - s.tok0;
-                s.paired = left > p.tpt;
-                s.rows[0] = min(left, p.tpt) * p.group;
-                s.rows[1] = s.paired ? min(left - p.tpt, p.tpt) * p.group : 0;
+            const int nt = attn_tiles(p, r, it);
+            const int take = min(units, nt + kAttnItemCost - pos);
+            const int t0 = pos, t1 = min(nt, pos + take);
+            if (t1 > t0) {
+                const int tok0 = it * 2 * p.tpt, left = r.n - tok0;
+                const bool paired = left > p.tpt;
+                s[kSegJobs] = (paired ? 4 : 2) * (t1 - t0);
+                s[kSegPaired] = paired; s[kSegT0] = t0; s[kSegT1] = t1; s[kSegTiles] = nt;
+                s[kSegKeys] = r.kv; s[kSegLimit] = r.kv - r.n + tok0;
+                s[kSegRow] = r.q0 + tok0; s[kSegHead] = kvh; s[kSegReq] = b;
+                s[kSegRows0] = min(left, p.tpt) * p.group;
+                s[kSegRows1] = paired ? min(left - p.tpt, p.tpt) * p.group : 0;
             }
             units -= take;
             pos += take;
-            if (pos == s.nt + kAttnItemCost) {
+            if (pos == nt + kAttnItemCost) {
                 pos = 0;
                 if (++it == r.items) {
                     it = 0;
@@ -231,7 +311,7 @@ struct AttnWalk {
                     }
                 }
             }
-            if (some) return true;
+            if (t1 > t0) return true;
         }
         return false;
     }
@@ -274,15 +354,22 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     auto empty_bar = [&](int s) { return bars + 8u * (kAttnMaxStages + s); };
     auto q_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + s); };
     auto q_empty = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 2 + s); };
-    auto s_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 4 + s); };
-    auto p_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 6 + s); };
-    const uint32_t o_full = bars + 8u * (2 * kAttnMaxStages + 8);
-    const uint32_t o_empty = o_full + 8, ml_full = o_full + 16, drain = o_full + 24;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (2 * kAttnMaxStages + 12));
+    auto s_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 4 + s); };            // 2 slot + half of its S columns
+    auto p_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 8 + s); };
+    auto s_free = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 12 + s); };           // the second product has read P there
+    auto seg_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 16 + s); };
+    auto seg_empty = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 16 + kSegQueue + s); };
+    constexpr int kBars = 2 * kAttnMaxStages + 16 + 2 * kSegQueue;
+    const uint32_t o_full = bars + 8u * kBars, o_empty = o_full + 8, ml_full = o_full + 16, drain = o_full + 24;
+    constexpr int kSegAt = (kBars + 10) * 8;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 5));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);       // [0] abort, [1] drain scratch
+    const uint32_t flag = bars + 8u * (kBars + 5) + 4u;
     int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range
-    long long* totals = reinterpret_cast<long long*>(small + 432);                   // [12] scan over the warps
-    float2* ml = reinterpret_cast<float2*>(small + 544);                             // [2][128]
+    int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
+    float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
+    long long* totals = reinterpret_cast<long long*>(ml);                            // [20] scan over the warps, before that
+    static_assert(kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int lane = threadIdx.x & 31;
@@ -293,10 +380,10 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1); mbar_init(s_full(s), 1); mbar_init(p_full(s), 4);
-        }
-        mbar_init(o_full, 1); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(drain, 1);
+        for (int s = 0; s < 2; ++s) { mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1); }
+        for (int s = 0; s < 4; ++s) { mbar_init(s_full(s), 1); mbar_init(p_full(s), 4); mbar_init(s_free(s), 1); }
+        for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 9); }
+        mbar_init(o_full, 1); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(drain, 1); mbar_init(drain + 8, 1);
         abort_flag[0] = 0; abort_flag[1] = 0;
         for (int i = 0; i < 5; ++i) start[i] = 0;
         fence_barrier_init();
@@ -367,37 +454,49 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
         __syncthreads();
     }
-    const uint32_t tmem = *tmem_slot;
-    const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P in the upper half of it, O at 256 + 128 s
-    AttnWalk walk;
-    walk.start(p, start);
-    AttnSeg seg;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P over its first half, O at 256 + 128 s
     long long issued = 0;                        // ring entries filled (producer warp; read again before the end)
     int q_issued = 0;
 
     if (warp < 4) {
         if (warp == 0) {
-            // ------------------------------------------------------------ TMA
+            // ------------------------------------------------------------ the work, and its TMA copies
+            AttnWalk walk;
+            walk.start(p, start);
+            int s[kSegWords];
             AttnRing rg;
-            bool ok = true;
+            bool ok = true, described = false;
             const int box_tok = min(1 << p.page_shift, kAttnTile);
-            while (ok && walk.next(p, seg)) {
+            const uint32_t box_bytes = static_cast<uint32_t>(box_tok) * (D * 2);
+            for (int item = 0; ok; ++item) {
+                const bool some = walk.next(p, s);
+                const int qi = item & (kSegQueue - 1);
+                ok = attn_wait_warp(seg_empty(qi), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
+                if (!ok) break;
+                if (lane == 0) {
+#pragma unroll
+                    for (int i = 0; i < kSegReq; ++i) queue[qi][i] = some ? s[i] : 0;
+                    mbar_arrive(seg_full(qi));
+                }
+                __syncwarp();
+                if (!some) break;
                 // queries: one buffer per row tile
-                for (int t = 0; ok && t < (seg.paired ? 2 : 1); ++t, ++q_issued) {
+                for (int t = 0; ok && t < (s[kSegPaired] ? 2 : 1); ++t, ++q_issued) {
                     const int qb = q_issued & 1;
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(q_empty(qb), ((q_issued >> 1) & 1u) ^ 1u, abort_flag, kAttnWaitClocks));
+                    ok = attn_wait_warp(q_empty(qb), ((q_issued >> 1) & 1u) ^ 1u, flag);
                     if (ok && elect_one()) {
                         mbar_expect_tx(q_full(qb), static_cast<uint32_t>(p.tpt * p.group) * 128u * kHalves);
                         for (int h = 0; h < kHalves; ++h)
-                            tma_load_5d(q_buf + qb * kStage + h * (kAttnTile * 128), &tmQ, 0, 0, seg.q0 + t * p.tpt, h, seg.kvh, q_full(qb));
+                            tma_load_5d(q_buf + qb * kStage + h * (kAttnTile * 128), &tmQ, 0, 0, s[kSegRow] + t * p.tpt, h, s[kSegHead], q_full(qb));
                     }
                     __syncwarp();
                 }
-                const int32_t* table = p.block_table + seg.b * p.table_stride;
-                for (int t = seg.t0; ok && t < seg.t1; ++t) {
+                const int32_t* table = p.block_table + s[kSegReq] * p.table_stride;
+                for (int t = s[kSegT0]; ok && t < s[kSegT1]; ++t) {
                     // this tile's pages: lane i holds the i-th one's first token group, for keys and for values
                     const int tok0 = t * kAttnTile;
-                    const int have = min(seg.kv - tok0, kAttnTile);       // keys that exist
+                    const int have = min(s[kSegKeys] - tok0, kAttnTile);             // keys that exist
                     const int pages = have <= 0 ? 0 : (have + box_tok - 1) / box_tok;
                     int gk = p.groups_k, gv = p.groups_v;
                     if (lane < pages) {
@@ -410,171 +509,178 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                         }
                     }
                     for (int kv = 0; ok && kv < 2; ++kv) {
-                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty_bar(rg.s), rg.ph ^ 1u, abort_flag, kAttnWaitClocks));
+                        ok = attn_wait_warp(empty_bar(rg.s), rg.ph ^ 1u, flag);
                         if (!ok) break;
                         const uint32_t dst = ring + rg.s * kStage, bar = full_bar(rg.s);
-                        const uint32_t box_bytes = static_cast<uint32_t>(box_tok) * (D * 2);
                         if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(pages) * box_bytes);
                         __syncwarp();
                         for (int i = 0; i < pages; ++i) {
                             const int g = __shfl_sync(0xffffffffu, kv ? gv : gk, i);
-                            if (elect_one()) tma_load_5d(dst + i * box_bytes, kv ? &tmV : &tmK, 0, 0, 0, seg.kvh, g, bar);
+                            if (elect_one()) tma_load_5d(dst + i * box_bytes, kv ? &tmV : &tmK, 0, 0, 0, s[kSegHead], g, bar);
                         }
                         __syncwarp();
                         ++issued;
                         rg.step(kStages);
                     }
                 }
+                // what the merge kernel has to know of an item that starts here and ends in another block: this is the last
+                // stretch of this block's range
+                if (s[kSegT0] == 0 && s[kSegT1] < s[kSegTiles]) {
+                    const long long last = (me + 1) * total / blocks - s[kSegT1] + s[kSegTiles] - 1;   // its last key tile on the line
+                    int parts = 1;               // blocks whose ranges reach it
+                    while ((me + parts) * total < (last + 1) * blocks) ++parts;
+                    if (lane == 0) {
+                        p.desc[2 * me] = make_int4(parts, s[kSegRow], s[kSegHead], s[kSegPaired] ? p.tpt : 0);
+                        p.desc[2 * me + 1] = make_int4(s[kSegRows0], s[kSegRows1], 0, 0);
+                    }
+                    described = true;
+                }
             }
-        } else if (warp == 1) {
-            // ------------------------------------------------------------ MMA
-            const uint32_t idS = attn_idesc<E>(kAttnTile, kAttnTile, false);
-            const uint32_t idO = attn_idesc<E>(kAttnTile, D, true);
-            AttnWalk wq = walk;                  // the S side runs two jobs ahead of the O side
-            AttnSeg sq, so;
-            int jq = 0, jo = 0;                  // jobs issued on either side, over all items
-            int nq = 0, no = 0;                  // job within the item
-            int Jq = 0, Jo = 0;
-            int q_used = 0;                      // query buffers released so far
-            int items = 0;
-            AttnRing rq, ro;                     // key entry of the S side's tile, value entry of the O side's
-            ro.step(kStages);
+            if (lane == 0 && !described) p.desc[2 * me] = make_int4(0, 0, 0, 0);
+        } else if (warp < 3) {
+            // ------------------------------------------------------------ MMA: warp 1 issues S = Q K^T, warp 2 O += P V, so that
+            // the one's waits (some 100 clocks each, barrier complete or not) lie under the other's products.  Job n of a stretch:
+            // slot n & 1; split: keys 64 (n & 1) .. of tile n / 2; paired: keys 64 (n / 2 & 1) .. of tile n / 4.
+            const bool second = warp == 2;
+            const uint32_t idesc = second ? attn_idesc<E>(kAttnTile, D, true) : attn_idesc<E>(kAttnTile, kAttnSub, false);
+            int j = 0;                           // jobs so far
+            int q_used = 0;                      // query buffers used so far
+            AttnRing rg;                         // the tile's key entry (S) or value entry (O)
+            if (second) rg.step(kStages);
             bool ok = true;
-
-            auto issue_s = [&]() {
-                if (nq == Jq) {
-                    if (!wq.next(p, sq)) { Jq = nq = -1; return; }
-                    nq = 0; Jq = sq.jobs();
-                }
-                if (Jq < 0) return;
-                const int slot = jq & 1, half = sq.paired ? (nq & 1) : 0;
-                const int qb = (q_used + half) & 1;
-                if (nq < (sq.paired ? 2 : 1)) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(q_full(qb), ((q_used + half) >> 1) & 1u, abort_flag, kAttnWaitClocks));
-                    if (!ok) return;
-                }
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_bar(rq.s), rq.ph, abort_flag, kAttnWaitClocks));
-                if (!ok) return;
-                tc_fence_after();
-                const bool last_use = !sq.paired || half == 1;
-                const bool q_done = nq + (sq.paired ? 2 : 1) >= Jq;
-                if (elect_one()) {
-                    const uint64_t a0 = attn_desc(q_buf + qb * kStage, 1024);
-                    const uint64_t b0 = attn_desc(ring + rq.s * kStage, kGroup);
+            for (int item = 0; ok; ++item) {
+                const int qi = item & (kSegQueue - 1);
+                ok = attn_wait_warp(seg_full(qi), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+                if (!ok) break;
+                const int J = __shfl_sync(0xffffffffu, queue[qi][kSegJobs], 0);      // (the compiler then knows it uniform)
+                const bool paired = __shfl_sync(0xffffffffu, queue[qi][kSegPaired], 0) != 0;
+                if (J == 0) break;
+                const int last = paired ? 3 : 1; // job of a tile's last use
+                if (!second) {
+                    const int q0 = q_used & 1, q1 = (q_used + (paired ? 1 : 0)) & 1;   // query buffers of slots 0 and 1
+                    ok = attn_wait_warp(q_full(q0), static_cast<uint32_t>(q_used >> 1) & 1u, flag);
+                    if (ok && paired) ok = attn_wait_warp(q_full(q1), static_cast<uint32_t>((q_used + 1) >> 1) & 1u, flag);
+                    for (int n = 0; ok && n < J; ++n, ++j) {
+                        ok = attn_wait_warp(s_free(j & 3), (static_cast<uint32_t>(j >> 2) & 1u) ^ 1u, flag);
+                        if (ok && (n & last) == 0) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int sub = (paired ? n >> 1 : n) & 1;
+                        const bool last_use = (n & last) == last;
+                        if (elect_one()) {
+                            const uint64_t a0 = attn_desc(q_buf + ((n & 1) ? q1 : q0) * kStage, 1024);
+                            const uint64_t b0 = attn_desc(ring + rg.s * kStage + sub * (kAttnSub / 8 * kGroup), kGroup);
+                            const uint32_t d = tS + (j & 1) * 128 + ((j >> 1) & 1) * kAttnSub;
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) {
-                        const uint64_t a = a0 + static_cast<uint64_t>(((k >> 2) * (kAttnTile * 128) + (k & 3) * 32) >> 4);
-                        const uint64_t b = b0 + static_cast<uint64_t>(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
-                        umma_bf16(tS + slot * 128, a, b, idS, k != 0);
+                            for (int k = 0; k < D / 16; ++k) {
+                                const uint64_t a = a0 + static_cast<uint64_t>(((k >> 2) * (kAttnTile * 128) + (k & 3) * 32) >> 4);
+                                const uint64_t b = b0 + static_cast<uint64_t>(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
+                                umma_bf16(d, a, b, idesc, k != 0);
+                            }
+                            umma_commit(s_full(j & 3));
+                            if (last_use) umma_commit(empty_bar(rg.s));
+                            if (n + 1 == J) {
+                                umma_commit(q_empty(q0));
+                                if (paired) umma_commit(q_empty(q1));
+                            }
+                        }
+                        __syncwarp();
+                        if (last_use) { rg.step(kStages); rg.step(kStages); }
                     }
-                    umma_commit(s_full(slot));
-                    if (last_use) umma_commit(empty_bar(rq.s));
-                    if (q_done) umma_commit(q_empty(qb));
-                }
-                __syncwarp();
-                if (last_use) { rq.step(kStages); rq.step(kStages); }
-                ++jq; ++nq;
-                if (nq == Jq) q_used += sq.paired ? 2 : 1;
-            };
-            auto issue_o = [&]() -> bool {
-                if (no == Jo) {
-                    if (!walk.next(p, so)) return false;
-                    no = 0; Jo = so.jobs();
-                    if (items > 0) {             // the previous item's O has been read
-                        ok = __all_sync(0xffffffffu, mbar_wait_bounded(o_empty, (items - 1) & 1u, abort_flag, kAttnWaitClocks));
-                        if (!ok) return false;
-                    }
-                }
-                const int slot = jo & 1, half = so.paired ? (no & 1) : 0;
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(p_full(slot), (jo >> 1) & 1u, abort_flag, kAttnWaitClocks));
-                if (!ok) return false;
-                if (half == 0) {
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_bar(ro.s), ro.ph, abort_flag, kAttnWaitClocks));
-                    if (!ok) return false;
-                }
-                tc_fence_after();
-                const bool last_use = !so.paired || half == 1;
-                const bool first = no < 2;       // the slot's first job of this item
-                if (elect_one()) {
-                    const uint64_t b0 = attn_desc(ring + ro.s * kStage, kGroup);
+                    q_used += paired ? 2 : 1;
+                } else {
+                    if (item > 0) ok = attn_wait_warp(o_empty, static_cast<uint32_t>(item - 1) & 1u, flag);   // the previous O has been read
+                    for (int n = 0; ok && n < J; ++n, ++j) {
+                        if ((n & last) == 0) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
+                        if (ok) ok = attn_wait_warp(p_full(j & 3), static_cast<uint32_t>(j >> 2) & 1u, flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const int sub = (paired ? n >> 1 : n) & 1;
+                        const bool last_use = (n & last) == last;
+                        if (elect_one()) {
+                            const uint64_t b0 = attn_desc(ring + rg.s * kStage + sub * (kAttnSub / 8 * kGroup), kGroup);
+                            const uint32_t a = tS + (j & 1) * 128 + ((j >> 1) & 1) * kAttnSub, d = tO + (j & 1) * 128;
 #pragma unroll
-                    for (int k = 0; k < kAttnTile / 16; ++k)
-                        umma_f16_ts(tO + slot * 128, tS + slot * 128 + 64 + k * 8, b0 + static_cast<uint64_t>((k * 2 * kGroup) >> 4), idO,
-                                    (!first || k != 0) ? 1u : 0u);
-                    if (last_use) umma_commit(empty_bar(ro.s));
-                    if (no + 1 == Jo) umma_commit(o_full);
+                            for (int k = 0; k < kAttnSub / 16; ++k)
+                                umma_f16_ts(d, a + k * 8, b0 + static_cast<uint64_t>((k * 2 * kGroup) >> 4), idesc,
+                                            (n > 1 || k != 0) ? 1u : 0u);            // a slot's first job overwrites O
+                            umma_commit(s_free(j & 3));
+                            if (last_use) umma_commit(empty_bar(rg.s));
+                            if (n + 1 == J) umma_commit(o_full);
+                        }
+                        __syncwarp();
+                        if (last_use) { rg.step(kStages); rg.step(kStages); }
+                    }
+                    if (ok && lane == 0) mbar_arrive(seg_empty(qi));
                 }
-                __syncwarp();
-                if (last_use) { ro.step(kStages); ro.step(kStages); }
-                ++jo; ++no;
-                if (no == Jo) ++items;
-                return true;
-            };
-            issue_s();
-            if (ok) issue_s();
-            while (ok && issue_o()) issue_s();
+            }
             if (!ok) {
-                if (elect_one()) umma_commit(drain);
+                const uint32_t mine = drain + (second ? 8 : 0);
+                if (elect_one()) umma_commit(mine);
                 __syncwarp();
-                mbar_wait_bounded(drain, 0, abort_flag + 1, kAttnWaitClocks);
+                attn_wait(mine, 0, flag + 4);
             }
         }
     } else {
-        // ---------------------------------------------------------------- softmax warpgroups
+        // ---------------------------------------------------------------- softmax: four warps per slot, a thread per row
         const int slot = (warp - 4) >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;        // row of the tile = TMEM lane
         const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
-        const uint32_t aS = tS + slot * 128 + lane_off, aO = tO + slot * 128 + lane_off;
-        const uint32_t aO_other = tO + (slot ^ 1) * 128 + lane_off;
-        const int my_tok = row / p.group, my_head = row % p.group;
-        int jobs = 0, items = 0, splits = 0, tiles = 0;      // over all items of the block
-        bool ok = true, described = false;
-        while (ok && walk.next(p, seg)) {
-            const int f = jobs & 1, n0 = slot ^ f, J = seg.jobs();
-            const int tile_rows = seg.paired ? seg.rows[n0] : seg.rows[0];
+        const uint32_t aS0 = tS + slot * 128 + lane_off, aO = tO + slot * 128 + lane_off;
+        uint32_t used = 0;                       // jobs of this slot so far
+        int tiles = 0;                           // key tiles in the stretches before
+        bool ok = true;
+        for (int item = 0; ok; ++item) {
+            const int* const sg = queue[item & (kSegQueue - 1)];
+            ok = attn_wait_warp(seg_full(item & (kSegQueue - 1)), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+            if (!ok) break;
+            const int J = sg[kSegJobs];
+            if (J == 0) break;
+            const bool paired = sg[kSegPaired];
+            const int tile_rows = paired && slot ? sg[kSegRows1] : sg[kSegRows0];
             const bool warp_has_rows = quad * 32 < tile_rows;
-            const int lim = seg.lim0 + my_tok + (seg.paired && n0 ? p.tpt : 0);     // last key that this row sees
+            const int key0 = sg[kSegT0] * kAttnTile + (paired ? 0 : slot * kAttnSub);
+            const int step = paired ? kAttnSub : 2 * kAttnSub;                       // keys from one job of the slot to its next
+            // columns of the job's keys past `cut` are masked for this row, rows of V from `have` on do not exist
+            int cut = sg[kSegLimit] + row / p.group + (paired && slot ? p.tpt : 0) - key0;
+            int have = sg[kSegKeys] - key0;
             float m = -CUDART_INF_F, l = 0.0f;
-            for (int n = n0; ok && n < J; n += 2) {
-                const int tile = seg.t0 + (seg.paired ? n >> 1 : n);
-                const uint32_t use = static_cast<uint32_t>((jobs + n) >> 1);
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(s_full(slot), use & 1u, abort_flag, kAttnWaitClocks));
+            for (int n = 0; n < J; n += 2) {
+                const uint32_t h = used & 1u;
+                ok = attn_wait_warp(s_full(2 * h + slot), (used >> 1) & 1u, flag);
                 if (!ok) break;
                 tc_fence_after();
+                const uint32_t aS = aS0 + h * kAttnSub;
+                uint32_t sr[kAttnSub];
+                float* const s = reinterpret_cast<float*>(sr);
+                float base_m = 0.0f;
                 if (warp_has_rows) {
-                    // The row in two halves of 64 columns, so that it fits the registers: maximum of the first, then of the second,
-                    // which stays for its exponentials; the first is read again for its own.  P goes to the upper half of
-                    // the slot's columns, which holds nothing that is still to be read.
-                    uint32_t sr[64];
-                    float* s = reinterpret_cast<float*>(sr);
-                    const int cut = lim - tile * kAttnTile;                          // columns past it are masked
-                    const bool masked = !__all_sync(0xffffffffu, cut >= kAttnTile - 1);
-                    float mx[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
-                    auto load_half = [&](int h) {
-                        tmem_ld32(aS + h * 64, sr);
-                        tmem_ld32(aS + h * 64 + 32, sr + 32);
-                        tmem_wait_ld();
-                        if (masked) {
+                    tmem_ld32(aS, sr);
+                    tmem_ld32(aS + 32, sr + 32);
+                    tmem_wait_ld();
+                    if (!__all_sync(0xffffffffu, cut >= kAttnSub - 1)) {
 #pragma unroll
-                            for (int c = 0; c < 64; ++c) s[c] = h * 64 + c <= cut ? s[c] : -CUDART_INF_F;
-                        }
-                    };
-                    auto max_half = [&]() {
+                        for (int c = 0; c < kAttnSub; ++c) s[c] = c <= cut ? s[c] : -CUDART_INF_F;
+                    }
+                    float mx[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                        for (int c = 0; c < 64; ++c) mx[c & 3] = fmaxf(mx[c & 3], s[c]);
-                    };
-                    load_half(0);
-                    max_half();
-                    load_half(1);
-                    max_half();
-                    const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;
+                    for (int c = 4; c < 60; c += 8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mx[i] = max3_nan(mx[i], s[c + 2 * i], s[c + 2 * i + 1]);
+                    }
+                    const float mt = max3_nan(max3_nan(mx[0], mx[1], s[60]), max3_nan(mx[2], mx[3], s[61]), max3_nan(s[62], s[63], s[63])) * p.scale_log2;
+                    if (mt != mt) l = mt;                                            // a NaN score reaches the row's result
                     const bool grow = mt > m + 8.0f;
                     if (__any_sync(0xffffffffu, grow)) {
                         const float m_new = grow ? mt : m;
                         const float a = grow ? attn_ex2(m - m_new) : 1.0f;
                         l *= a;
                         m = m_new;
-                        if (n >= 2) {
+                        if (n > 0) {
+                            // O holds the jobs up to the last but one for certain; its rescaling waits for that one too
+                            ok = attn_wait_warp(s_free(2 * (h ^ 1u) + slot), ((used - 1) >> 1) & 1u, flag);
+                            if (!ok) break;
+                            tc_fence_after();
 #pragma unroll
                             for (int c = 0; c < D; c += 16) {
                                 uint32_t o[16];
@@ -586,66 +692,69 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                             }
                         }
                     }
-                    const float base_m = m == -CUDART_INF_F ? 0.0f : m;
-                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    auto exp_half = [&](int h) {
-#pragma unroll
-                        for (int c = 0; c < 64; c += 32) {
-                            uint32_t pk[16];
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const float x = attn_ex2(fmaf(s[c + i], p.scale_log2, -base_m));
-                                const float y = attn_ex2(fmaf(s[c + i + 1], p.scale_log2, -base_m));
-                                sum[i & 2] += x;
-                                sum[(i & 2) + 1] += y;
-                                pk[i / 2] = pack2<E>(x, y);
-                            }
-                            tmem_st16(aS + 64 + h * 32 + c / 2, pk);
-                        }
-                    };
-                    exp_half(1);
-                    load_half(0);
-                    exp_half(0);
-                    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                    tmem_wait_st();
+                    base_m = m == -CUDART_INF_F ? 0.0f : -m;
                 }
-                const int have = max(seg.kv - tile * kAttnTile, 0);
-                if (have < kAttnTile) {
+                if (have < kAttnSub) {
                     // Value rows behind the last key: their probabilities are 0, but 0 times what happens to lie there could be
-                    // NaN.  (Both warpgroups of a paired item clear them: zeros over zeros.)  Row r of a tile lies in group r / 8
+                    // NaN.  (Both slots of a paired item clear them: zeros over zeros.)  Row r of a tile lies in group r / 8
                     // at 128 (r % 8), once per 64 columns.  The stage cannot be recycled before this job's second product.
-                    const int e = 2 * (tiles + tile - seg.t0) + 1, st = e % kStages;
-                    ok = __all_sync(0xffffffffu, mbar_wait_bounded(full_bar(st), static_cast<uint32_t>(e / kStages) & 1u, abort_flag, kAttnWaitClocks));
+                    const int tile = tiles + (paired ? n >> 2 : n >> 1), sub = paired ? (n >> 1) & 1 : slot;
+                    const int e = 2 * tile + 1, st = e % kStages;
+                    ok = attn_wait_warp(full_bar(st), static_cast<uint32_t>(e / kStages) & 1u, flag);
                     if (!ok) break;
-                    for (int i = row; i < (kAttnTile - have) * kHalves * 8; i += 128) {
-                        const int r = have + i / (kHalves * 8), c = i % (kHalves * 8);
+                    const int r0 = sub * kAttnSub + max(have, 0), r1 = sub * kAttnSub + kAttnSub;
+                    for (int i = row; i < (r1 - r0) * kHalves * 8; i += 128) {
+                        const int r = r0 + i / (kHalves * 8), c = i % (kHalves * 8);
                         const uint32_t at = ring + st * kStage + (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16;
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
                     }
                     fence_proxy_async();
                 }
+                if (warp_has_rows) {
+                    // A masked score's exponential is 0 from the special-function unit and 2^-126 from the polynomial, against
+                    // numerators of 2^-8 and more in any row that sees a key; a row that sees none is told by its maximum.
+                    const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), base2 = pair(base_m, base_m);
+                    uint64_t sum[2] = {0, 0};
+#pragma unroll
+                    for (int c = 0; c < kAttnSub; c += 32) {
+                        uint32_t pk[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint64_t x = fma2(pair(s[c + 2 * i], s[c + 2 * i + 1]), scale2, base2);
+                            const uint64_t e = (i & 7) < kAttnPoly ? exp2_poly2(x) : pair(attn_ex2(low(x)), attn_ex2(high(x)));
+                            sum[i & 1] = add2(sum[i & 1], e);
+                            pk[i] = pack2<E>(low(e), high(e));
+                        }
+                        tmem_st16(aS + c / 2, pk);
+                    }
+                    const uint64_t both = add2(sum[0], sum[1]);
+                    l += low(both) + high(both);
+                    tmem_wait_st();
+                }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(slot));
+                if (lane == 0) mbar_arrive(p_full(2 * h + slot));
+                cut -= step;
+                have -= step;
+                ++used;
             }
             if (!ok) break;
 
-            // ---- the item (or its stretch) is done: O of both slots is complete.  A split item's two halves are put
-            // together here, each warpgroup taking one half of the columns of both accumulators.
-            if (!seg.paired) {
-                ml[slot * 128 + row] = make_float2(m, l);
-                __syncwarp();
-                if (lane == 0) mbar_arrive(ml_full);
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(ml_full, static_cast<uint32_t>(splits & 1), abort_flag, kAttnWaitClocks));
-                if (!ok) break;
-                ++splits;
-            }
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(o_full, static_cast<uint32_t>(items & 1), abort_flag, kAttnWaitClocks));
+            // ---- the item (or its stretch) is done once O is complete (which also says that nobody reads the previous
+            // stretch's m and l any more).  The slots' (m, l) are exchanged: a split item is put together here from both
+            // accumulators, each slot taking half of the columns.
+            ok = attn_wait_warp(o_full, static_cast<uint32_t>(item) & 1u, flag);
             if (!ok) break;
             tc_fence_after();
+            if (m == -CUDART_INF_F && l == l) l = 0.0f;                              // the row has seen no key (and no NaN)
+            ml[slot * 128 + row] = make_float2(m, l);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ml_full);
+            ok = attn_wait_warp(ml_full, static_cast<uint32_t>(item) & 1u, flag);
+            if (!ok) break;
             if (warp_has_rows) {
                 float wa = 1.0f, wb = 0.0f;      // weights of this slot's accumulator and of the other one's
-                if (!seg.paired) {
+                if (!paired) {
                     const float2 o = ml[(slot ^ 1) * 128 + row];
                     const float mm = fmaxf(m, o.x);
                     wa = m == -CUDART_INF_F ? 0.0f : attn_ex2(m - mm);
@@ -653,79 +762,64 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     l = l * wa + o.y * wb;
                     m = mm;
                 }
-                const bool valid = row < tile_rows, whole = seg.whole();
-                const bool use_a = seg.paired || n0 < J, use_b = !seg.paired && (n0 ^ 1) < J;      // the slot had a job
-                const int c0 = seg.paired ? 0 : slot * (D / 2), c1 = seg.paired ? D : c0 + D / 2;
-                const int part = static_cast<int>(blockIdx.x) * 2 + (seg.t0 == 0 ? 1 : 0);
-                const int part_row = part * 256 + (seg.paired ? n0 * 128 : 0) + row;
-                const int tok = seg.q0 + my_tok + (seg.paired && n0 ? p.tpt : 0), head = seg.kvh * p.group + my_head;
-                E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh;
-                float* const dst_part = p.part_o + static_cast<size_t>(part_row) * D;
-                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+                const bool valid = row < tile_rows, first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
+                const int c0 = paired ? 0 : slot * (D / 2), c1 = paired ? D : c0 + D / 2;
+                const int part_row = (static_cast<int>(blockIdx.x) * 2 + (first ? 1 : 0)) * 256 + (paired ? slot * 128 : 0) + row;
+                const int tok = sg[kSegRow] + row / p.group + (paired && slot ? p.tpt : 0), head = sg[kSegHead] * p.group + row % p.group;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
                 if (whole) { wa *= inv; wb *= inv; }
+                const uint32_t aO_other = tO + (slot ^ 1) * 128 + lane_off;
                 for (int c = c0; c < c1; c += 32) {
                     uint32_t o[32];
                     float x[32];
-                    if (use_a) {
-                        tmem_ld32(aO + c, o);
-                        tmem_wait_ld();
+                    tmem_ld32(aO + c, o);
+                    tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(o[i]) * wa;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = 0.0f;
-                    }
-                    if (use_b) {
+                    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(o[i]) * wa;
+                    if (!paired) {
                         tmem_ld32(aO_other + c, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) x[i] = fmaf(__uint_as_float(o[i]), wb, x[i]);
                     }
                     if (valid && whole) {
+                        E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + c;
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
-                            *reinterpret_cast<uint4*>(dst + c + i) =
+                            *reinterpret_cast<uint4*>(dst + i) =
                                 make_uint4(pack2<E>(x[i], x[i + 1]), pack2<E>(x[i + 2], x[i + 3]), pack2<E>(x[i + 4], x[i + 5]),
                                            pack2<E>(x[i + 6], x[i + 7]));
                     } else if (valid) {
+                        float* const dst = p.part_o + static_cast<size_t>(part_row) * D + c;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4*>(dst_part + c + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                            *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
                     }
                 }
-                if (valid && (seg.paired || slot == 0)) {
+                if (valid && (paired || slot == 0)) {
                     if (!whole) p.part_ml[part_row] = make_float2(m, l);
                     else if (p.lse)
                         p.lse[static_cast<int64_t>(tok) * (p.n_kv * p.group) + head] =
-                            l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+                            l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f;
                 }
-            }
-            // what the merge kernel has to know of an item that starts here and ends in another block: this is the last stretch
-            // of this block's range
-            if (warp == 4 && lane == 0 && seg.t0 == 0 && seg.t1 < seg.nt) {
-                const long long last = (me + 1) * total / blocks - seg.t1 + seg.nt - 1;           // its last key tile on the line
-                const int parts = static_cast<int>(((last + 1) * blocks - 1) / total) - me + 1;
-                p.desc[2 * me] = make_int4(parts, seg.q0, seg.kvh, seg.paired ? p.tpt : 0);
-                p.desc[2 * me + 1] = make_int4(seg.rows[0], seg.rows[1], 0, 0);
-                described = true;
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(o_empty);
-            jobs += J;
-            tiles += seg.t1 - seg.t0;
-            ++items;
+            tiles += sg[kSegT1] - sg[kSegT0];
+            if (lane == 0) {
+                mbar_arrive(o_empty);
+                mbar_arrive(seg_empty(item & (kSegQueue - 1)));
+            }
         }
-        if (warp == 4 && lane == 0 && !described) p.desc[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
     }
 
     __syncthreads();
     if (warp == 0 && lane == 0 && abort_flag[0] != 0) {
         // after a time-out: the copies still in flight have to land before this block's shared memory is given up
         for (long long i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-            mbar_wait_bounded(full_bar(static_cast<int>(i % kStages)), static_cast<uint32_t>((i / kStages) & 1), abort_flag + 1, kAttnWaitClocks);
+            attn_wait(full_bar(static_cast<int>(i % kStages)), static_cast<uint32_t>((i / kStages) & 1), flag + 4);
         for (int i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i)
-            mbar_wait_bounded(q_full(i & 1), static_cast<uint32_t>((i >> 1) & 1), abort_flag + 1, kAttnWaitClocks);
+            attn_wait(q_full(i & 1), static_cast<uint32_t>((i >> 1) & 1), flag + 4);
     }
     tc_fence_before();
     __syncthreads();
@@ -795,7 +889,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnMer
                 }
             }
         }
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
         const int tok = d.y + r / p.group + second * d.w, head = d.z * p.group + r % p.group;
         E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + lane * N;
         if (N == 4)
@@ -803,7 +897,7 @@ __global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnMer
         else
             *reinterpret_cast<uint32_t*>(dst) = pack2<E>(acc[0] * inv, acc[1] * inv);
         if (p.lse && lane == 0)
-            p.lse[static_cast<int64_t>(tok) * p.n_heads + head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -CUDART_INF_F;
+            p.lse[static_cast<int64_t>(tok) * p.n_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f;
     }
 }
 

@@ -209,10 +209,10 @@ class PagedCache:
             T = B * n_new
         ptr = None if uniform else _array("n_new", n_new, i32, B, dev)
         if out is None:
-            # one allocation for the int32 arrays, one for the slots
-            q_off, kv_len, status, positions = _empty(torch, stream, 3 * B + 1 + T, i32, self.device).split_with_sizes(
-                (B + 1, B, B, T))
-            out = WindowLayout(q_off, kv_len, _empty(torch, stream, T, i64, self.device), positions, status)
+            # one allocation, the 64-bit slots first
+            slots, q_off, kv_len, status, positions = _empty(torch, stream, 3 * (T + B) + 1, i32, self.device).split_with_sizes(
+                (2 * T, B + 1, B, B, T))
+            out = WindowLayout(q_off, kv_len, slots.view(i64), positions, status)
         lay = _pack_layout(_array("out.q_off", out.q_off, i32, B + 1, dev), _array("out.kv_len", out.kv_len, i32, B, dev),
                            _array("out.slot_map", out.slot_map, i64, T, dev),
                            _array("out.positions", out.positions, i32, T, dev),
@@ -335,7 +335,7 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
     elif draft_ids is not None:
         raise ValueError("draft_ids without draft_probs")
     if out is None:
-        a, t, m, st = _empty(torch, stream, (4, B), i32, target_probs.device).unbind()
+        a, t, m, st = _empty(torch, stream, 4 * B, i32, target_probs.device).split_with_sizes((B, B, B, B))
         out = ResidualOutput(a, t, m.view(f32), st)
     r = _pack_residual(B, 0 if k_off is not None else K, 0 if k_off is None else _array("k_off", k_off, i32, B + 1, dev), T, V,
                        target_probs.data_ptr(), _row_stride(target_probs), tdt,
