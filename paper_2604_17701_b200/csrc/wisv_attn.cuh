@@ -11,8 +11,8 @@
 // keys at D = 128) is faster than its 64 KB of keys and values (some 2800 clocks at a 148th of the measured copy
 // rate).  Prompt chunks are bound by the MMAs and by the exponentials, 1024 clocks each per 128 x 128 tile.
 //
-// Roles.  One block per SM, persistent: a warp that walks the work and issues the TMA copies, two warps that issue the MMAs,
-// and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
+// Roles.  One block per SM, persistent: a warp that walks the work and issues the TMA copies, four warps that issue the
+// MMAs, and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
 // "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
 // single row tile is left, "split": the slots take the key tiles in turn and are put together at the end.  Either way
 // the jobs (row tile, key tile) alternate between the slots, and the MMA warp issues S of job j + 2 behind O of job j,
@@ -35,7 +35,8 @@
 
 namespace wisv {
 
-constexpr int kAttnThreads = 384;
+constexpr int kAttnMmaWarps = 4;
+constexpr int kAttnThreads = 512;
 constexpr int kAttnTile = 128;                   // rows of a row tile, keys of a key tile
 constexpr int kAttnSub = 64;                     // keys of a job
 constexpr int kAttnMaxStages = 12;
@@ -87,7 +88,7 @@ __device__ __forceinline__ float attn_ex2(float x)
 
 // Bounded wait; `flag` is the shared-memory address of the block's abort flag.  One inline try and everything else out of
 // line: a try that is the condition of an inline loop costs some 370 clocks even where the barrier is complete.
-static __device__ __noinline__ bool attn_wait_slow(uint32_t bar, uint32_t parity, uint32_t flag)
+static __device__ __forceinline__ bool attn_wait_slow(uint32_t bar, uint32_t parity, uint32_t flag)
 {
     const long long t0 = clock64();
     uint32_t n = 0;
@@ -146,7 +147,7 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
 // r in [-1/2, 1/2] through the degree-4 polynomial with the least relative error there (2.6e-6; fitted by Remez's exchange).
 // The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both
 // matrix products; kAttnPoly of every 8 pairs go this way instead.
-constexpr int kAttnPoly = 0;
+constexpr int kAttnPoly = 2;
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x)
 {
     const uint64_t magic = pair(12582912.0f, 12582912.0f), unmagic = pair(-12582912.0f, -12582912.0f);
@@ -361,14 +362,14 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     auto seg_empty = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 16 + kSegQueue + s); };
     constexpr int kBars = 2 * kAttnMaxStages + 16 + 2 * kSegQueue;
     const uint32_t o_full = bars + 8u * kBars, o_empty = o_full + 8, ml_full = o_full + 16, drain = o_full + 24;
-    constexpr int kSegAt = (kBars + 10) * 8;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 5));
+    constexpr int kSegAt = (kBars + 12) * 8;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 7));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);       // [0] abort, [1] drain scratch
-    const uint32_t flag = bars + 8u * (kBars + 5) + 4u;
+    const uint32_t flag = bars + 8u * (kBars + 7) + 4u;
     int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
-    long long* totals = reinterpret_cast<long long*>(ml);                            // [20] scan over the warps, before that
+    long long* totals = reinterpret_cast<long long*>(ml);                            // [16] scan over the warps, before that
     static_assert(kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -379,11 +380,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         return;
     }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(q_full(s), 1); mbar_init(q_empty(s), 1); }
+        for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 2); }
+        for (int s = 0; s < 2; ++s) { mbar_init(q_full(s), 1); mbar_init(q_empty(s), 2); }
         for (int s = 0; s < 4; ++s) { mbar_init(s_full(s), 1); mbar_init(p_full(s), 4); mbar_init(s_free(s), 1); }
-        for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 9); }
-        mbar_init(o_full, 1); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(drain, 1); mbar_init(drain + 8, 1);
+        for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 10); }
+        mbar_init(o_full, 2); mbar_init(o_empty, 8); mbar_init(ml_full, 8); for (int s = 0; s < kAttnMmaWarps; ++s) mbar_init(drain + 8 * s, 1);
         abort_flag[0] = 0; abort_flag[1] = 0;
         for (int i = 0; i < 5; ++i) start[i] = 0;
         fence_barrier_init();
@@ -459,7 +460,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     long long issued = 0;                        // ring entries filled (producer warp; read again before the end)
     int q_issued = 0;
 
-    if (warp < 4) {
+    if (warp < 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
             // ------------------------------------------------------------ the work, and its TMA copies
             AttnWalk walk;
@@ -537,13 +539,16 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 }
             }
             if (lane == 0 && !described) p.desc[2 * me] = make_int4(0, 0, 0, 0);
-        } else if (warp < 3) {
-            // ------------------------------------------------------------ MMA: warp 1 issues S = Q K^T, warp 2 O += P V, so that
-            // the one's waits (some 100 clocks each, barrier complete or not) lie under the other's products.  Job n of a stretch:
-            // slot n & 1; split: keys 64 (n & 1) .. of tile n / 2; paired: keys 64 (n / 2 & 1) .. of tile n / 4.
-            const bool second = warp == 2;
+        } else if (warp < 1 + kAttnMmaWarps) {
+            // ------------------------------------------------------------ MMA: two warps issue S = Q K^T, one per slot, and two
+            // O += P V.  Each waits (some 100 clocks and more behind its own products, barrier complete or not) under the
+            // others' products.  Job n of a slot in a stretch: split: keys 64 slot .. of tile n; paired: keys 64 (n & 1) .. of
+            // tile n / 2.
+            const int slot = (warp - 1) & 1;
+            const bool second = warp > 2;
             const uint32_t idesc = second ? attn_idesc<E>(kAttnTile, D, true) : attn_idesc<E>(kAttnTile, kAttnSub, false);
-            int j = 0;                           // jobs so far
+            const uint32_t sS = tS + slot * 128, sO = tO + slot * 128;
+            uint32_t used = 0;                   // jobs of this slot so far
             int q_used = 0;                      // query buffers used so far
             AttnRing rg;                         // the tile's key entry (S) or value entry (O)
             if (second) rg.step(kStages);
@@ -552,70 +557,64 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const int qi = item & (kSegQueue - 1);
                 ok = attn_wait_warp(seg_full(qi), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
                 if (!ok) break;
-                const int J = __shfl_sync(0xffffffffu, queue[qi][kSegJobs], 0);      // (the compiler then knows it uniform)
+                const int jobs = __shfl_sync(0xffffffffu, queue[qi][kSegJobs], 0);   // (the compiler then knows it uniform)
                 const bool paired = __shfl_sync(0xffffffffu, queue[qi][kSegPaired], 0) != 0;
-                if (J == 0) break;
-                const int last = paired ? 3 : 1; // job of a tile's last use
+                if (jobs == 0) break;
+                const int J = jobs >> 1;
+                const int qb = (q_used + (paired ? slot : 0)) & 1;                   // the slot's query buffer
                 if (!second) {
-                    const int q0 = q_used & 1, q1 = (q_used + (paired ? 1 : 0)) & 1;   // query buffers of slots 0 and 1
-                    ok = attn_wait_warp(q_full(q0), static_cast<uint32_t>(q_used >> 1) & 1u, flag);
-                    if (ok && paired) ok = attn_wait_warp(q_full(q1), static_cast<uint32_t>((q_used + 1) >> 1) & 1u, flag);
-                    for (int n = 0; ok && n < J; ++n, ++j) {
-                        ok = attn_wait_warp(s_free(j & 3), (static_cast<uint32_t>(j >> 2) & 1u) ^ 1u, flag);
-                        if (ok && (n & last) == 0) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
+                    ok = attn_wait_warp(q_full(qb), static_cast<uint32_t>((q_used + (paired ? slot : 0)) >> 1) & 1u, flag);
+                    q_used += paired ? 2 : 1;
+                } else if (item > 0) {
+                    ok = attn_wait_warp(o_empty, static_cast<uint32_t>(item - 1) & 1u, flag);         // the previous O has been read
+                }
+                for (int n = 0; ok && n < J; ++n, ++used) {
+                    const uint32_t h = used & 1u, ph = (used >> 1) & 1u;
+                    const bool first_use = !paired || (n & 1) == 0, last_use = !paired || (n & 1) == 1;
+                    const uint32_t b_at = ring + rg.s * kStage + (paired ? (n & 1) : slot) * (kAttnSub / 8 * kGroup);
+                    if (!second) {
+                        ok = attn_wait_warp(s_free(2 * h + slot), ph ^ 1u, flag);
+                        if (ok && first_use) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
                         if (!ok) break;
                         tc_fence_after();
-                        const int sub = (paired ? n >> 1 : n) & 1;
-                        const bool last_use = (n & last) == last;
                         if (elect_one()) {
-                            const uint64_t a0 = attn_desc(q_buf + ((n & 1) ? q1 : q0) * kStage, 1024);
-                            const uint64_t b0 = attn_desc(ring + rg.s * kStage + sub * (kAttnSub / 8 * kGroup), kGroup);
-                            const uint32_t d = tS + (j & 1) * 128 + ((j >> 1) & 1) * kAttnSub;
+                            const uint64_t a0 = attn_desc(q_buf + qb * kStage, 1024), b0 = attn_desc(b_at, kGroup);
 #pragma unroll
                             for (int k = 0; k < D / 16; ++k) {
                                 const uint64_t a = a0 + static_cast<uint64_t>(((k >> 2) * (kAttnTile * 128) + (k & 3) * 32) >> 4);
                                 const uint64_t b = b0 + static_cast<uint64_t>(((k >> 2) * 1024 + (k & 3) * 32) >> 4);
-                                umma_bf16(d, a, b, idesc, k != 0);
+                                umma_bf16(sS + h * kAttnSub, a, b, idesc, k != 0);
                             }
-                            umma_commit(s_full(j & 3));
+                            umma_commit(s_full(2 * h + slot));
                             if (last_use) umma_commit(empty_bar(rg.s));
                             if (n + 1 == J) {
-                                umma_commit(q_empty(q0));
-                                if (paired) umma_commit(q_empty(q1));
+                                umma_commit(q_empty(qb));
+                                if (paired) umma_commit(q_empty(qb));                // (a split item's buffer hears from both warps)
                             }
                         }
-                        __syncwarp();
-                        if (last_use) { rg.step(kStages); rg.step(kStages); }
-                    }
-                    q_used += paired ? 2 : 1;
-                } else {
-                    if (item > 0) ok = attn_wait_warp(o_empty, static_cast<uint32_t>(item - 1) & 1u, flag);   // the previous O has been read
-                    for (int n = 0; ok && n < J; ++n, ++j) {
-                        if ((n & last) == 0) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
-                        if (ok) ok = attn_wait_warp(p_full(j & 3), static_cast<uint32_t>(j >> 2) & 1u, flag);
+                    } else {
+                        if (first_use) ok = attn_wait_warp(full_bar(rg.s), rg.ph, flag);
+                        if (ok) ok = attn_wait_warp(p_full(2 * h + slot), ph, flag);
                         if (!ok) break;
                         tc_fence_after();
-                        const int sub = (paired ? n >> 1 : n) & 1;
-                        const bool last_use = (n & last) == last;
                         if (elect_one()) {
-                            const uint64_t b0 = attn_desc(ring + rg.s * kStage + sub * (kAttnSub / 8 * kGroup), kGroup);
-                            const uint32_t a = tS + (j & 1) * 128 + ((j >> 1) & 1) * kAttnSub, d = tO + (j & 1) * 128;
+                            const uint64_t b0 = attn_desc(b_at, kGroup);
 #pragma unroll
                             for (int k = 0; k < kAttnSub / 16; ++k)
-                                umma_f16_ts(d, a + k * 8, b0 + static_cast<uint64_t>((k * 2 * kGroup) >> 4), idesc,
-                                            (n > 1 || k != 0) ? 1u : 0u);            // a slot's first job overwrites O
-                            umma_commit(s_free(j & 3));
+                                umma_f16_ts(sO, sS + h * kAttnSub + k * 8, b0 + static_cast<uint64_t>((k * 2 * kGroup) >> 4), idesc,
+                                            (n != 0 || k != 0) ? 1u : 0u);           // a slot's first job overwrites O
+                            umma_commit(s_free(2 * h + slot));
                             if (last_use) umma_commit(empty_bar(rg.s));
                             if (n + 1 == J) umma_commit(o_full);
                         }
-                        __syncwarp();
-                        if (last_use) { rg.step(kStages); rg.step(kStages); }
                     }
-                    if (ok && lane == 0) mbar_arrive(seg_empty(qi));
+                    __syncwarp();
+                    if (last_use) { rg.step(kStages); rg.step(kStages); }
                 }
+                if (ok && second && lane == 0) mbar_arrive(seg_empty(qi));
             }
             if (!ok) {
-                const uint32_t mine = drain + (second ? 8 : 0);
+                const uint32_t mine = drain + 8 * (warp - 1);
                 if (elect_one()) umma_commit(mine);
                 __syncwarp();
                 attn_wait(mine, 0, flag + 4);
@@ -623,7 +622,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
     } else {
         // ---------------------------------------------------------------- softmax: four warps per slot, a thread per row
-        const int slot = (warp - 4) >> 2, quad = warp & 3;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        const int slot = (warp - 8) >> 2, quad = warp & 3;
         const int row = quad * 32 + lane;        // row of the tile = TMEM lane
         const uint32_t lane_off = static_cast<uint32_t>(quad * 32) << 16;
         const uint32_t aS0 = tS + slot * 128 + lane_off, aO = tO + slot * 128 + lane_off;
