@@ -20,7 +20,8 @@
 //
 // Work split.  The key tiles of all items form one line, cut into equal contiguous ranges, one per block; every block finds
 // its range from the lengths on the device, so the host knows no lengths and a captured graph stays balanced.  An item cut by a
-// range boundary leaves fp32 partials (at most two per block) that attn_merge_kernel adds in block order.
+// range boundary leaves fp32 partials (at most two per block); the block that comes last with its own adds them all, in block
+// order, so the result does not depend on who that is.
 //
 // Keys and values come in 128-byte swizzled tiles laid out [8 tokens][D / 64][8][64]: one TMA per page (five dimensions: 64
 // columns, 8 tokens, column halves, head, token groups), whatever the page size, with both the K-major view for the first product and
@@ -55,11 +56,11 @@ struct AttnParams {
     int64_t table_stride;
     void* out; int64_t ot, oh;
     float* lse;
-    float scale_log2;
+    float scale_log2, inv_group;
     int32_t* err;
     float* part_o;                               // [2 * blocks][256][D]
     float2* part_ml;                             // [2 * blocks][256]
-    int4* desc;                                  // [blocks][2]: the item whose merge starts with this block
+    int32_t* count;                              // [blocks]: arrivals at the item that starts in a block's range and ends in another's; 0 between calls
 };
 
 template <typename E> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
@@ -75,9 +76,24 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// the token of a row of a row tile: row / group for row < 128 (the product is off by 1e-5 at most, the nearest wrong answer 1/128)
+__device__ __forceinline__ int attn_token(const AttnParams& p, int row) { return static_cast<int>((row + 0.5f) * p.inv_group); }
+__device__ __forceinline__ float attn_lg2(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 template <typename E> struct is_bf16 { static constexpr bool value = false; };
 template <> struct is_bf16<__nv_bfloat16> { static constexpr bool value = true; };
 
+// 1 / x by the hardware approximation (1 ulp): the full division may call a function, which this kernel cannot
+__device__ __forceinline__ float attn_rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // 2^x by the hardware approximation (relative error 2^-22)
 __device__ __forceinline__ float attn_ex2(float x)
 {
@@ -263,7 +279,9 @@ enum {
     kSegLimit,                                   // last key that the item's first token sees
     kSegRow, kSegHead,                           // first row of the item in q, key head
     kSegRows0, kSegRows1,                        // valid rows of its row tiles
-    kSegReq, kSegWords = 16
+    kSegReq,
+    kSegFirst, kSegParts,                        // blocks that share the item: the first one, how many
+    kSegLeft, kSegWords = 16                     // (units of the range before the stretch; the walking warp's own)
 };
 constexpr int kSegQueue = 4;
 
@@ -295,7 +313,7 @@ struct AttnWalk {
                 s[kSegJobs] = (paired ? 4 : 2) * (t1 - t0);
                 s[kSegPaired] = paired; s[kSegT0] = t0; s[kSegT1] = t1; s[kSegTiles] = nt;
                 s[kSegKeys] = r.kv; s[kSegLimit] = r.kv - r.n + tok0;
-                s[kSegRow] = r.q0 + tok0; s[kSegHead] = kvh; s[kSegReq] = b;
+                s[kSegRow] = r.q0 + tok0; s[kSegHead] = kvh; s[kSegReq] = b; s[kSegLeft] = units;
                 s[kSegRows0] = min(left, p.tpt) * p.group;
                 s[kSegRows1] = paired ? min(left - p.tpt, p.tpt) * p.group : 0;
             }
@@ -318,6 +336,83 @@ struct AttnWalk {
     }
 };
 
+// The merge of an item's partials by the eight softmax warps of the block that came last.  A warp takes four rows at a time, so
+// that enough loads are under way: the partials' maxima and sums first (lane: partial), then the outputs (lane: D / 32
+// columns), in block order.  Reads go past L1, which other blocks' writes do not reach.
+template <typename E, int D>
+__device__ __forceinline__ void attn_merge(const AttnParams& p, const int* sg, int w, int lane)
+{
+    constexpr int N = D / 32, R = 4;
+    // (through shuffles, so that the compiler knows the loops uniform: shuffles in loops that might diverge become calls)
+    const int first = sg[kSegFirst], parts = __shfl_sync(0xffffffffu, sg[kSegParts], 0), rows0 = sg[kSegRows0];
+    const int rows = __shfl_sync(0xffffffffu, rows0 + sg[kSegRows1], 0);
+    __threadfence();
+    for (int r0 = w * R; r0 < rows; r0 += 8 * R) {
+        // row i of the four: where its partials lie in a block's buffer (rows of the second tile from 128 on)
+        auto at = [&](int i) { const int r = min(r0 + i, rows - 1); return r < rows0 ? r : 128 + r - rows0; };
+        auto buffer = [&](int j) { return (j == 0 ? 2 * first + 1 : 2 * (first + j)) * 256; };
+        float m[R], l[R], acc[R][N];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            m[i] = -CUDART_INF_F; l[i] = 0.0f;
+#pragma unroll
+            for (int c = 0; c < N; ++c) acc[i][c] = 0.0f;
+        }
+        for (int j0 = 0; j0 < parts; j0 += 32) {
+            const int j = min(j0 + lane, parts - 1);
+#pragma unroll
+            for (int i = 0; i < R; ++i) m[i] = fmaxf(m[i], __ldcg(p.part_ml + buffer(j) + at(i)).x);
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int o = 16; o; o >>= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
+        for (int j0 = 0; j0 < parts; j0 += 32) {
+            float f[R], g[R];                    // lane's partial: its weight, and its weighted sum
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const float2 x = j0 + lane < parts ? __ldcg(p.part_ml + buffer(j0 + lane) + at(i)) : make_float2(-CUDART_INF_F, 0.0f);
+                f[i] = x.x == -CUDART_INF_F ? 0.0f : attn_ex2(x.x - m[i]);
+                g[i] = f[i] * x.y;
+            }
+            const int here = min(32, parts - j0);
+#pragma unroll 2
+            for (int u = 0; u < here; ++u) {
+                const float* src = p.part_o + static_cast<size_t>(buffer(j0 + u)) * D + lane * N;
+#pragma unroll
+                for (int i = 0; i < R; ++i) {
+                    const float fi = __shfl_sync(0xffffffffu, f[i], u);
+                    l[i] += __shfl_sync(0xffffffffu, g[i], u);
+                    if (N == 4) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + at(i) * D));
+                        acc[i][0] = fmaf(fi, v.x, acc[i][0]); acc[i][1] = fmaf(fi, v.y, acc[i][1]);
+                        acc[i][2 % N] = fmaf(fi, v.z, acc[i][2 % N]); acc[i][3 % N] = fmaf(fi, v.w, acc[i][3 % N]);
+                    } else {
+                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + at(i) * D));
+                        acc[i][0] = fmaf(fi, v.x, acc[i][0]); acc[i][1] = fmaf(fi, v.y, acc[i][1]);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int r = r0 + i, in = r < rows0 ? r : r - rows0;
+            if (r >= rows) break;
+            const float inv = l[i] == 0.0f ? 0.0f : attn_rcp(l[i]);
+            const int t = attn_token(p, in), tok = sg[kSegRow] + t + (r < rows0 ? 0 : p.tpt);
+            const int head = sg[kSegHead] * p.group + in - t * p.group;
+            E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + lane * N;
+            if (N == 4)
+                *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<E>(acc[i][0] * inv, acc[i][1] * inv), pack2<E>(acc[i][2 % N] * inv, acc[i][3 % N] * inv));
+            else
+                *reinterpret_cast<uint32_t*>(dst) = pack2<E>(acc[i][0] * inv, acc[i][1] * inv);
+            if (p.lse && lane == 0)
+                p.lse[static_cast<int64_t>(tok) * (p.n_kv * p.group) + head] =
+                    l[i] == 0.0f ? -CUDART_INF_F : (m[i] + attn_lg2(l[i])) * 0.6931471805599453f;
+        }
+    }
+}
+
 // Position in the ring of key and value tiles: tile g uses entries 2 g (keys) and 2 g + 1 (values).
 struct AttnRing {
     int s = 0;
@@ -330,6 +425,44 @@ template <int D> __host__ __device__ constexpr int attn_stages()
 {
     return (kAttnSmem - kAttnSmall - kAttnSlack - 2 * attn_stage_bytes<D>()) / attn_stage_bytes<D>() < kAttnMaxStages
                ? (kAttnSmem - kAttnSmall - kAttnSlack - 2 * attn_stage_bytes<D>()) / attn_stage_bytes<D>() : kAttnMaxStages;
+}
+
+// The copies of key (or value) tiles t0 .. t1 - 1 of a request into every other entry of the ring, by one warp.
+template <int D>
+__device__ __forceinline__ bool attn_load_tiles(const AttnParams& p, const CUtensorMap* map, int page_groups, int groups, int req, int t0,
+                                                int t1, int keys, int head, uint32_t ring, uint32_t bars, uint32_t flag, int lane,
+                                                AttnRing& rg, int& issued)
+{
+    constexpr int kStages = attn_stages<D>();
+    const int box_tok = min(1 << p.page_shift, kAttnTile);
+    const uint32_t box_bytes = static_cast<uint32_t>(box_tok) * (D * 2);
+    const int32_t* table = p.block_table + req * p.table_stride;
+    // lane i: the first token group of the tile's i-th page.  The table entry of the next tile is read a tile ahead.
+    auto page_of = [&](int t) {
+        const int tok = t * kAttnTile + lane * box_tok;
+        return t < t1 && lane * box_tok < kAttnTile && tok < keys ? __ldg(table + (tok >> p.page_shift)) : -1;
+    };
+    int pg = page_of(t0);
+    for (int t = t0; t < t1; ++t) {
+        const int tok0 = t * kAttnTile;
+        const int pages = max(min(keys - tok0, kAttnTile) + box_tok - 1, 0) / box_tok;               // that hold keys
+        const int at = ((tok0 + lane * box_tok) & ((1 << p.page_shift) - 1)) >> 3;
+        const int g = pg >= 0 && pg < p.n_pages ? pg * page_groups + at : groups;                    // out of range: zeros
+        pg = page_of(t + 1);
+        if (!attn_wait_warp(bars + 8u * (kAttnMaxStages + rg.s), rg.ph ^ 1u, flag)) return false;
+        const uint32_t dst = ring + rg.s * attn_stage_bytes<D>(), bar = bars + 8u * rg.s;
+        if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(pages) * box_bytes);
+        __syncwarp();
+        for (int i = 0; i < pages; ++i) {
+            const int gi = __shfl_sync(0xffffffffu, g, i);
+            if (elect_one()) tma_load_5d(dst + i * box_bytes, map, 0, 0, 0, head, gi, bar);
+        }
+        __syncwarp();
+        ++issued;
+        rg.step(kStages);
+        rg.step(kStages);
+    }
+    return true;
 }
 
 template <typename E, int D>
@@ -361,12 +494,12 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     auto seg_full = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 16 + s); };
     auto seg_empty = [&](int s) { return bars + 8u * (2 * kAttnMaxStages + 16 + kSegQueue + s); };
     constexpr int kBars = 2 * kAttnMaxStages + 16 + 2 * kSegQueue;
-    const uint32_t o_full = bars + 8u * kBars, o_empty = o_full + 8, ml_full = o_full + 16, drain = o_full + 24;
-    constexpr int kSegAt = (kBars + 12) * 8;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 7));
+    const uint32_t o_full = bars + 8u * kBars, o_empty = o_full + 8, ml_full = o_full + 16, part_full = o_full + 24, last_full = o_full + 32, drain = o_full + 40;
+    constexpr int kSegAt = (kBars + 14) * 8;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 9));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);       // [0] abort, [1] drain scratch
-    const uint32_t flag = bars + 8u * (kBars + 7) + 4u;
-    int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range
+    const uint32_t flag = bars + 8u * (kBars + 9) + 4u;
+    int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range; [5]: whether this block came last
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
     long long* totals = reinterpret_cast<long long*>(ml);                            // [16] scan over the warps, before that
@@ -376,15 +509,15 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const int lane = threadIdx.x & 31;
 
     if (small_off + kAttnSmall > static_cast<uint32_t>(kAttnSmem)) {          // (dynamic shared memory starts 1024-byte aligned)
-        if (threadIdx.x == 0) { atomicOr(p.err, 2); p.desc[2 * blockIdx.x] = make_int4(0, 0, 0, 0); }
+        if (threadIdx.x == 0) atomicOr(p.err, 2);
         return;
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 2); }
         for (int s = 0; s < 2; ++s) { mbar_init(q_full(s), 1); mbar_init(q_empty(s), 2); }
         for (int s = 0; s < 4; ++s) { mbar_init(s_full(s), 1); mbar_init(p_full(s), 4); mbar_init(s_free(s), 1); }
-        for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 10); }
-        mbar_init(o_full, 2); mbar_init(o_empty, 8); mbar_init(ml_full, 8); for (int s = 0; s < kAttnMmaWarps; ++s) mbar_init(drain + 8 * s, 1);
+        for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 11); }
+        mbar_init(o_full, 2); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(part_full, 8); mbar_init(last_full, 1); for (int s = 0; s < kAttnMmaWarps; ++s) mbar_init(drain + 8 * s, 1);
         abort_flag[0] = 0; abort_flag[1] = 0;
         for (int i = 0; i < 5; ++i) start[i] = 0;
         fence_barrier_init();
@@ -457,28 +590,35 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     }
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P over its first half, O at 256 + 128 s
-    long long issued = 0;                        // ring entries filled (producer warp; read again before the end)
-    int q_issued = 0;
+    int issued = 0, q_issued = 0;                // ring entries and query buffers filled (copying warps; read again before the end)
 
     if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (warp == 0) {
-            // ------------------------------------------------------------ the work, and its TMA copies
+            // ------------------------------------------------------------ the work, and the TMA copies of queries and keys
             AttnWalk walk;
             walk.start(p, start);
             int s[kSegWords];
             AttnRing rg;
-            bool ok = true, described = false;
-            const int box_tok = min(1 << p.page_shift, kAttnTile);
-            const uint32_t box_bytes = static_cast<uint32_t>(box_tok) * (D * 2);
+            bool ok = true;
             for (int item = 0; ok; ++item) {
                 const bool some = walk.next(p, s);
                 const int qi = item & (kSegQueue - 1);
+                if (some) {
+                    s[kSegFirst] = me; s[kSegParts] = 1;
+                    if (s[kSegT0] > 0 || s[kSegT1] < s[kSegTiles]) {                 // shared: whose ranges does the item reach?
+                        const long long unit0 = (me + 1) * total / blocks - s[kSegLeft] - s[kSegT0], end = unit0 + s[kSegTiles];
+                        int first = me, last = me;
+                        while (first * total >= (unit0 + 1) * blocks) --first;
+                        while ((last + 1) * total < end * blocks) ++last;
+                        s[kSegFirst] = first; s[kSegParts] = last - first + 1;
+                    }
+                }
                 ok = attn_wait_warp(seg_empty(qi), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
                 if (!ok) break;
                 if (lane == 0) {
 #pragma unroll
-                    for (int i = 0; i < kSegReq; ++i) queue[qi][i] = some ? s[i] : 0;
+                    for (int i = 0; i < kSegLeft; ++i) queue[qi][i] = some ? s[i] : 0;
                     mbar_arrive(seg_full(qi));
                 }
                 __syncwarp();
@@ -494,51 +634,24 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     }
                     __syncwarp();
                 }
-                const int32_t* table = p.block_table + s[kSegReq] * p.table_stride;
-                for (int t = s[kSegT0]; ok && t < s[kSegT1]; ++t) {
-                    // this tile's pages: lane i holds the i-th one's first token group, for keys and for values
-                    const int tok0 = t * kAttnTile;
-                    const int have = min(s[kSegKeys] - tok0, kAttnTile);             // keys that exist
-                    const int pages = have <= 0 ? 0 : (have + box_tok - 1) / box_tok;
-                    int gk = p.groups_k, gv = p.groups_v;
-                    if (lane < pages) {
-                        const int tok = tok0 + lane * box_tok;
-                        const int pg = __ldg(table + (tok >> p.page_shift));
-                        if (pg >= 0 && pg < p.n_pages) {
-                            const int in = (tok & ((1 << p.page_shift) - 1)) >> 3;
-                            gk = pg * p.page_groups_k + in;
-                            gv = pg * p.page_groups_v + in;
-                        }
-                    }
-                    for (int kv = 0; ok && kv < 2; ++kv) {
-                        ok = attn_wait_warp(empty_bar(rg.s), rg.ph ^ 1u, flag);
-                        if (!ok) break;
-                        const uint32_t dst = ring + rg.s * kStage, bar = full_bar(rg.s);
-                        if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(pages) * box_bytes);
-                        __syncwarp();
-                        for (int i = 0; i < pages; ++i) {
-                            const int g = __shfl_sync(0xffffffffu, kv ? gv : gk, i);
-                            if (elect_one()) tma_load_5d(dst + i * box_bytes, kv ? &tmV : &tmK, 0, 0, 0, s[kSegHead], g, bar);
-                        }
-                        __syncwarp();
-                        ++issued;
-                        rg.step(kStages);
-                    }
-                }
-                // what the merge kernel has to know of an item that starts here and ends in another block: this is the last
-                // stretch of this block's range
-                if (s[kSegT0] == 0 && s[kSegT1] < s[kSegTiles]) {
-                    const long long last = (me + 1) * total / blocks - s[kSegT1] + s[kSegTiles] - 1;   // its last key tile on the line
-                    int parts = 1;               // blocks whose ranges reach it
-                    while ((me + parts) * total < (last + 1) * blocks) ++parts;
-                    if (lane == 0) {
-                        p.desc[2 * me] = make_int4(parts, s[kSegRow], s[kSegHead], s[kSegPaired] ? p.tpt : 0);
-                        p.desc[2 * me + 1] = make_int4(s[kSegRows0], s[kSegRows1], 0, 0);
-                    }
-                    described = true;
-                }
+                ok = ok && attn_load_tiles<D>(p, &tmK, p.page_groups_k, p.groups_k, s[kSegReq], s[kSegT0], s[kSegT1], s[kSegKeys],
+                                              s[kSegHead], ring, bars, flag, lane, rg, issued);
             }
-            if (lane == 0 && !described) p.desc[2 * me] = make_int4(0, 0, 0, 0);
+        } else if (warp == 1 + kAttnMmaWarps) {
+            // ------------------------------------------------------------ the TMA copies of values (pages of 16 tokens are eight
+            // copies a tile, some 80 clocks each: one warp for both would be late)
+            AttnRing rg;
+            rg.step(kStages);
+            bool ok = true;
+            for (int item = 0; ok; ++item) {
+                const int qi = item & (kSegQueue - 1);
+                ok = attn_wait_warp(seg_full(qi), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+                if (!ok || queue[qi][kSegJobs] == 0) break;
+                ok = attn_load_tiles<D>(p, &tmV, p.page_groups_v, p.groups_v, queue[qi][kSegReq], queue[qi][kSegT0], queue[qi][kSegT1],
+                                        queue[qi][kSegKeys], queue[qi][kSegHead], ring, bars, flag, lane, rg, issued);
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(seg_empty(qi));
+            }
         } else if (warp < 1 + kAttnMmaWarps) {
             // ------------------------------------------------------------ MMA: two warps issue S = Q K^T, one per slot, and two
             // O += P V.  Each waits (some 100 clocks and more behind its own products, barrier complete or not) under the
@@ -629,6 +742,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         const uint32_t aS0 = tS + slot * 128 + lane_off, aO = tO + slot * 128 + lane_off;
         uint32_t used = 0;                       // jobs of this slot so far
         int tiles = 0;                           // key tiles in the stretches before
+        uint32_t splits = 0;                     // stretches of shared items so far
         bool ok = true;
         for (int item = 0; ok; ++item) {
             const int* const sg = queue[item & (kSegQueue - 1)];
@@ -642,7 +756,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             const int key0 = sg[kSegT0] * kAttnTile + (paired ? 0 : slot * kAttnSub);
             const int step = paired ? kAttnSub : 2 * kAttnSub;                       // keys from one job of the slot to its next
             // columns of the job's keys past `cut` are masked for this row, rows of V from `have` on do not exist
-            int cut = sg[kSegLimit] + row / p.group + (paired && slot ? p.tpt : 0) - key0;
+            int cut = sg[kSegLimit] + attn_token(p, row) + (paired && slot ? p.tpt : 0) - key0;
             int have = sg[kSegKeys] - key0;
             float m = -CUDART_INF_F, l = 0.0f;
             for (int n = 0; n < J; n += 2) {
@@ -765,8 +879,9 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const bool valid = row < tile_rows, first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
                 const int c0 = paired ? 0 : slot * (D / 2), c1 = paired ? D : c0 + D / 2;
                 const int part_row = (static_cast<int>(blockIdx.x) * 2 + (first ? 1 : 0)) * 256 + (paired ? slot * 128 : 0) + row;
-                const int tok = sg[kSegRow] + row / p.group + (paired && slot ? p.tpt : 0), head = sg[kSegHead] * p.group + row % p.group;
-                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+                const int t = attn_token(p, row), tok = sg[kSegRow] + t + (paired && slot ? p.tpt : 0);
+                const int head = sg[kSegHead] * p.group + row - t * p.group;
+                const float inv = l == 0.0f ? 0.0f : attn_rcp(l);
                 if (whole) { wa *= inv; wb *= inv; }
                 const uint32_t aO_other = tO + (slot ^ 1) * 128 + lane_off;
                 for (int c = c0; c < c1; c += 32) {
@@ -800,24 +915,47 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     if (!whole) p.part_ml[part_row] = make_float2(m, l);
                     else if (p.lse)
                         p.lse[static_cast<int64_t>(tok) * (p.n_kv * p.group) + head] =
-                            l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f;
+                            l == 0.0f ? -CUDART_INF_F : (m + attn_lg2(l)) * 0.6931471805599453f;
                 }
             }
             tc_fence_before();
             __syncwarp();
+            if (lane == 0) mbar_arrive(o_empty);
             tiles += sg[kSegT1] - sg[kSegT0];
-            if (lane == 0) {
-                mbar_arrive(o_empty);
-                mbar_arrive(seg_empty(item & (kSegQueue - 1)));
+            if (sg[kSegParts] > 1) {
+                // The item is shared: count this block's part, and if it is the last one to arrive, add all of them.
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(part_full);
+                ok = attn_wait_warp(part_full, splits & 1u, flag);
+                if (!ok) break;
+                const int first_block = sg[kSegFirst], parts = sg[kSegParts];
+                if (warp == 8 && lane == 0) {
+                    const int before = atomicAdd(p.count + first_block, 1);
+                    start[5] = before == parts - 1;
+                    if (before == parts - 1) p.count[first_block] = 0;
+                    __threadfence();
+                    mbar_arrive(last_full);
+                }
+                __syncwarp();
+                ok = attn_wait_warp(last_full, splits & 1u, flag);
+                if (!ok) break;
+                ++splits;
+                if (__shfl_sync(0xffffffffu, start[5], 0)) attn_merge<E, D>(p, sg, warp - 8, lane);
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(seg_empty(item & (kSegQueue - 1)));
         }
     }
 
     __syncthreads();
-    if (warp == 0 && lane == 0 && abort_flag[0] != 0) {
+    if ((warp == 0 || warp == 1 + kAttnMmaWarps) && lane == 0 && abort_flag[0] != 0) {
         // after a time-out: the copies still in flight have to land before this block's shared memory is given up
-        for (long long i = issued > kStages ? issued - kStages : 0; i < issued; ++i)
-            attn_wait(full_bar(static_cast<int>(i % kStages)), static_cast<uint32_t>((i / kStages) & 1), flag + 4);
+        const int kind = warp == 0 ? 0 : 1;
+        for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
+            const int e = 2 * i + kind;
+            attn_wait(full_bar(e % kStages), static_cast<uint32_t>(e / kStages) & 1u, flag + 4);
+        }
         for (int i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i)
             attn_wait(q_full(i & 1), static_cast<uint32_t>((i >> 1) & 1), flag + 4);
     }
@@ -828,77 +966,6 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tmem_dealloc(tmem, 512);
     }
     if (threadIdx.x == 0 && abort_flag[0] != 0) atomicOr(p.err, 1);
-}
-
-// ---------------------------------------------------------------- merge of the items that several blocks share
-// Block c looks after the item that starts in block c's range and ends in a later one; a warp takes a row: the partials' maxima
-// and sums first, then D / 32 columns per lane, partials in block order (so the result does not depend on timing).
-struct AttnMerge {
-    const float* part_o;
-    const float2* part_ml;
-    const int4* desc;
-    void* out; int64_t ot, oh;
-    float* lse;
-    int32_t group, n_heads;
-};
-
-constexpr int kMergeThreads = 128;
-
-template <typename E, int D>
-__global__ void __launch_bounds__(kMergeThreads) attn_merge_kernel(const AttnMerge p)
-{
-    griddep_wait();
-    griddep_launch_dependents();
-    const int c = blockIdx.x;
-    const int4 d = p.desc[2 * c];
-    const int parts = d.x;
-    if (parts < 2) return;
-    const int4 e = p.desc[2 * c + 1];
-    const int lane = threadIdx.x & 31;
-    constexpr int N = D / 32;
-    for (int w = blockIdx.y * (kMergeThreads / 32) + (threadIdx.x >> 5); w < e.x + e.y; w += gridDim.y * (kMergeThreads / 32)) {
-        const int second = w >= e.x ? 1 : 0;
-        const int r = second ? w - e.x : w;
-        const int at = second * 128 + r;
-        auto row_of = [&](int j) { return (j == 0 ? 2 * c + 1 : 2 * (c + j)) * 256 + at; };
-        float m = -CUDART_INF_F;
-        for (int j = lane; j < parts; j += 32) m = fmaxf(m, p.part_ml[row_of(j)].x);
-#pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        float l = 0.0f, acc[N] = {};
-        for (int j0 = 0; j0 < parts; j0 += 32) {
-            float wt = 0.0f, wl = 0.0f;
-            if (j0 + lane < parts) {
-                const float2 x = p.part_ml[row_of(j0 + lane)];
-                wt = x.x == -CUDART_INF_F ? 0.0f : attn_ex2(x.x - m);
-                wl = wt * x.y;
-            }
-            const int here = min(32, parts - j0);
-#pragma unroll 4
-            for (int u = 0; u < here; ++u) {
-                const float f = __shfl_sync(0xffffffffu, wt, u);
-                l += __shfl_sync(0xffffffffu, wl, u);
-                const float* src = p.part_o + static_cast<size_t>(row_of(j0 + u)) * D + lane * N;
-                if (N == 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(src);
-                    acc[0] = fmaf(f, v.x, acc[0]); acc[1] = fmaf(f, v.y, acc[1]);
-                    acc[2 % N] = fmaf(f, v.z, acc[2 % N]); acc[3 % N] = fmaf(f, v.w, acc[3 % N]);
-                } else {
-                    const float2 v = *reinterpret_cast<const float2*>(src);
-                    acc[0] = fmaf(f, v.x, acc[0]); acc[1] = fmaf(f, v.y, acc[1]);
-                }
-            }
-        }
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const int tok = d.y + r / p.group + second * d.w, head = d.z * p.group + r % p.group;
-        E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + lane * N;
-        if (N == 4)
-            *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[2 % N] * inv, acc[3 % N] * inv));
-        else
-            *reinterpret_cast<uint32_t*>(dst) = pack2<E>(acc[0] * inv, acc[1] * inv);
-        if (p.lse && lane == 0)
-            p.lse[static_cast<int64_t>(tok) * p.n_heads + head] = l == 0.0f ? -CUDART_INF_F : (m + log2f(l)) * 0.6931471805599453f;
-    }
 }
 
 }  // namespace wisv

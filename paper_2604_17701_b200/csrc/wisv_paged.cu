@@ -23,10 +23,10 @@ struct wisv_cache {
     int sm_count = 0;
     int page_shift = 0;
     int64_t launches = 0;
-    // one allocation: [error word | merge descriptors | partial maxima and sums | partial outputs]
+    // one allocation: [error word | arrival counters | partial maxima and sums | partial outputs]
     void* work = nullptr;
     int32_t* err = nullptr;
-    int4* desc = nullptr;
+    int32_t* count = nullptr;
     float2* part_ml = nullptr;
     float* part_o = nullptr;
     EncodeTiledFn encode = nullptr;
@@ -126,12 +126,11 @@ constexpr int kCommitOneBlockRequests = 64;
 
 // the smallest stretch of key tiles worth a block of its own: two run at the same time, one per warpgroup
 constexpr int kAttnMinUnits = 2;
-constexpr int kMergeRowBlocks = 8;
 
-// the attention kernel and, behind it with programmatic dependent launch, the merge of what its blocks share
+// Programmatic dependent launch: the block set-up (barriers, TMEM) runs while the kernel before it in the stream ends.
 template <typename E, int D>
 int launch_attn(const wisv_cache* c, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const AttnParams& p,
-                const AttnMerge& m, cudaStream_t st)
+                cudaStream_t st)
 {
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -145,10 +144,6 @@ int launch_attn(const wisv_cache* c, const CUtensorMap& tmQ, const CUtensorMap& 
     cfg.blockDim = dim3(kAttnThreads);
     cfg.dynamicSmemBytes = kAttnSmem;
     WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn_kernel<E, D>, tmQ, tmK, tmV, p));
-    cfg.gridDim = dim3((unsigned)c->sm_count, kMergeRowBlocks);
-    cfg.blockDim = dim3(kMergeThreads);
-    cfg.dynamicSmemBytes = 0;
-    WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn_merge_kernel<E, D>, m));
     return WISV_OK;
 }
 
@@ -197,15 +192,15 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
         cudaFuncSetAttribute(attn_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
     if (!ready) { (void)cudaGetLastError(); delete c; return WISV_ECUDA; }
     c->encode = reinterpret_cast<EncodeTiledFn>(fn);
-    const size_t n_ml = (size_t)sms * 2 * 256, off_desc = 256, off_ml = off_desc + (size_t)sms * 32,
-                 off_o = (off_ml + n_ml * 8 + 255) / 256 * 256;
+    const size_t n_ml = (size_t)sms * 2 * 256, off_count = 256,
+                 off_ml = (off_count + (size_t)sms * 4 + 255) / 256 * 256, off_o = (off_ml + n_ml * 8 + 255) / 256 * 256;
     if (cudaMalloc(&c->work, off_o + n_ml * cfg->head_dim * 4) != cudaSuccess) { (void)cudaGetLastError(); delete c; return WISV_ENOMEM; }
     char* w = static_cast<char*>(c->work);
     c->err = reinterpret_cast<int32_t*>(w);
-    c->desc = reinterpret_cast<int4*>(w + off_desc);
+    c->count = reinterpret_cast<int32_t*>(w + off_count);
     c->part_ml = reinterpret_cast<float2*>(w + off_ml);
     c->part_o = reinterpret_cast<float*>(w + off_o);
-    if (cudaMemset(c->err, 0, 256) != cudaSuccess || cudaStreamSynchronize(0) != cudaSuccess) {
+    if (cudaMemset(c->err, 0, off_ml) != cudaSuccess || cudaStreamSynchronize(0) != cudaSuccess) {
         (void)cudaGetLastError();
         cudaFree(c->work);
         delete c;
@@ -230,7 +225,8 @@ int wisv_cache_error(wisv_cache* c, void* cuda_stream, int32_t* flags)
     if (!c || !flags) return WISV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     WISV_TRY_CUDA(cudaMemcpyAsync(flags, c->err, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
-    WISV_TRY_CUDA(cudaMemsetAsync(c->err, 0, sizeof(int32_t), st));
+    // (a kernel that gave up may leave arrival counters behind)
+    WISV_TRY_CUDA(cudaMemsetAsync(c->err, 0, 256 + (size_t)c->sm_count * 4, st));
     WISV_TRY_CUDA(cudaStreamSynchronize(st));
     return WISV_OK;
 }
@@ -350,15 +346,13 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     p.table_stride = a->table_stride;
     p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;
     p.scale_log2 = (a->scale > 0.0f ? a->scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
-    p.err = c->err; p.part_o = c->part_o; p.part_ml = c->part_ml; p.desc = c->desc;
-    AttnMerge m;
-    m.part_o = p.part_o; m.part_ml = p.part_ml; m.desc = p.desc;
-    m.out = p.out; m.ot = p.ot; m.oh = p.oh; m.lse = p.lse; m.group = group; m.n_heads = c->cfg.n_heads;
+    p.inv_group = 1.0f / (float)group;
+    p.err = c->err; p.part_o = c->part_o; p.part_ml = c->part_ml; p.count = c->count;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool bf = c->cfg.dtype == WISV_DT_BF16;
-    if (D == 128) r = bf ? launch_attn<__nv_bfloat16, 128>(c, tmQ, tmK, tmV, p, m, st) : launch_attn<__half, 128>(c, tmQ, tmK, tmV, p, m, st);
-    else r = bf ? launch_attn<__nv_bfloat16, 64>(c, tmQ, tmK, tmV, p, m, st) : launch_attn<__half, 64>(c, tmQ, tmK, tmV, p, m, st);
-    if (r == WISV_OK) c->launches += 2;
+    if (D == 128) r = bf ? launch_attn<__nv_bfloat16, 128>(c, tmQ, tmK, tmV, p, st) : launch_attn<__half, 128>(c, tmQ, tmK, tmV, p, st);
+    else r = bf ? launch_attn<__nv_bfloat16, 64>(c, tmQ, tmK, tmV, p, st) : launch_attn<__half, 64>(c, tmQ, tmK, tmV, p, st);
+    if (r == WISV_OK) ++c->launches;
     return r;
 }
 
