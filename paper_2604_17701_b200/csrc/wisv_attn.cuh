@@ -41,6 +41,7 @@ constexpr int kAttnThreads = 512;
 constexpr int kAttnTile = 128;                   // rows of a row tile, keys of a key tile
 constexpr int kAttnSub = 64;                     // keys of a job
 constexpr int kAttnMaxStages = 12;
+constexpr int kAttnMinUnits = 2;                 // the smallest stretch worth a block of its own: shorter ones cost more to merge than they save
 constexpr int kAttnItemCost = 1;                 // key tiles that starting and finishing an item is worth
 constexpr int kAttnSmem = 232448;                // all of an SM's shared memory that a block can have
 constexpr int kAttnSmall = 2816;                 // barriers, the queue of stretches, the slots' exchange of m and l
@@ -48,7 +49,7 @@ constexpr int kAttnSlack = 256;                  // for aligning the tiles to 10
 constexpr uint64_t kAttnWaitClocks = 4000000000ull;
 
 struct AttnParams {
-    int32_t B, T, max_new, n_kv, group, tpt, page_shift, n_pages, max_blocks, min_units;
+    int32_t B, T, max_new, n_kv, group, tpt, page_shift, n_pages, max_blocks;
     int32_t page_groups_k, page_groups_v;        // 8-token groups from one page to the next
     int32_t groups_k, groups_v;                  // 8-token groups in the whole pool: the first coordinate out of range
     int32_t uniform;                             // rows per request where q_off is NULL
@@ -58,7 +59,7 @@ struct AttnParams {
     float* lse;
     float scale_log2, inv_group;
     int32_t* err;
-    float* part_o;                               // [2 * blocks][256][D]
+    float* part_o;                               // [2 * blocks][D / 4][256 rows][4]: rows side by side, as the lanes that write and read them
     float2* part_ml;                             // [2 * blocks][256]
     int32_t* count;                              // [blocks]: arrivals at the item that starts in a block's range and ends in another's; 0 between calls
 };
@@ -336,79 +337,69 @@ struct AttnWalk {
     }
 };
 
-// The merge of an item's partials by the eight softmax warps of the block that came last.  A warp takes four rows at a time, so
-// that enough loads are under way: the partials' maxima and sums first (lane: partial), then the outputs (lane: D / 32
-// columns), in block order.  Reads go past L1, which other blocks' writes do not reach.
+// The merge of an item's partials by the eight softmax warps of the block that came last.  A lane takes a row, a warp 32 rows and
+// 16 columns; four partials' maxima, sums and outputs are loaded together and put onto the running ones, in block order.  Reads
+// go past L1, which other blocks' writes do not reach.
 template <typename E, int D>
 __device__ __forceinline__ void attn_merge(const AttnParams& p, const int* sg, int w, int lane)
 {
-    constexpr int N = D / 32, R = 4;
-    // (through shuffles, so that the compiler knows the loops uniform: shuffles in loops that might diverge become calls)
-    const int first = sg[kSegFirst], parts = __shfl_sync(0xffffffffu, sg[kSegParts], 0), rows0 = sg[kSegRows0];
-    const int rows = __shfl_sync(0xffffffffu, rows0 + sg[kSegRows1], 0);
-    __threadfence();
-    for (int r0 = w * R; r0 < rows; r0 += 8 * R) {
-        // row i of the four: where its partials lie in a block's buffer (rows of the second tile from 128 on)
-        auto at = [&](int i) { const int r = min(r0 + i, rows - 1); return r < rows0 ? r : 128 + r - rows0; };
-        auto buffer = [&](int j) { return (j == 0 ? 2 * first + 1 : 2 * (first + j)) * 256; };
-        float m[R], l[R], acc[R][N];
+    constexpr int G = D / 16, U = 4;
+    // (through shuffles, so that the compiler knows the loops uniform)
+    const int parts = __shfl_sync(0xffffffffu, sg[kSegParts], 0);
+    const int rows0 = __shfl_sync(0xffffffffu, sg[kSegRows0], 0), rows1 = __shfl_sync(0xffffffffu, sg[kSegRows1], 0);
+    const int first = sg[kSegFirst], nb0 = (rows0 + 31) >> 5, nb = nb0 + ((rows1 + 31) >> 5);
+    for (int unit = w; unit < nb * G; unit += 8) {
+        const int rb = unit / G, g = unit % G;
+        const bool second = rb >= nb0;           // the second row tile's rows lie from 128 on
+        const int in = (second ? rb - nb0 : rb) * 32 + lane, at = in + (second ? 128 : 0);
+        float m = -CUDART_INF_F, l = 0.0f, acc[16];
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            m[i] = -CUDART_INF_F; l[i] = 0.0f;
+        for (int c = 0; c < 16; ++c) acc[c] = 0.0f;
+        for (int j0 = 0; j0 < parts; j0 += U) {
+            float2 x[U];
+            float4 v[U][4];
 #pragma unroll
-            for (int c = 0; c < N; ++c) acc[i][c] = 0.0f;
-        }
-        for (int j0 = 0; j0 < parts; j0 += 32) {
-            const int j = min(j0 + lane, parts - 1);
+            for (int u = 0; u < U; ++u) {
+                const int j = min(j0 + u, parts - 1), buf = j == 0 ? 2 * first + 1 : 2 * (first + j);
+                x[u] = __ldcg(p.part_ml + buf * 256 + at);
+                const float4* src = reinterpret_cast<const float4*>(p.part_o) + (static_cast<size_t>(buf) * (D / 4) + g * 4) * 256 + at;
 #pragma unroll
-            for (int i = 0; i < R; ++i) m[i] = fmaxf(m[i], __ldcg(p.part_ml + buffer(j) + at(i)).x);
-        }
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-#pragma unroll
-            for (int o = 16; o; o >>= 1) m[i] = fmaxf(m[i], __shfl_xor_sync(0xffffffffu, m[i], o));
-        for (int j0 = 0; j0 < parts; j0 += 32) {
-            float f[R], g[R];                    // lane's partial: its weight, and its weighted sum
-#pragma unroll
-            for (int i = 0; i < R; ++i) {
-                const float2 x = j0 + lane < parts ? __ldcg(p.part_ml + buffer(j0 + lane) + at(i)) : make_float2(-CUDART_INF_F, 0.0f);
-                f[i] = x.x == -CUDART_INF_F ? 0.0f : attn_ex2(x.x - m[i]);
-                g[i] = f[i] * x.y;
+                for (int c = 0; c < 4; ++c) v[u][c] = __ldcg(src + c * 256);
+                if (j0 + u >= parts) x[u] = make_float2(-CUDART_INF_F, 0.0f);
             }
-            const int here = min(32, parts - j0);
-#pragma unroll 2
-            for (int u = 0; u < here; ++u) {
-                const float* src = p.part_o + static_cast<size_t>(buffer(j0 + u)) * D + lane * N;
+            float mm = m;
 #pragma unroll
-                for (int i = 0; i < R; ++i) {
-                    const float fi = __shfl_sync(0xffffffffu, f[i], u);
-                    l[i] += __shfl_sync(0xffffffffu, g[i], u);
-                    if (N == 4) {
-                        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + at(i) * D));
-                        acc[i][0] = fmaf(fi, v.x, acc[i][0]); acc[i][1] = fmaf(fi, v.y, acc[i][1]);
-                        acc[i][2 % N] = fmaf(fi, v.z, acc[i][2 % N]); acc[i][3 % N] = fmaf(fi, v.w, acc[i][3 % N]);
-                    } else {
-                        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + at(i) * D));
-                        acc[i][0] = fmaf(fi, v.x, acc[i][0]); acc[i][1] = fmaf(fi, v.y, acc[i][1]);
-                    }
+            for (int u = 0; u < U; ++u) mm = fmaxf(mm, x[u].x);
+            const float f0 = m == -CUDART_INF_F ? 0.0f : attn_ex2(m - mm);
+            l *= f0;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) acc[c] *= f0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool some = x[u].x != -CUDART_INF_F;           // (else its outputs may be anything)
+                const float f = some ? attn_ex2(x[u].x - mm) : 0.0f;
+                l = fmaf(f, x[u].y, l);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    acc[4 * c] = some ? fmaf(f, v[u][c].x, acc[4 * c]) : acc[4 * c];
+                    acc[4 * c + 1] = some ? fmaf(f, v[u][c].y, acc[4 * c + 1]) : acc[4 * c + 1];
+                    acc[4 * c + 2] = some ? fmaf(f, v[u][c].z, acc[4 * c + 2]) : acc[4 * c + 2];
+                    acc[4 * c + 3] = some ? fmaf(f, v[u][c].w, acc[4 * c + 3]) : acc[4 * c + 3];
                 }
             }
+            m = mm;
         }
+        if (in < (second ? rows1 : rows0)) {
+            const float inv = l == 0.0f ? 0.0f : attn_rcp(l);
+            const int t = attn_token(p, in), tok = sg[kSegRow] + t + (second ? p.tpt : 0), head = sg[kSegHead] * p.group + in - t * p.group;
+            uint4* const dst = reinterpret_cast<uint4*>(static_cast<E*>(p.out) + tok * p.ot + head * p.oh + g * 16);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int r = r0 + i, in = r < rows0 ? r : r - rows0;
-            if (r >= rows) break;
-            const float inv = l[i] == 0.0f ? 0.0f : attn_rcp(l[i]);
-            const int t = attn_token(p, in), tok = sg[kSegRow] + t + (r < rows0 ? 0 : p.tpt);
-            const int head = sg[kSegHead] * p.group + in - t * p.group;
-            E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + lane * N;
-            if (N == 4)
-                *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<E>(acc[i][0] * inv, acc[i][1] * inv), pack2<E>(acc[i][2 % N] * inv, acc[i][3 % N] * inv));
-            else
-                *reinterpret_cast<uint32_t*>(dst) = pack2<E>(acc[i][0] * inv, acc[i][1] * inv);
-            if (p.lse && lane == 0)
+            for (int c = 0; c < 2; ++c)
+                dst[c] = make_uint4(pack2<E>(acc[8 * c] * inv, acc[8 * c + 1] * inv), pack2<E>(acc[8 * c + 2] * inv, acc[8 * c + 3] * inv),
+                                    pack2<E>(acc[8 * c + 4] * inv, acc[8 * c + 5] * inv), pack2<E>(acc[8 * c + 6] * inv, acc[8 * c + 7] * inv));
+            if (p.lse && g == 0)
                 p.lse[static_cast<int64_t>(tok) * (p.n_kv * p.group) + head] =
-                    l[i] == 0.0f ? -CUDART_INF_F : (m[i] + attn_lg2(l[i])) * 0.6931471805599453f;
+                    l == 0.0f ? -CUDART_INF_F : (m + attn_lg2(l)) * 0.6931471805599453f;
         }
     }
 }
@@ -502,7 +493,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range; [5]: whether this block came last
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
-    long long* totals = reinterpret_cast<long long*>(ml);                            // [16] scan over the warps, before that
+    unsigned* totals = reinterpret_cast<unsigned*>(ml);                              // [32] scan over the warps, before that
     static_assert(kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -532,58 +523,66 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     griddep_wait();                              // lengths, tables and the cache itself come from kernels before this one
     griddep_launch_dependents();
 
-    // ---- the block's range of the line of key tiles
-    long long total;
-    int blocks, me;
+    // ---- the block's range of the line of key tiles: `share` units each, one more for the first `more` blocks (the host has
+    // made sure that all of them together fit 31 bits, unless the offsets on the device overlap: then nothing is done and bit 2 of
+    // the error word set)
+    unsigned share, more;
+    const unsigned me = blockIdx.x;
     {
         const int per = (p.B + kAttnThreads - 1) / kAttnThreads;
         const int b0 = min(static_cast<int>(threadIdx.x) * per, p.B), b1 = min(b0 + per, p.B);
         auto units_of = [&](const AttnReq& r) {
-            long long u = 0;
+            unsigned u = 0;
             for (int i = 0; i < r.items; ++i) u += attn_tiles(p, r, i) + kAttnItemCost;
             return u;
         };
-        long long mine = 0;
-        for (int b = b0; b < b1; ++b) mine += units_of(attn_request(p, b)) * p.n_kv;
-        long long upto = mine;
+        unsigned long long sum = 0;
+        for (int b = b0; b < b1; ++b) sum += units_of(attn_request(p, b)) * p.n_kv;
+        const unsigned mine = static_cast<unsigned>(sum);
+        const unsigned high = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(min(sum >> 16, 1ull << 20)));
+        unsigned upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long x = __shfl_up_sync(0xffffffffu, upto, o);
+            const unsigned x = __shfl_up_sync(0xffffffffu, upto, o);
             if (lane >= o) upto += x;
         }
-        if (lane == 31) totals[warp] = upto;
+        if (lane == 31) { totals[warp] = upto; totals[16 + warp] = high; }
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-        total = 0;
+        unsigned total = 0, highs = 0;
+#pragma unroll
         for (int w = 0; w < kAttnThreads / 32; ++w) {
-            if (w < warp) upto += totals[w];
-            total += totals[w];
+            const unsigned x = totals[w];
+            highs += totals[16 + w];
+            upto += w < warp ? x : 0;
+            total += x;
         }
-        const long long want = total / p.min_units;
-        blocks = static_cast<int>(min(static_cast<long long>(gridDim.x), max(want, 1ll)));
-        me = blockIdx.x;
-        if (me < blocks && total > 0) {
-            const long long lo = me * total / blocks, hi = (me + 1) * total / blocks;
-            const long long first = upto - mine;
-            if (mine > 0 && lo >= first && lo < upto) {          // one thread's requests hold the start
-                long long x = lo - first;
-                for (int b = b0; b < b1; ++b) {
-                    const AttnReq r = attn_request(p, b);
-                    const long long one = units_of(r);
-                    if (x >= one * p.n_kv) { x -= one * p.n_kv; continue; }
-                    const int h = static_cast<int>(x / one);
-                    x -= h * one;
-                    int it = 0;
-                    for (; ; ++it) {
-                        const int u = attn_tiles(p, r, it) + kAttnItemCost;
-                        if (x < u) break;
-                        x -= u;
-                    }
-                    start[0] = b; start[1] = h; start[2] = it; start[3] = static_cast<int>(x);
-                    start[4] = static_cast<int>(hi - lo);
-                    break;
+        if (highs >= 0x7fffu) {
+            total = upto = 0;
+            if (threadIdx.x == 0) atomicOr(p.err, 4);
+        }
+        const unsigned blocks = min(gridDim.x, max(total / kAttnMinUnits, 1u));
+        share = total / blocks;
+        more = total - share * blocks;
+        const unsigned lo = me * share + min(me, more);
+        if (me < blocks && lo < upto && lo >= upto - mine) {     // one thread's requests hold the start
+            unsigned x = lo - (upto - mine);
+            for (int b = b0; b < b1; ++b) {
+                const AttnReq r = attn_request(p, b);
+                const unsigned one = units_of(r);
+                if (x >= one * p.n_kv) { x -= one * p.n_kv; continue; }
+                const unsigned h = x / one;
+                x -= h * one;
+                int it = 0;
+                for (; ; ++it) {
+                    const unsigned u = attn_tiles(p, r, it) + kAttnItemCost;
+                    if (x < u) break;
+                    x -= u;
                 }
+                start[0] = b; start[1] = h; start[2] = it; start[3] = x;
+                start[4] = share + (me < more ? 1 : 0);
+                break;
             }
         }
         __syncthreads();
@@ -605,12 +604,13 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const bool some = walk.next(p, s);
                 const int qi = item & (kSegQueue - 1);
                 if (some) {
-                    s[kSegFirst] = me; s[kSegParts] = 1;
+                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1;
                     if (s[kSegT0] > 0 || s[kSegT1] < s[kSegTiles]) {                 // shared: whose ranges does the item reach?
-                        const long long unit0 = (me + 1) * total / blocks - s[kSegLeft] - s[kSegT0], end = unit0 + s[kSegTiles];
-                        int first = me, last = me;
-                        while (first * total >= (unit0 + 1) * blocks) --first;
-                        while ((last + 1) * total < end * blocks) ++last;
+                        auto block_of = [&](unsigned u) {
+                            return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share;
+                        };
+                        const unsigned unit0 = (me + 1) * share + min(me + 1, more) - s[kSegLeft] - s[kSegT0];
+                        const unsigned first = block_of(unit0), last = block_of(unit0 + s[kSegTiles] - 1);
                         s[kSegFirst] = first; s[kSegParts] = last - first + 1;
                     }
                 }
@@ -878,7 +878,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 }
                 const bool valid = row < tile_rows, first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
                 const int c0 = paired ? 0 : slot * (D / 2), c1 = paired ? D : c0 + D / 2;
-                const int part_row = (static_cast<int>(blockIdx.x) * 2 + (first ? 1 : 0)) * 256 + (paired ? slot * 128 : 0) + row;
+                const int part = static_cast<int>(me) * 2 + (first ? 1 : 0), part_row = (paired ? slot * 128 : 0) + row;
                 const int t = attn_token(p, row), tok = sg[kSegRow] + t + (paired && slot ? p.tpt : 0);
                 const int head = sg[kSegHead] * p.group + row - t * p.group;
                 const float inv = l == 0.0f ? 0.0f : attn_rcp(l);
@@ -905,14 +905,13 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                                 make_uint4(pack2<E>(x[i], x[i + 1]), pack2<E>(x[i + 2], x[i + 3]), pack2<E>(x[i + 4], x[i + 5]),
                                            pack2<E>(x[i + 6], x[i + 7]));
                     } else if (valid) {
-                        float* const dst = p.part_o + static_cast<size_t>(part_row) * D + c;
+                        float4* const dst = reinterpret_cast<float4*>(p.part_o) + (static_cast<size_t>(part) * (D / 4) + c / 4) * 256 + part_row;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4)
-                            *reinterpret_cast<float4*>(dst + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+                        for (int i = 0; i < 32; i += 4) dst[i / 4 * 256] = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
                     }
                 }
                 if (valid && (paired || slot == 0)) {
-                    if (!whole) p.part_ml[part_row] = make_float2(m, l);
+                    if (!whole) p.part_ml[part * 256 + part_row] = make_float2(m, l);
                     else if (p.lse)
                         p.lse[static_cast<int64_t>(tok) * (p.n_kv * p.group) + head] =
                             l == 0.0f ? -CUDART_INF_F : (m + attn_lg2(l)) * 0.6931471805599453f;
@@ -923,21 +922,23 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             if (lane == 0) mbar_arrive(o_empty);
             tiles += sg[kSegT1] - sg[kSegT0];
             if (sg[kSegParts] > 1) {
-                // The item is shared: count this block's part, and if it is the last one to arrive, add all of them.
-                __threadfence();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(part_full);
-                ok = attn_wait_warp(part_full, splits & 1u, flag);
-                if (!ok) break;
+                // The item is shared: count this block's part, and if it is the last one to arrive, add all of them.  (One
+                // thread's fences stand for the block: the barriers before and after order the others' writes and reads.)
                 const int first_block = sg[kSegFirst], parts = sg[kSegParts];
-                if (warp == 8 && lane == 0) {
-                    const int before = atomicAdd(p.count + first_block, 1);
-                    start[5] = before == parts - 1;
-                    if (before == parts - 1) p.count[first_block] = 0;
-                    __threadfence();
-                    mbar_arrive(last_full);
+                if (lane == 0) mbar_arrive(part_full);
+                if (warp == 8) {
+                    ok = attn_wait_warp(part_full, splits & 1u, flag);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        __threadfence();
+                        const int before = atomicAdd(p.count + first_block, 1);
+                        start[5] = before == parts - 1;
+                        if (before == parts - 1) p.count[first_block] = 0;
+                        __threadfence();
+                        mbar_arrive(last_full);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
                 ok = attn_wait_warp(last_full, splits & 1u, flag);
                 if (!ok) break;
                 ++splits;

@@ -124,9 +124,6 @@ void fill_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B, PagesParam
 constexpr int kExtendOneBlockRows = 4096;
 constexpr int kCommitOneBlockRequests = 64;
 
-// the smallest stretch of key tiles worth a block of its own: two run at the same time, one per warpgroup
-constexpr int kAttnMinUnits = 2;
-
 // Programmatic dependent launch: the block set-up (barriers, TMEM) runs while the kernel before it in the stream ends.
 template <typename E, int D>
 int launch_attn(const wisv_cache* c, const CUtensorMap& tmQ, const CUtensorMap& tmK, const CUtensorMap& tmV, const AttnParams& p,
@@ -340,8 +337,11 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
         r = encode_5d(c, &tmQ, a->q, dims, strides, box);
         if (r != WISV_OK) return r;
     }
+    // every key tile of every item has to count in 31 bits, whatever the lengths on the device say
+    const int64_t items = (a->T + p.tpt - 1) / p.tpt + a->B, tiles = ((int64_t)a->max_blocks << c->page_shift) / kAttnTile + 2;
+    if (items * tiles > 0x7ffe0000LL / c->cfg.n_kv_heads) return WISV_ESHAPE;
     p.B = a->B; p.T = a->T; p.max_new = a->max_new; p.n_kv = c->cfg.n_kv_heads; p.group = group;
-    p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks; p.min_units = kAttnMinUnits;
+    p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
     p.uniform = a->max_new; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
     p.table_stride = a->table_stride;
     p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;

@@ -180,20 +180,24 @@ class PagedCache:
             raise WisvError(rc, name)
 
     def _rows(self, what, t, heads, rows=None):
-        s = t.shape
-        if t.dtype is not self.dtype or len(s) != 3 or s[1] != heads or s[2] != self.head_dim or \
-                (rows is not None and s[0] != rows) or t.get_device() != self._index or t.stride(2) != 1:
-            raise ValueError("%s must be [%s, %d, %d] %s on %s with a head's elements contiguous" %
-                             (what, "T" if rows is None else rows, heads, self.head_dim, self.dtype, self.device))
-        return t.data_ptr(), t.stride(0), t.stride(1)
+        """(address, token stride, head stride, rows) of [rows, heads, head_dim] rows."""
+        shape = t.shape
+        if len(shape) == 3 and t.dtype is self.dtype and t.get_device() == self._index:
+            n, h, d = shape
+            a, b, c = t.stride()
+            if h == heads and d == self.head_dim and c == 1 and (rows is None or n == rows):
+                return t.data_ptr(), a, b, n
+        raise ValueError("%s must be [%s, %d, %d] %s on %s with a head's elements contiguous" %
+                         (what, "T" if rows is None else rows, heads, self.head_dim, self.dtype, self.device))
 
     def _pages_of(self, what, t):
-        if t.dtype is not self.dtype or t.shape != self._pool or t.get_device() != self._index:
-            raise ValueError("%s must be [%d, %d, %d, %d] %s on %s" % ((what,) + self._pool + (self.dtype, self.device)))
-        st = t.stride()
-        if st[3] != 1:
-            raise ValueError("%s must keep a head's elements contiguous" % what)
-        return t.data_ptr(), st[0], st[1], st[2]
+        """(address, page stride, token stride, head stride) of a page pool."""
+        if t.shape == self._pool and t.dtype is self.dtype and t.get_device() == self._index:
+            a, b, c, d = t.stride()
+            if d == 1:
+                return t.data_ptr(), a, b, c
+        raise ValueError("%s must be [%d, %d, %d, %d] %s on %s with a head's elements contiguous" %
+                         ((what,) + self._pool + (self.dtype, self.device)))
 
     # ------------------------------------------------------------------ calls
     def extend(self, *, B: int, n_new, T: Optional[int] = None, out: Optional[WindowLayout] = None,
@@ -210,13 +214,16 @@ class PagedCache:
         ptr = None if uniform else _array("n_new", n_new, i32, B, dev)
         if out is None:
             # one allocation, the 64-bit slots first
-            slots, q_off, kv_len, status, positions = _empty(torch, stream, 3 * (T + B) + 1, i32, self.device).split_with_sizes(
-                (2 * T, B + 1, B, B, T))
+            buf = _empty(torch, stream, 3 * (T + B) + 1, i32, self.device)
+            slots, q_off, kv_len, status, positions = buf.split_with_sizes((2 * T, B + 1, B, B, T))
             out = WindowLayout(q_off, kv_len, slots.view(i64), positions, status)
-        lay = _pack_layout(_array("out.q_off", out.q_off, i32, B + 1, dev), _array("out.kv_len", out.kv_len, i32, B, dev),
-                           _array("out.slot_map", out.slot_map, i64, T, dev),
-                           _array("out.positions", out.positions, i32, T, dev),
-                           0 if out.status is None else _array("out.status", out.status, i32, B, dev))
+            at = buf.data_ptr()
+            lay = _pack_layout(at + 8 * T, at + 8 * T + 4 * (B + 1), at, at + 8 * T + 4 * (3 * B + 1), at + 8 * T + 4 * (2 * B + 1))
+        else:
+            lay = _pack_layout(_array("out.q_off", out.q_off, i32, B + 1, dev), _array("out.kv_len", out.kv_len, i32, B, dev),
+                               _array("out.slot_map", out.slot_map, i64, T, dev),
+                               _array("out.positions", out.positions, i32, T, dev),
+                               0 if out.status is None else _array("out.status", out.status, i32, B, dev))
         self._call("wisv_cache_extend", stream, self._pages_at, B, T, ptr, n_new if uniform else 0, lay)
         return out
 
@@ -225,15 +232,16 @@ class PagedCache:
         i32 = self._torch.int32
         if status is None:
             status = _empty(self._torch, stream, B, i32, self.device)
-        self._call("wisv_cache_commit", stream, self._pages_at, B, _array("new_len", new_len, i32, B, self._index),
-                   _array("status", status, i32, B, self._index))
+            at = status.data_ptr()
+        else:
+            at = _array("status", status, i32, B, self._index)
+        self._call("wisv_cache_commit", stream, self._pages_at, B, _array("new_len", new_len, i32, B, self._index), at)
         return status
 
     def append(self, k, v, k_pages, v_pages, slot_map, *, stream=None):
         """wisv_cache_append: one layer's new keys and values [T, n_kv_heads, head_dim] into their slots."""
-        T = k.shape[0]
-        kp, kt, kh = self._rows("k", k, self.n_kv_heads)
-        vp, vt, vh = self._rows("v", v, self.n_kv_heads, T)
+        kp, kt, kh, T = self._rows("k", k, self.n_kv_heads)
+        vp, vt, vh, _ = self._rows("v", v, self.n_kv_heads, T)
         kpool, k0, k1, k2 = self._pages_of("k_pages", k_pages)
         vpool, v0, v1, v2 = self._pages_of("v_pages", v_pages)
         self._call("wisv_cache_append", stream,
@@ -246,14 +254,16 @@ class PagedCache:
         themselves.  kv_len: int32 [B], new tokens included; q_off: int32 [B+1], or None for max_new rows each."""
         torch, dev = self._torch, self._index
         i32 = torch.int32
-        qp, qt, qh = self._rows("q", q, self.n_heads)
-        T = q.shape[0]
+        H, D = self.n_heads, self.head_dim
+        qp, qt, qh, T = self._rows("q", q, H)
         kpool, k0, k1, k2 = self._pages_of("k_pages", k_pages)
         vpool, v0, v1, v2 = self._pages_of("v_pages", v_pages)
         if out is None:
-            out = _empty(torch, stream, (T, self.n_heads, self.head_dim), self.dtype, self.device)
-        op, ot, oh = self._rows("out", out, self.n_heads, T)
-        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, self.n_heads) or
+            out = _empty(torch, stream, (T, H, D), self.dtype, self.device)
+            op, ot, oh = out.data_ptr(), H * D, D
+        else:
+            op, ot, oh, _ = self._rows("out", out, H, T)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, H) or
                                 not lse.is_contiguous() or lse.get_device() != dev):
             raise ValueError("lse must be a contiguous float32 [T, n_heads] tensor")
         if scale is not None and not scale > 0:
@@ -335,17 +345,21 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
     elif draft_ids is not None:
         raise ValueError("draft_ids without draft_probs")
     if out is None:
-        a, t, m, st = _empty(torch, stream, 4 * B, i32, target_probs.device).split_with_sizes((B, B, B, B))
+        buf = _empty(torch, stream, 4 * B, i32, target_probs.device)
+        a, t, m, st = buf.split_with_sizes((B, B, B, B))
         out = ResidualOutput(a, t, m.view(f32), st)
+        at = buf.data_ptr()
+        outs = (at, at + 4 * B, at + 8 * B, at + 12 * B)
+    else:
+        outs = (_array("out.accept_len", out.accept_len, i32, B, dev), _array("out.token", out.token, i32, B, dev),
+                0 if out.mass is None else _array("out.mass", out.mass, f32, B, dev),
+                0 if out.status is None else _array("out.status", out.status, i32, B, dev))
     r = _pack_residual(B, 0 if k_off is not None else K, 0 if k_off is None else _array("k_off", k_off, i32, B + 1, dev), T, V,
                        target_probs.data_ptr(), _row_stride(target_probs), tdt,
                        _array("draft_tokens", draft_tokens, i32, T, dev), qp, qs, qdt, ids, n_top,
                        0 if uniforms is None else _array("uniforms", uniforms, f32, T, dev),
                        _array("u_draw", u_draw, f32, B, dev),
-                       0 if accept_len is None else _array("accept_len", accept_len, i32, B, dev),
-                       _array("out.accept_len", out.accept_len, i32, B, dev), _array("out.token", out.token, i32, B, dev),
-                       0 if out.mass is None else _array("out.mass", out.mass, f32, B, dev),
-                       0 if out.status is None else _array("out.status", out.status, i32, B, dev))
+                       0 if accept_len is None else _array("accept_len", accept_len, i32, B, dev), *outs)
     s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
     if torch.cuda.current_device() != dev:
         with torch.cuda.device(dev):
