@@ -443,6 +443,8 @@ typedef struct {
     int32_t max_requests;   /* rows of the block table, 1..WISV_MAX_REQUESTS */
     int32_t max_blocks;     /* columns of the block table: a request holds at most max_blocks * page_size tokens */
     int32_t dtype;          /* WISV_DT_BF16 or WISV_DT_F16: keys, values, queries and outputs */
+    void*   workspace;      /* dev, 256-byte aligned, or NULL: allocated by wisv_cache_create */
+    int64_t workspace_bytes;
 } wisv_cache_config;
 
 /* bookkeeping arrays, all device memory of the caller */
@@ -464,9 +466,11 @@ typedef struct {
 } wisv_layout;
 
 /*
- * Create a cache context on the current device: checks the configuration and allocates the workspace of
- * wisv_cache_attend (partial results of the blocks; 2 * SMs * 256 rows).  *out is NULL on failure.
+ * Create a cache context on the current device: checks the configuration and takes the caller's workspace or allocates one
+ * (partial results of wisv_cache_attend: 2 * SMs * 256 rows, 39 MB at head_dim 128; wisv_cache_workspace says how
+ * much).  *out is NULL on failure.
  */
+int wisv_cache_workspace(const wisv_cache_config* cfg, int64_t* bytes);
 int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out);
 int wisv_cache_destroy(wisv_cache* cache);          /* the caller must have synchronised */
 int64_t wisv_cache_launch_count(const wisv_cache* cache);

@@ -162,9 +162,9 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
 }
 // 2^x of a pair by multiply-adds, for x <= 8 (below -126 as at -126): the nearest whole number goes to the exponent, the rest
 // r in [-1/2, 1/2] through the degree-4 polynomial with the least relative error there (2.6e-6; fitted by Remez's exchange).
-// The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both
-// matrix products; kAttnPoly of every 8 pairs go this way instead.
-constexpr int kAttnPoly = 2;
+// The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both matrix products;
+// kAttnPoly of every 8 pairs go this way instead (2048-row chunks under the power cap: 574, 566, 577, 592 us with 0 to 3).
+constexpr int kAttnPoly = 1;
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x)
 {
     const uint64_t magic = pair(12582912.0f, 12582912.0f), unmagic = pair(-12582912.0f, -12582912.0f);
@@ -516,6 +516,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tma_prefetch_desc(&tmK);
         tma_prefetch_desc(&tmV);
     }
+    // Rows of a row tile that the query box does not reach stay zero: the MMAs compute them all the same, and with zeros (and
+    // probabilities of zero, below) they cost far less of the power that caps the clock.
+    for (int i = threadIdx.x * 16; i < static_cast<int>(2 * kStage) && p.tpt * p.group < kAttnTile; i += kAttnThreads * 16)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(q_buf + i), "r"(0) : "memory");
+    fence_proxy_async();
     if (warp == 1) {
         tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
@@ -752,7 +757,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             if (J == 0) break;
             const bool paired = sg[kSegPaired];
             const int tile_rows = paired && slot ? sg[kSegRows1] : sg[kSegRows0];
-            const bool warp_has_rows = quad * 32 < tile_rows;
+            const bool warp_has_rows = quad * 32 < tile_rows, valid = row < tile_rows;
             const int key0 = sg[kSegT0] * kAttnTile + (paired ? 0 : slot * kAttnSub);
             const int step = paired ? kAttnSub : 2 * kAttnSub;                       // keys from one job of the slot to its next
             // columns of the job's keys past `cut` are masked for this row, rows of V from `have` on do not exist
@@ -784,7 +789,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     }
                     const float mt = max3_nan(max3_nan(mx[0], mx[1], s[60]), max3_nan(mx[2], mx[3], s[61]), max3_nan(s[62], s[63], s[63])) * p.scale_log2;
                     if (mt != mt) l = mt;                                            // a NaN score reaches the row's result
-                    const bool grow = mt > m + 8.0f;
+                    const bool grow = valid && mt > m + 8.0f;
                     if (__any_sync(0xffffffffu, grow)) {
                         const float m_new = grow ? mt : m;
                         const float a = grow ? attn_ex2(m - m_new) : 1.0f;
@@ -806,7 +811,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                             }
                         }
                     }
-                    base_m = m == -CUDART_INF_F ? 0.0f : -m;
+                    base_m = !valid ? -CUDART_INF_F : m == -CUDART_INF_F ? 0.0f : -m;
                 }
                 if (have < kAttnSub) {
                     // Value rows behind the last key: their probabilities are 0, but 0 times what happens to lie there could be
@@ -876,7 +881,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     l = l * wa + o.y * wb;
                     m = mm;
                 }
-                const bool valid = row < tile_rows, first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
+                const bool first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
                 const int c0 = paired ? 0 : slot * (D / 2), c1 = paired ? D : c0 + D / 2;
                 const int part = static_cast<int>(me) * 2 + (first ? 1 : 0), part_row = (paired ? slot * 128 : 0) + row;
                 const int t = attn_token(p, row), tok = sg[kSegRow] + t + (paired && slot ? p.tpt : 0);

@@ -24,7 +24,7 @@ struct wisv_cache {
     int page_shift = 0;
     int64_t launches = 0;
     // one allocation: [error word | arrival counters | partial maxima and sums | partial outputs]
-    void* work = nullptr;
+    void* work = nullptr;         // NULL: the caller's
     int32_t* err = nullptr;
     int32_t* count = nullptr;
     float2* part_ml = nullptr;
@@ -98,6 +98,36 @@ int encode_pool(const wisv_cache* c, CUtensorMap* out, const void* base, int64_t
     return encode_5d(c, out, base, dims, strides, box);
 }
 
+int check_config(const wisv_cache_config* cfg, int* dev, int* sms)
+{
+    if (cfg->dtype != WISV_DT_BF16 && cfg->dtype != WISV_DT_F16) return WISV_EINVAL;
+    if (cfg->n_kv_heads < 1 || cfg->n_heads < 1 || cfg->n_heads % cfg->n_kv_heads ||
+        cfg->n_heads / cfg->n_kv_heads > WISV_MAX_GROUP || cfg->n_kv_heads > 1024 ||
+        (cfg->head_dim != 64 && cfg->head_dim != 128) || cfg->page_size < 16 || cfg->page_size > 256 ||
+        log2_exact(cfg->page_size) < 0 || cfg->n_pages < 1 || cfg->max_requests < 1 ||
+        cfg->max_requests > WISV_MAX_REQUESTS || cfg->max_blocks < 1 ||
+        (int64_t)cfg->max_blocks * cfg->page_size > 0x7fff0000LL || (int64_t)cfg->n_pages * cfg->page_size > 0x7fff0000LL)
+        return WISV_ESHAPE;
+    int major = 0;       // attributes one by one: cudaGetDeviceProperties takes milliseconds
+    WISV_TRY_CUDA(cudaGetDevice(dev));
+    WISV_TRY_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, *dev));
+    WISV_TRY_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, *dev));
+    return major == 10 ? WISV_OK : WISV_EARCH;
+}
+
+// offsets in the workspace: error word at 0, arrival counters, partial maxima and sums, partial outputs
+struct Workspace { int64_t count, ml, o, bytes; };
+Workspace layout_of(const wisv_cache_config* cfg, int sms)
+{
+    Workspace w;
+    const int64_t rows = (int64_t)sms * 2 * 256;
+    w.count = 256;
+    w.ml = (w.count + (int64_t)sms * 4 + 255) / 256 * 256;
+    w.o = (w.ml + rows * 8 + 255) / 256 * 256;
+    w.bytes = w.o + rows * cfg->head_dim * 4;
+    return w;
+}
+
 int check_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B)
 {
     if (!c || !pg || !pg->free_list || !pg->n_free || !pg->block_table || !pg->n_blocks || !pg->seq_len) return WISV_EINVAL;
@@ -148,24 +178,25 @@ int launch_attn(const wisv_cache* c, const CUtensorMap& tmQ, const CUtensorMap& 
 
 extern "C" {
 
+int wisv_cache_workspace(const wisv_cache_config* cfg, int64_t* bytes)
+{
+    if (!cfg || !bytes) return WISV_EINVAL;
+    int dev = 0, sms = 0;
+    const int rc = check_config(cfg, &dev, &sms);
+    if (rc == WISV_OK) *bytes = layout_of(cfg, sms).bytes;
+    return rc;
+}
+
 int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
 {
     if (out) *out = nullptr;
     if (!cfg || !out) return WISV_EINVAL;
-    if (cfg->dtype != WISV_DT_BF16 && cfg->dtype != WISV_DT_F16) return WISV_EINVAL;
-    if (cfg->n_kv_heads < 1 || cfg->n_heads < 1 || cfg->n_heads % cfg->n_kv_heads ||
-        cfg->n_heads / cfg->n_kv_heads > WISV_MAX_GROUP || cfg->n_kv_heads > 1024 ||
-        (cfg->head_dim != 64 && cfg->head_dim != 128) || cfg->page_size < 16 || cfg->page_size > 256 ||
-        log2_exact(cfg->page_size) < 0 || cfg->n_pages < 1 || cfg->max_requests < 1 ||
-        cfg->max_requests > WISV_MAX_REQUESTS || cfg->max_blocks < 1 ||
-        (int64_t)cfg->max_blocks * cfg->page_size > 0x7fff0000LL || (int64_t)cfg->n_pages * cfg->page_size > 0x7fff0000LL)
-        return WISV_ESHAPE;
-    int dev = 0;
-    WISV_TRY_CUDA(cudaGetDevice(&dev));
-    int major = 0, sms = 0;       // attributes one by one: cudaGetDeviceProperties takes milliseconds
-    WISV_TRY_CUDA(cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev));
-    WISV_TRY_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    if (major != 10) return WISV_EARCH;
+    int dev = 0, sms = 0;
+    const int rc = check_config(cfg, &dev, &sms);
+    if (rc != WISV_OK) return rc;
+    const Workspace lay = layout_of(cfg, sms);
+    if (cfg->workspace && (reinterpret_cast<uintptr_t>(cfg->workspace) & 255u)) return WISV_EALIGN;
+    if (cfg->workspace && cfg->workspace_bytes < lay.bytes) return WISV_ECAPACITY;
     wisv_cache* c = new (std::nothrow) wisv_cache;
     if (!c) return WISV_ENOMEM;
     c->cfg = *cfg;
@@ -189,17 +220,19 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
         cudaFuncSetAttribute(attn_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
     if (!ready) { (void)cudaGetLastError(); delete c; return WISV_ECUDA; }
     c->encode = reinterpret_cast<EncodeTiledFn>(fn);
-    const size_t n_ml = (size_t)sms * 2 * 256, off_count = 256,
-                 off_ml = (off_count + (size_t)sms * 4 + 255) / 256 * 256, off_o = (off_ml + n_ml * 8 + 255) / 256 * 256;
-    if (cudaMalloc(&c->work, off_o + n_ml * cfg->head_dim * 4) != cudaSuccess) { (void)cudaGetLastError(); delete c; return WISV_ENOMEM; }
-    char* w = static_cast<char*>(c->work);
-    c->err = reinterpret_cast<int32_t*>(w);
-    c->count = reinterpret_cast<int32_t*>(w + off_count);
-    c->part_ml = reinterpret_cast<float2*>(w + off_ml);
-    c->part_o = reinterpret_cast<float*>(w + off_o);
-    if (cudaMemset(c->err, 0, off_ml) != cudaSuccess || cudaStreamSynchronize(0) != cudaSuccess) {
+    if (!cfg->workspace && cudaMalloc(&c->work, (size_t)lay.bytes) != cudaSuccess) {
         (void)cudaGetLastError();
-        cudaFree(c->work);
+        delete c;
+        return WISV_ENOMEM;
+    }
+    char* w = static_cast<char*>(cfg->workspace ? cfg->workspace : c->work);
+    c->err = reinterpret_cast<int32_t*>(w);
+    c->count = reinterpret_cast<int32_t*>(w + lay.count);
+    c->part_ml = reinterpret_cast<float2*>(w + lay.ml);
+    c->part_o = reinterpret_cast<float*>(w + lay.o);
+    if (cudaMemset(c->err, 0, (size_t)lay.ml) != cudaSuccess || cudaStreamSynchronize(0) != cudaSuccess) {
+        (void)cudaGetLastError();
+        if (c->work) cudaFree(c->work);
         delete c;
         return WISV_ECUDA;
     }
@@ -210,7 +243,7 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out)
 int wisv_cache_destroy(wisv_cache* c)
 {
     if (!c) return WISV_EINVAL;
-    cudaFree(c->work);
+    if (c->work) cudaFree(c->work);
     delete c;
     return WISV_OK;
 }

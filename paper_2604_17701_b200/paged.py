@@ -11,7 +11,8 @@ from .binding import DT_BF16, DT_F16, DT_F32, WisvError, _check, load_library
 
 class _CacheConfig(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_requests",
-                                         "max_blocks", "dtype")]
+                                         "max_blocks", "dtype")] + [("workspace", C.c_void_p),
+                                                                    ("workspace_bytes", C.c_int64)]
 
 
 class _Pages(C.Structure):
@@ -69,6 +70,7 @@ def _lib():
     if not _declared:
         P, I = C.c_void_p, C.c_int32                           # argument blocks go as packed bytes
         for name, args in (("wisv_cache_create", [C.POINTER(_CacheConfig), C.POINTER(P)]), ("wisv_cache_destroy", [P]),
+                           ("wisv_cache_workspace", [C.POINTER(_CacheConfig), C.POINTER(C.c_int64)]),
                            ("wisv_cache_error", [P, P, C.POINTER(I)]),
                            ("wisv_cache_extend", [P, P, I, I, P, I, P, P]), ("wisv_cache_commit", [P, P, I, P, P, P]),
                            ("wisv_cache_append", [P, P, P]), ("wisv_cache_attend", [P, P, P]),
@@ -132,8 +134,13 @@ class PagedCache:
             raise ValueError("the paged cache lives on a CUDA device")
         self.device = torch.device("cuda", torch.cuda.current_device() if device.index is None else device.index)
         cfg = _CacheConfig(n_heads, n_kv_heads, head_dim, page_size, n_pages, max_requests, max_blocks, dtype)
-        h = C.c_void_p()
+        h, need = C.c_void_p(), C.c_int64()
         with torch.cuda.device(self.device):
+            _check(self.lib.wisv_cache_workspace(C.byref(cfg), C.byref(need)), "wisv_cache_create")
+            self._workspace = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+            cfg.workspace, cfg.workspace_bytes = self._workspace.data_ptr(), need.value
+            # (the allocator orders the memory on the current stream, the library clears it on the default one)
+            torch.cuda.current_stream(self.device).synchronize()
             _check(self.lib.wisv_cache_create(C.byref(cfg), C.byref(h)), "wisv_cache_create")
         self._h = h
         self.n_heads, self.n_kv_heads, self.head_dim = n_heads, n_kv_heads, head_dim

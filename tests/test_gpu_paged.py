@@ -454,3 +454,52 @@ def test_refusals():
     assert cache.attend(q[:0], kp, kp, n, B=1, max_new=4, q_off=dev([0, 0])).shape == (0, 8, 64)
     assert cache.device_error() == 0
     cache.close()
+
+
+def test_a_workspace_of_the_callers():
+    import ctypes as C
+    from paper_2604_17701_b200 import paged
+    lib = paged._lib()
+    cfg = paged._CacheConfig(8, 2, 64, 16, 64, 8, 16, wisv.DT_BF16)
+    need, h = C.c_int64(), C.c_void_p()
+    assert lib.wisv_cache_workspace(C.byref(cfg), C.byref(need)) == 0 and need.value > 0
+    buf = torch.full((need.value + 256,), 255, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    for shift, size, code in ((8, need.value, -3), (0, need.value - 1, -4), (0, need.value, 0)):
+        cfg.workspace, cfg.workspace_bytes = buf.data_ptr() + shift, size
+        assert lib.wisv_cache_create(C.byref(cfg), C.byref(h)) == code
+        assert bool(h.value) == (code == 0)
+    flags = C.c_int32(9)
+    assert lib.wisv_cache_error(h, None, C.byref(flags)) == 0 and flags.value == 0     # cleared at create
+    assert lib.wisv_cache_destroy(h) == 0
+    cfg.workspace, cfg.workspace_bytes = None, 0                                       # one of its own
+    assert lib.wisv_cache_create(C.byref(cfg), C.byref(h)) == 0 and lib.wisv_cache_destroy(h) == 0
+
+
+def test_stale_workspace_does_not_matter():
+    """Everything a call reads of its workspace it has written itself (the arrival counters and the error word excepted)."""
+    n_new, kv_len = [9, 300], [3000, 1000]
+    cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=32, kv=8, d=128, page=16, dtype="bf16")
+    args = (q, kp, vp, dev(kv_len))
+    kw = dict(B=2, max_new=300, q_off=dev(q_off))
+    first = cache.attend(*args, **kw)
+    cache._workspace[1024:] = 255                              # NaN in every partial result
+    assert torch.equal(cache.attend(*args, **kw), first)
+    cache.close()
+
+
+def test_offsets_that_overlap_are_reported():
+    """Row offsets that run back and forth make more work than the line of key tiles can count: nothing runs, an error bit says so,
+    and the cache stays usable."""
+    B, T = 4096, 1 << 20
+    cache = make_cache(n_heads=1, n_kv_heads=1, page_size=256, max_requests=B, max_blocks=4096, n_pages=4)
+    q = torch.zeros(T, 1, 64, dtype=torch.bfloat16, device=DEV)
+    kp = torch.zeros(4, 256, 1, 64, dtype=torch.bfloat16, device=DEV)
+    off = torch.zeros(B + 1, dtype=torch.int32, device=DEV)
+    off[1::2] = T
+    # 2048 times all rows, each over up to 2^20 keys: 3e10 key tiles
+    cache.attend(q, kp, kp, torch.full((B,), 1 << 20, dtype=torch.int32, device=DEV), B=B, max_new=128, q_off=off)
+    assert cache.device_error() == 4 and cache.device_error() == 0
+    out = cache.attend(q[:5], kp, kp, dev([5]), B=1, max_new=5)
+    assert torch.isfinite(out).all() and cache.device_error() == 0
+    cache.close()
