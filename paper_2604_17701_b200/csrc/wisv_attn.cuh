@@ -596,9 +596,12 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P over its first half, O at 256 + 128 s
     int issued = 0, q_issued = 0;                // ring entries and query buffers filled (copying warps; read again before the end)
 
+    // Warps 0 and 4 idle: they share a scheduler with the softmax warps of rows 0 .. 31, the only ones at work where a row tile has
+    // few rows.  Warps 1, 2, 3, 5, 6, 7 are roles 0 .. 5.
+    const int role = warp > 7 || (warp & 3) == 0 ? -1 : warp < 4 ? warp - 1 : warp - 2;
     if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 0) {
+        if (role == 0) {
             // ------------------------------------------------------------ the work, and the TMA copies of queries and keys
             AttnWalk walk;
             walk.start(p, start);
@@ -642,7 +645,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 ok = ok && attn_load_tiles<D>(p, &tmK, p.page_groups_k, p.groups_k, s[kSegReq], s[kSegT0], s[kSegT1], s[kSegKeys],
                                               s[kSegHead], ring, bars, flag, lane, rg, issued);
             }
-        } else if (warp == 1 + kAttnMmaWarps) {
+        } else if (role == 1 + kAttnMmaWarps) {
             // ------------------------------------------------------------ the TMA copies of values (pages of 16 tokens are eight
             // copies a tile, some 80 clocks each: one warp for both would be late)
             AttnRing rg;
@@ -657,13 +660,13 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 __syncwarp();
                 if (ok && lane == 0) mbar_arrive(seg_empty(qi));
             }
-        } else if (warp < 1 + kAttnMmaWarps) {
+        } else if (role > 0) {
             // ------------------------------------------------------------ MMA: two warps issue S = Q K^T, one per slot, and two
             // O += P V.  Each waits (some 100 clocks and more behind its own products, barrier complete or not) under the
             // others' products.  Job n of a slot in a stretch: split: keys 64 slot .. of tile n; paired: keys 64 (n & 1) .. of
             // tile n / 2.
-            const int slot = (warp - 1) & 1;
-            const bool second = warp > 2;
+            const int slot = (role - 1) & 1;
+            const bool second = role > 2;
             const uint32_t idesc = second ? attn_idesc<E>(kAttnTile, D, true) : attn_idesc<E>(kAttnTile, kAttnSub, false);
             const uint32_t sS = tS + slot * 128, sO = tO + slot * 128;
             uint32_t used = 0;                   // jobs of this slot so far
@@ -732,7 +735,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 if (ok && second && lane == 0) mbar_arrive(seg_empty(qi));
             }
             if (!ok) {
-                const uint32_t mine = drain + 8 * (warp - 1);
+                const uint32_t mine = drain + 8 * (role - 1);
                 if (elect_one()) umma_commit(mine);
                 __syncwarp();
                 attn_wait(mine, 0, flag + 4);
@@ -955,9 +958,9 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     }
 
     __syncthreads();
-    if ((warp == 0 || warp == 1 + kAttnMmaWarps) && lane == 0 && abort_flag[0] != 0) {
+    if ((role == 0 || role == 1 + kAttnMmaWarps) && lane == 0 && abort_flag[0] != 0) {
         // after a time-out: the copies still in flight have to land before this block's shared memory is given up
-        const int kind = warp == 0 ? 0 : 1;
+        const int kind = role == 0 ? 0 : 1;
         for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
             const int e = 2 * i + kind;
             attn_wait(full_bar(e % kStages), static_cast<uint32_t>(e / kStages) & 1u, flag + 4);

@@ -47,7 +47,8 @@ int log2_exact(int x)
     return -1;
 }
 
-// one kernel on `st`, as a cluster of `cluster` blocks when that is more than 1
+// One kernel on `st`, as a cluster of `cluster` blocks when that is more than 1, with programmatic dependent launch: its blocks are
+// set up while the kernel before it in the stream ends, and wait for it (griddepcontrol.wait) before they read anything.
 template <typename P>
 int launch(void (*kernel)(P), int grid, int block, size_t smem, int cluster, cudaStream_t st, const P& p)
 {
@@ -57,15 +58,17 @@ int launch(void (*kernel)(P), int grid, int block, size_t smem, int cluster, cud
     cfg.blockDim = dim3((unsigned)block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
     if (cluster > 1) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)cluster;
-        attr[0].val.clusterDim.y = 1;
-        attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)cluster;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
     }
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, kernel, p));
     return WISV_OK;
 }

@@ -79,6 +79,8 @@ __global__ void __launch_bounds__(kPageThreads) pages_extend_kernel(const PagesP
     const int ctas = kClustered ? kPageCluster : 1;
     const int b0 = threadIdx.x * kPagePer;
     if (threadIdx.x == 0) taken = 0;
+    griddep_wait();
+    griddep_launch_dependents();
     int nv[kPagePer], sv[kPagePer], hv[kPagePer], cv[kPagePer];
     bool fits[kPagePer], bad[kPagePer];
     long long rows = 0, lack = 0;
@@ -168,6 +170,8 @@ __global__ void __launch_bounds__(kPageThreads) pages_commit_kernel(const PagesP
     const int rank = kClustered ? static_cast<int>(cluster_ctarank()) : 0;
     const int ctas = kClustered ? kPageCluster : 1;
     const int b0 = threadIdx.x * kPagePer;
+    griddep_wait();
+    griddep_launch_dependents();
     const int n_free = min(max(*p.n_free, 0), p.n_pages);
     int lv[kPagePer], kv[kPagePer], hv[kPagePer];
     bool bad[kPagePer];
@@ -241,6 +245,8 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(const AppendPara
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kAppendThreads + threadIdx.x;
     const int64_t t = i / p.vecs;
+    griddep_wait();
+    griddep_launch_dependents();
     if (t >= p.T) return;
     const int x = static_cast<int>(i - t * p.vecs);
     const int h = x >> p.vec_shift, e = x & ((1 << p.vec_shift) - 1);
