@@ -289,12 +289,6 @@ constexpr int kSegQueue = 4;
 struct AttnWalk {
     int b, kvh, it, pos, units;                  // position on the line of key tiles, and what is left of the range
     AttnReq r;
-
-    __device__ __forceinline__ void start(const AttnParams& p, const int* s)
-    {
-        b = s[0]; kvh = s[1]; it = s[2]; pos = s[3]; units = s[4];
-        if (units > 0) r = attn_request(p, b);
-    }
     // The next stretch; false at the end of the range.
     __device__ __forceinline__ bool next(const AttnParams& p, int (&s)[kSegWords])
     {
@@ -336,6 +330,68 @@ struct AttnWalk {
         return false;
     }
 };
+
+// This block's range of the line of key tiles, found by one warp: `share` units each, one more for the first `more` blocks.  (The host
+// has made sure that all of them together fit 31 bits, unless the offsets on the device overlap: then nothing is done and bit 2 of
+// the error word set.)
+template <int D>
+__device__ __forceinline__ void attn_range(const AttnParams& p, unsigned me, int lane, AttnWalk& w, unsigned& share, unsigned& more)
+{
+    const int per = (p.B + 31) >> 5, b0 = min(lane * per, p.B), b1 = min(b0 + per, p.B);
+    auto units_of = [&](const AttnReq& r) {
+        unsigned u = 0;
+        for (int i = 0; i < r.items; ++i) u += attn_tiles(p, r, i) + kAttnItemCost;
+        return u;
+    };
+    unsigned long long sum = 0;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) sum += units_of(attn_request(p, b)) * p.n_kv;
+    const unsigned mine = static_cast<unsigned>(sum);
+    const unsigned high = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(min(sum >> 16, 1ull << 20)));
+    unsigned upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    unsigned total = __shfl_sync(0xffffffffu, upto, 31);
+    if (high >= 0x7fffu) {
+        total = upto = 0;
+        if (lane == 0) atomicOr(p.err, 4);
+    }
+    const unsigned blocks = min(gridDim.x, max(total / kAttnMinUnits, 1u));
+    share = total / blocks;
+    more = total - share * blocks;
+    const unsigned lo = me * share + min(me, more);
+    w.b = w.kvh = w.it = w.pos = w.units = 0;
+    const bool mine_starts = me < blocks && lo < upto && lo >= upto - mine;          // one lane's requests hold the start
+    if (mine_starts) {
+        unsigned x = lo - (upto - mine);
+        for (int b = b0; b < b1; ++b) {
+            const AttnReq r = attn_request(p, b);
+            const unsigned one = units_of(r);
+            if (x >= one * p.n_kv) { x -= one * p.n_kv; continue; }
+            const unsigned h = x / one;
+            x -= h * one;
+            int it = 0;
+            for (; ; ++it) {
+                const unsigned u = attn_tiles(p, r, it) + kAttnItemCost;
+                if (x < u) break;
+                x -= u;
+            }
+            w.b = b; w.kvh = h; w.it = it; w.pos = x;
+            break;
+        }
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, mine_starts);
+    const int src = who ? __ffs(who) - 1 : 0;
+    w.b = __shfl_sync(0xffffffffu, w.b, src);
+    w.kvh = __shfl_sync(0xffffffffu, w.kvh, src);
+    w.it = __shfl_sync(0xffffffffu, w.it, src);
+    w.pos = __shfl_sync(0xffffffffu, w.pos, src);
+    w.units = who ? share + (me < more ? 1 : 0) : 0;
+    if (who) w.r = attn_request(p, w.b);
+}
 
 // The merge of an item's partials by the eight softmax warps of the block that came last.  A lane takes a row, a warp 32 rows and
 // 16 columns; four partials' maxima, sums and outputs are loaded together and put onto the running ones, in block order.  Reads
@@ -418,28 +474,29 @@ template <int D> __host__ __device__ constexpr int attn_stages()
                ? (kAttnSmem - kAttnSmall - kAttnSlack - 2 * attn_stage_bytes<D>()) / attn_stage_bytes<D>() : kAttnMaxStages;
 }
 
-// The copies of key (or value) tiles t0 .. t1 - 1 of a request into every other entry of the ring, by one warp.
+// Table entry of the lane's page (of at most 128 tokens) of key tile t; -1 where the tile has none.
+__device__ __forceinline__ int attn_page(const AttnParams& p, int req, int t, int t1, int keys, int lane)
+{
+    const int box_tok = min(1 << p.page_shift, kAttnTile), tok = t * kAttnTile + lane * box_tok;
+    return t < t1 && lane * box_tok < kAttnTile && tok < keys ? __ldg(p.block_table + req * p.table_stride + (tok >> p.page_shift)) : -1;
+}
+
+// The copies of key (or value) tiles t0 .. t1 - 1 of a request into every other entry of the ring, by one warp.  `pg`: attn_page
+// of tile t0; that of the next tile is read a tile ahead.
 template <int D>
-__device__ __forceinline__ bool attn_load_tiles(const AttnParams& p, const CUtensorMap* map, int page_groups, int groups, int req, int t0,
+__device__ __forceinline__ bool attn_load_tiles(const AttnParams& p, const CUtensorMap* map, int page_groups, int groups, int req, int pg, int t0,
                                                 int t1, int keys, int head, uint32_t ring, uint32_t bars, uint32_t flag, int lane,
                                                 AttnRing& rg, int& issued)
 {
     constexpr int kStages = attn_stages<D>();
     const int box_tok = min(1 << p.page_shift, kAttnTile);
     const uint32_t box_bytes = static_cast<uint32_t>(box_tok) * (D * 2);
-    const int32_t* table = p.block_table + req * p.table_stride;
-    // lane i: the first token group of the tile's i-th page.  The table entry of the next tile is read a tile ahead.
-    auto page_of = [&](int t) {
-        const int tok = t * kAttnTile + lane * box_tok;
-        return t < t1 && lane * box_tok < kAttnTile && tok < keys ? __ldg(table + (tok >> p.page_shift)) : -1;
-    };
-    int pg = page_of(t0);
     for (int t = t0; t < t1; ++t) {
         const int tok0 = t * kAttnTile;
         const int pages = max(min(keys - tok0, kAttnTile) + box_tok - 1, 0) / box_tok;               // that hold keys
         const int at = ((tok0 + lane * box_tok) & ((1 << p.page_shift) - 1)) >> 3;
         const int g = pg >= 0 && pg < p.n_pages ? pg * page_groups + at : groups;                    // out of range: zeros
-        pg = page_of(t + 1);
+        pg = attn_page(p, req, t + 1, t1, keys, lane);
         if (!attn_wait_warp(bars + 8u * (kAttnMaxStages + rg.s), rg.ph ^ 1u, flag)) return false;
         const uint32_t dst = ring + rg.s * attn_stage_bytes<D>(), bar = bars + 8u * rg.s;
         if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(pages) * box_bytes);
@@ -490,10 +547,10 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(small + 8 * (kBars + 9));
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);       // [0] abort, [1] drain scratch
     const uint32_t flag = bars + 8u * (kBars + 9) + 4u;
-    int* start = reinterpret_cast<int*>(tmem_slot + 3);                              // [5] start of the range; [5]: whether this block came last
+    volatile int* came_last = reinterpret_cast<volatile int*>(tmem_slot + 3);        // whether this block was the last at a shared item
+    const unsigned me = blockIdx.x;
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
-    unsigned* totals = reinterpret_cast<unsigned*>(ml);                              // [32] scan over the warps, before that
     static_assert(kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
@@ -510,7 +567,6 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 11); }
         mbar_init(o_full, 2); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(part_full, 8); mbar_init(last_full, 1); for (int s = 0; s < kAttnMmaWarps; ++s) mbar_init(drain + 8 * s, 1);
         abort_flag[0] = 0; abort_flag[1] = 0;
-        for (int i = 0; i < 5; ++i) start[i] = 0;
         fence_barrier_init();
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmK);
@@ -525,73 +581,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tmem_alloc(smem_u32(tmem_slot), 512);
         tmem_relinquish();
     }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
     griddep_wait();                              // lengths, tables and the cache itself come from kernels before this one
     griddep_launch_dependents();
-
-    // ---- the block's range of the line of key tiles: `share` units each, one more for the first `more` blocks (the host has
-    // made sure that all of them together fit 31 bits, unless the offsets on the device overlap: then nothing is done and bit 2 of
-    // the error word set)
-    unsigned share, more;
-    const unsigned me = blockIdx.x;
-    {
-        const int per = (p.B + kAttnThreads - 1) / kAttnThreads;
-        const int b0 = min(static_cast<int>(threadIdx.x) * per, p.B), b1 = min(b0 + per, p.B);
-        auto units_of = [&](const AttnReq& r) {
-            unsigned u = 0;
-            for (int i = 0; i < r.items; ++i) u += attn_tiles(p, r, i) + kAttnItemCost;
-            return u;
-        };
-        unsigned long long sum = 0;
-        for (int b = b0; b < b1; ++b) sum += units_of(attn_request(p, b)) * p.n_kv;
-        const unsigned mine = static_cast<unsigned>(sum);
-        const unsigned high = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(min(sum >> 16, 1ull << 20)));
-        unsigned upto = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const unsigned x = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += x;
-        }
-        if (lane == 31) { totals[warp] = upto; totals[16 + warp] = high; }
-        tc_fence_before();
-        __syncthreads();
-        tc_fence_after();
-        unsigned total = 0, highs = 0;
-#pragma unroll
-        for (int w = 0; w < kAttnThreads / 32; ++w) {
-            const unsigned x = totals[w];
-            highs += totals[16 + w];
-            upto += w < warp ? x : 0;
-            total += x;
-        }
-        if (highs >= 0x7fffu) {
-            total = upto = 0;
-            if (threadIdx.x == 0) atomicOr(p.err, 4);
-        }
-        const unsigned blocks = min(gridDim.x, max(total / kAttnMinUnits, 1u));
-        share = total / blocks;
-        more = total - share * blocks;
-        const unsigned lo = me * share + min(me, more);
-        if (me < blocks && lo < upto && lo >= upto - mine) {     // one thread's requests hold the start
-            unsigned x = lo - (upto - mine);
-            for (int b = b0; b < b1; ++b) {
-                const AttnReq r = attn_request(p, b);
-                const unsigned one = units_of(r);
-                if (x >= one * p.n_kv) { x -= one * p.n_kv; continue; }
-                const unsigned h = x / one;
-                x -= h * one;
-                int it = 0;
-                for (; ; ++it) {
-                    const unsigned u = attn_tiles(p, r, it) + kAttnItemCost;
-                    if (x < u) break;
-                    x -= u;
-                }
-                start[0] = b; start[1] = h; start[2] = it; start[3] = x;
-                start[4] = share + (me < more ? 1 : 0);
-                break;
-            }
-        }
-        __syncthreads();
-    }
     const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P over its first half, O at 256 + 128 s
     int issued = 0, q_issued = 0;                // ring entries and query buffers filled (copying warps; read again before the end)
@@ -604,7 +598,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         if (role == 0) {
             // ------------------------------------------------------------ the work, and the TMA copies of queries and keys
             AttnWalk walk;
-            walk.start(p, start);
+            unsigned share, more;
+            attn_range<D>(p, me, lane, walk, share, more);
             int s[kSegWords];
             AttnRing rg;
             bool ok = true;
@@ -631,6 +626,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 }
                 __syncwarp();
                 if (!some) break;
+                const int pg = attn_page(p, s[kSegReq], s[kSegT0], s[kSegT1], s[kSegKeys], lane);
                 // queries: one buffer per row tile
                 for (int t = 0; ok && t < (s[kSegPaired] ? 2 : 1); ++t, ++q_issued) {
                     const int qb = q_issued & 1;
@@ -642,7 +638,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     }
                     __syncwarp();
                 }
-                ok = ok && attn_load_tiles<D>(p, &tmK, p.page_groups_k, p.groups_k, s[kSegReq], s[kSegT0], s[kSegT1], s[kSegKeys],
+                ok = ok && attn_load_tiles<D>(p, &tmK, p.page_groups_k, p.groups_k, s[kSegReq], pg, s[kSegT0], s[kSegT1], s[kSegKeys],
                                               s[kSegHead], ring, bars, flag, lane, rg, issued);
             }
         } else if (role == 1 + kAttnMmaWarps) {
@@ -655,8 +651,9 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const int qi = item & (kSegQueue - 1);
                 ok = attn_wait_warp(seg_full(qi), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
                 if (!ok || queue[qi][kSegJobs] == 0) break;
-                ok = attn_load_tiles<D>(p, &tmV, p.page_groups_v, p.groups_v, queue[qi][kSegReq], queue[qi][kSegT0], queue[qi][kSegT1],
-                                        queue[qi][kSegKeys], queue[qi][kSegHead], ring, bars, flag, lane, rg, issued);
+                const int req = queue[qi][kSegReq], t0 = queue[qi][kSegT0], t1 = queue[qi][kSegT1], keys = queue[qi][kSegKeys];
+                ok = attn_load_tiles<D>(p, &tmV, p.page_groups_v, p.groups_v, req, attn_page(p, req, t0, t1, keys, lane), t0, t1, keys,
+                                        queue[qi][kSegHead], ring, bars, flag, lane, rg, issued);
                 __syncwarp();
                 if (ok && lane == 0) mbar_arrive(seg_empty(qi));
             }
@@ -940,7 +937,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     if (lane == 0) {
                         __threadfence();
                         const int before = atomicAdd(p.count + first_block, 1);
-                        start[5] = before == parts - 1;
+                        *came_last = before == parts - 1;
                         if (before == parts - 1) p.count[first_block] = 0;
                         __threadfence();
                         mbar_arrive(last_full);
@@ -950,7 +947,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 ok = attn_wait_warp(last_full, splits & 1u, flag);
                 if (!ok) break;
                 ++splits;
-                if (__shfl_sync(0xffffffffu, start[5], 0)) attn_merge<E, D>(p, sg, warp - 8, lane);
+                if (__shfl_sync(0xffffffffu, *came_last, 0)) attn_merge<E, D>(p, sg, warp - 8, lane);
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(seg_empty(item & (kSegQueue - 1)));
