@@ -5,7 +5,8 @@
 // (n_b) and in the free list (c_b); every new page and every new row then finds its request by a binary search in those
 // prefix sums, which shared memory holds.  pages_commit_kernel is the way back.
 //
-// What bounds them is latency: a launch, four dependent loads, two block-wide scans.  So everything happens in ONE launch:
+// What bounds them is latency: a launch, four dependent loads, two block-wide scans (extend and commit together 5.8 us for one
+// request, 10.2 us for 512 with 5632 rows).  So everything happens in ONE launch:
 // a single block for small rounds, a cluster of eight blocks for rounds with many rows, each of which repeats the
 // scan (cheaper than handing its result on) and takes its share of the pages and rows; the arrays that are
 // both read and written are written after a cluster barrier.
@@ -228,7 +229,8 @@ __global__ void __launch_bounds__(kPageThreads) pages_commit_kernel(const PagesP
 
 // ---------------------------------------------------------------- append
 // One thread moves 16 bytes of a key row and the same 16 bytes of the value row; a row of n_kv_heads * head_dim elements
-// takes `vecs` threads.  A plain stream: bound by HBM for long chunks, by the launch for a window.
+// takes `vecs` threads.  A plain stream: bound by HBM for long chunks (8192 rows of 8 x 128: 67 MB in 11.7 us, 5.7 TB/s), by the launch
+// for a window (1.6 us).
 struct AppendParams {
     int32_t T, vecs, vec_shift, page_shift;       // vec_shift: log2 of 16-byte pieces per head
     int64_t n_slots;
