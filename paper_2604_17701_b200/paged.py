@@ -85,9 +85,9 @@ def _lib():
 
 def _array(what, t, dtype, n, index):
     """Address of a contiguous tensor of the documented type, at least the documented size and on device `index`."""
-    if t.dtype is not dtype or not t.is_contiguous() or t.numel() < n or t.get_device() != index:
-        raise ValueError("%s must be a contiguous %s tensor with %d entries on cuda:%d" % (what, dtype, n, index))
-    return t.data_ptr()
+    if t.dtype is dtype and t.get_device() == index and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError("%s must be a contiguous %s tensor with %d entries on cuda:%d" % (what, dtype, n, index))
 
 
 def _row_stride(t) -> int:
@@ -160,7 +160,7 @@ class PagedCache:
         self._index = self.device.index
         self._row = (n_kv_heads, head_dim)
         self._pool = (n_pages, page_size, n_kv_heads, head_dim)
-        self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+        self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
     def close(self):
         if getattr(self, "_h", None):
@@ -177,8 +177,9 @@ class PagedCache:
     # ------------------------------------------------------------------ helpers
     def _call(self, name, stream, *args):
         """One library call with this cache's device current; the stream goes last."""
-        st = self._raw_stream(self._index) if stream is None else stream.cuda_stream
-        if self._current() != self._index:
+        index = self._index
+        st = self._raw_stream(index) if stream is None else stream.cuda_stream
+        if self._current() != index:
             with self._torch.cuda.device(self.device):
                 rc = getattr(self.lib, name)(self._h, *args, st)
         else:
@@ -298,6 +299,17 @@ class PagedCache:
         return int(self.lib.wisv_cache_launch_count(self._h))
 
 
+_residual_call = None
+
+
+def _torch_and_call():
+    global _residual_call
+    if _residual_call is None:
+        import torch
+        _residual_call = torch, _lib().wisv_verify_residual
+    return _residual_call
+
+
 @dataclass
 class ResidualOutput:
     accept_len: "object"
@@ -306,12 +318,14 @@ class ResidualOutput:
     status: "object" = None
 
 
-def _probs_dtype(torch, t) -> int:
-    dt = t.dtype
+def _probs(torch, t, index):
+    """(address, rows, columns, row stride, WISV_DT_*) of a matrix of probabilities on device `index`."""
+    dt, stride = t.dtype, t.stride()
     code = DT_F32 if dt is torch.float32 else DT_BF16 if dt is torch.bfloat16 else DT_F16 if dt is torch.float16 else None
-    if code is None or t.dim() != 2 or t.stride(1) != 1:
-        raise ValueError("probabilities must be 2-D float32, bfloat16 or float16 tensors with contiguous rows")
-    return code
+    if code is None or len(stride) != 2 or stride[1] != 1 or t.get_device() != index:
+        raise ValueError("probabilities must be 2-D float32, bfloat16 or float16 tensors with contiguous rows, on one device")
+    rows, columns = t.shape
+    return t.data_ptr(), rows, columns, stride[0] if rows > 1 else columns, code
 
 
 def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: int = 0, k_off=None,
@@ -324,24 +338,20 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
     [B], a verdict of Verifier.verify) the windows are taken as decided and only the token is drawn.
     Asynchronous on the current (or given) torch stream; nothing is kept between calls.
     """
-    import torch
-    lib = _lib()
+    torch, call = _torch_and_call()
     dev, i32, f32 = target_probs.get_device(), torch.int32, torch.float32
     if dev < 0:
         raise ValueError("target_probs must be a CUDA tensor")
     if T is None:
         T = B * K if k_off is None else draft_tokens.shape[0]
-    tdt = _probs_dtype(torch, target_probs)
-    rows, V = target_probs.shape
+    tp, rows, V, ts, tdt = _probs(torch, target_probs, dev)
     if rows < T + B:
         raise ValueError("target_probs must have T + B rows")
     qp, qs, qdt, n_top, ids = 0, 0, DT_F32, 0, 0
     if draft_probs is not None:
-        qdt = _probs_dtype(torch, draft_probs)
-        n, width = draft_probs.shape
-        if n < T or draft_probs.get_device() != dev:
-            raise ValueError("draft_probs must have T rows on the target's device")
-        qp, qs = draft_probs.data_ptr(), _row_stride(draft_probs)
+        qp, n, width, qs, qdt = _probs(torch, draft_probs, dev)
+        if n < T:
+            raise ValueError("draft_probs must have T rows")
         if draft_ids is not None:
             if qdt != DT_F32 or draft_ids.shape != draft_probs.shape:
                 raise ValueError("listed draft_probs are float32 and of draft_ids' shape")
@@ -362,15 +372,17 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
                 0 if out.mass is None else _array("out.mass", out.mass, f32, B, dev),
                 0 if out.status is None else _array("out.status", out.status, i32, B, dev))
     r = _pack_residual(B, 0 if k_off is not None else K, 0 if k_off is None else _array("k_off", k_off, i32, B + 1, dev), T, V,
-                       target_probs.data_ptr(), _row_stride(target_probs), tdt,
+                       tp, ts, tdt,
                        _array("draft_tokens", draft_tokens, i32, T, dev), qp, qs, qdt, ids, n_top,
                        0 if uniforms is None else _array("uniforms", uniforms, f32, T, dev),
                        _array("u_draw", u_draw, f32, B, dev),
                        0 if accept_len is None else _array("accept_len", accept_len, i32, B, dev), *outs)
     s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() != dev:
+    if torch._C._cuda_getDevice() != dev:
         with torch.cuda.device(dev):
-            _check(lib.wisv_verify_residual(r, s), "wisv_verify_residual")
+            rc = call(r, s)
     else:
-        _check(lib.wisv_verify_residual(r, s), "wisv_verify_residual")
+        rc = call(r, s)
+    if rc:
+        raise WisvError(rc, "wisv_verify_residual")
     return out
