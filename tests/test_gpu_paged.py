@@ -503,3 +503,20 @@ def test_offsets_that_overlap_are_reported():
     out = cache.attend(q[:5], kp, kp, dev([5]), B=1, max_new=5)
     assert torch.isfinite(out).all() and cache.device_error() == 0
     cache.close()
+
+
+def test_nan_keys_reach_the_rows_that_see_them_and_no_others():
+    n_new, kv_len = [6, 40], [500, 300]
+    for where in (3, 64, 65, 200, 297):                        # cached keys; the third new token of the second request
+        cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=4, kv=2, d=128, page=16, dtype="bf16", seed=where)
+        pg = int(cache.block_table[1, where // 16])
+        kp[pg, where % 16, 1] = float("nan")
+        out = cache.attend(q, kp, vp, dev(kv_len), B=2, max_new=40, q_off=dev(q_off))
+        bad = torch.isnan(out).all(2)
+        assert torch.equal(bad, torch.isnan(out).any(2))
+        want = torch.zeros_like(bad)
+        first = max(0, where - (300 - 40))                     # the first new row whose keys include it
+        want[6 + first:, 2:] = True
+        assert torch.equal(bad, want), where
+        assert cache.device_error() == 0
+        cache.close()
