@@ -465,6 +465,10 @@ __device__ __forceinline__ void attn_merge(const AttnParams& p, const int* sg, i
 }
 
 // Position in the ring of key and value tiles: tile g uses entries 2 g (keys) and 2 g + 1 (values).
+// The ring of key and value tiles, in turn.  A barrier's phase is one bit, so whoever waits for a fill (or a release) of a stage must know
+// that the one before it is past.  Here that hangs on S of a job being issued only after O of the slot's last job but one (s_free): the
+// values of tile t - 3, whose stage the keys of tile t take over where the stages are five, are then in, and the keys of tile t - 3
+// released only after the values of tile t - 5.  A product S that runs further ahead needs stages of keys and of values apart.
 struct AttnRing {
     int s = 0;
     uint32_t ph = 0;
@@ -685,8 +689,9 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const int J = jobs >> 1;
                 const int qb = (q_used + (paired ? slot : 0)) & 1;                   // the slot's query buffer
                 if (!second) {
-                    ok = attn_wait_warp(q_full(qb), static_cast<uint32_t>((q_used + (paired ? slot : 0)) >> 1) & 1u, flag);
-                    q_used += paired ? 2 : 1;
+                    // (a paired item's other buffer too, so that no warp skips a phase)
+                    for (const int end = q_used + (paired ? 2 : 1); ok && q_used < end; ++q_used)
+                        ok = attn_wait_warp(q_full(q_used & 1), static_cast<uint32_t>(q_used >> 1) & 1u, flag);
                 } else if (item > 0) {
                     ok = attn_wait_warp(o_empty, static_cast<uint32_t>(item - 1) & 1u, flag);         // the previous O has been read
                 }

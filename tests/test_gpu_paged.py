@@ -520,3 +520,23 @@ def test_nan_keys_reach_the_rows_that_see_them_and_no_others():
         assert torch.equal(bad, want), where
         assert cache.device_error() == 0
         cache.close()
+
+
+@pytest.mark.parametrize("rows, d, dtype", [(1, 128, "fp16"), (1, 64, "bf16"), (40, 128, "bf16")])
+def test_batches_that_fill_memory_bandwidth(rows, d, dtype):
+    """Every block works at a stretch of some twenty tiles of several requests, one or two row tiles each, keys and values arriving
+    later than they are asked for: whatever runs ahead has to stop for what it needs."""
+    rng = np.random.default_rng(rows + d)
+    B, H, kv, page = 96, 16, 4, 32
+    n_new = [1] * B if rows == 1 else [int(x) for x in rng.integers(1, rows + 1, B)]
+    kv_len = [int(x) for x in rng.integers(64, 5000, B)]
+    cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=H, kv=kv, d=d, page=page, dtype=dtype, seed=rows)
+    args = dict(B=B, max_new=max(n_new), q_off=dev(q_off))
+    length = dev(kv_len)
+    outs = [cache.attend(q, kp, vp, length, **args) for _ in range(6)]
+    ref = reference(q, kp.nan_to_num(0.0), vp.nan_to_num(0.0), cache.block_table, kv_len, q_off, d ** -0.5)
+    check(outs[0], None, ref, dtype, max(kv_len))
+    for o in outs[1:]:
+        assert torch.equal(o, outs[0])
+    assert cache.device_error() == 0
+    cache.close()
