@@ -7,7 +7,7 @@
 // more than 2^8 since its last rescaling: P then stays below 2^8, which loses nothing in a floating-point type.
 //
 // Measured (8B shape: 32 query heads, 8 key heads, D = 128): 64 requests of one row over 258 k keys in all 165 us, 6.4 TB/s, 0.98 of the
-// copy rate, 175-184 us back to back under the power cap; 2 x 2048 rows over 8 k keys 485-500 us, 1.1 PFLOP/s, 561-567 us under the
+// copy rate, 175-187 us back to back under the power cap; 2 x 2048 rows over 8 k keys 485-500 us, 1.1 PFLOP/s, 561-571 us under the
 // cap; one request of 9 rows over 709 keys 12.2 us.
 //
 // What bounds it.  A window of K + 1 rows has group * (K + 1) rows per key head, so up to some 64 of them the kernel moves
