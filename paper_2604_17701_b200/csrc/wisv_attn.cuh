@@ -15,12 +15,12 @@
 // keys at D = 128) is faster than its 64 KB of keys and values (some 2800 clocks at a 148th of the measured copy
 // rate).  Prompt chunks are bound by the MMAs and by the exponentials, 1024 clocks each per 128 x 128 tile.
 //
-// Roles.  One block per SM, persistent: a warp that walks the work and issues the TMA copies, four warps that issue the
-// MMAs, and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
+// Roles.  One block per SM, persistent: a warp that walks the work and copies queries and keys by TMA, one that copies values, four
+// that issue the MMAs (S and O of each slot), and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
 // "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
 // single row tile is left, "split": the slots take the key tiles in turn and are put together at the end.  Either way
-// the jobs (row tile, key tile) alternate between the slots, and the MMA warp issues S of job j + 2 behind O of job j,
-// so one slot's exponentials run under the other's MMAs.
+// the slots work at different 64-key jobs, and each has two S of 64 columns in turn: S of a job waits for O of the slot's last job but
+// one alone, so it is computed under the exponentials of the job before and under the other slot's products.
 //
 // Work split.  The key tiles of all items form one line, cut into equal contiguous ranges, one per block; every block finds
 // its range from the lengths on the device, so the host knows no lengths and a captured graph stays balanced.  An item cut by a
