@@ -103,6 +103,12 @@ def _empty(torch, stream, shape, dtype, device):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
+def _full(torch, stream, shape, value, dtype, device):
+    """torch.full on `stream` (None: the current one)."""
+    with torch.cuda.stream(stream):
+        return torch.full(shape, value, dtype=dtype, device=device)
+
+
 @dataclass
 class WindowLayout:
     """What PagedCache.extend lays out for a round (see wisv_layout)."""
@@ -333,9 +339,10 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
                     out: Optional[ResidualOutput] = None, stream=None) -> ResidualOutput:
     """wisv_verify_residual: verify drafts against the target's probabilities [T + B, V] and draw the next token.
 
-    draft_probs: the drafter's distributions, [T, V] dense, or float32 [T, n_top] with draft_ids int32 [T, n_top], or
-    None for a deterministic drafter.  uniforms [T] decide acceptance, u_draw [B] the token.  With accept_len (int32
-    [B], a verdict of Verifier.verify) the windows are taken as decided and only the token is drawn.
+    draft_probs: the drafter's distributions, [T, V] dense, or float32 [T, n_top] with draft_ids int32 [T, n_top] (n_top = 0
+    names no token: Q is 0 everywhere), or None for a deterministic drafter.  uniforms [T] decide acceptance, u_draw [B]
+    the token.  With accept_len (int32 [B], a verdict of Verifier.verify) the windows are taken as decided and only the
+    token is drawn.
     Asynchronous on the current (or given) torch stream; nothing is kept between calls.
     """
     torch, call = _torch_and_call()
@@ -355,6 +362,11 @@ def verify_residual(target_probs, draft_tokens, uniforms, u_draw, *, B: int, K: 
         if draft_ids is not None:
             if qdt != DT_F32 or draft_ids.shape != draft_probs.shape:
                 raise ValueError("listed draft_probs are float32 and of draft_ids' shape")
+            if width == 0:
+                # lists without entries name no token; torch gives them the address 0, which stands for a deterministic drafter
+                draft_ids = _full(torch, stream, (T, 1), -1, i32, target_probs.device)
+                draft_probs = _full(torch, stream, (T, 1), 0.0, f32, target_probs.device)
+                qp, qs, width = draft_probs.data_ptr(), 1, 1
             n_top = width
             ids = _array("draft_ids", draft_ids, i32, T * n_top, dev)
         elif width != V:

@@ -274,3 +274,18 @@ def test_refusals():
         with pytest.raises(wisv.WisvError) as e:
             wisv.verify_residual(**{**good, **bad})
         assert e.value.code == code
+
+
+@pytest.mark.parametrize("dtype, accept", [("fp32", None), ("bf16", None), ("fp16", [1, 0, 2, 3])])
+def test_an_empty_list_names_no_token(dtype, accept):
+    """Lists of no entries: Q is 0 everywhere, so a draft is accepted iff P(y) > 0 and the token is drawn from P."""
+    c = make([2, 0, 5, 3], 700, dtype, "top", 4, seed=12)
+    c["Q"], c["ids"] = c["Q"][:, :0], c["ids"][:, :0]
+    c["P"][1, c["tokens"][1]] = 0.0                             # request 0 stops at its second draft
+    want = check(c, call(c, accept), accept)
+    assert accept is not None or want[0].tolist() == [1, 0, 5, 3]
+    for side in (torch.cuda.Stream(),):
+        side.wait_stream(torch.cuda.current_stream())
+        r = call(c, accept, stream=side)
+        side.synchronize()
+        check(c, r, accept)
