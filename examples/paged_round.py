@@ -8,7 +8,8 @@ sends K drafted tokens per round and the drafter's distribution; one round is
     PagedCache.attend          per layer: the window over everything cached
     Verifier.verify            the LM head and the decision head on the final hidden states: what is accepted
     verify_residual            the token behind the accepted drafts, drawn from max(P - Q, 0) or, for a full accept, from P
-    PagedCache.commit          the kept lengths; pages of rejected drafts go back to the pool
+    PagedCache.commit          the kept lengths; pages of rejected drafts go back to the pool (a request that the pool had no
+                               pages for keeps its old length)
 
 Lengths, verdicts and pages stay on the device; the host sees tokens only when it prints them.
 
@@ -90,10 +91,18 @@ class Server:
         n_new = torch.tensor(lengths, dtype=torch.int32, device=self.model.device)
         layout = self.cache.extend(B=self.B, n_new=n_new, T=sum(lengths))
         self.forward(tokens, layout, max(lengths))
-        self.cache.commit(layout.kv_len - 1, B=self.B)             # the last token is the first row of the next window
+        self.commit(layout, layout.kv_len - 1)                     # the last token is the first row of the next window
+
+    def commit(self, layout, new_len):
+        """Keeps new_len tokens of the requests that the round served and the old length of the others; returns who was served.
+        (A request that got no pages has kv_len 0: nothing of its window is cached.)"""
+        served = layout.kv_len > 0
+        self.cache.commit(torch.where(served, new_len, self.cache.seq_len[:self.B]), B=self.B)
+        return served
 
     def round(self, last, drafts, draft_probs, draft_hidden, csi, u, u_draw, semantic=True):
-        """One window per request: `last` [B] the newest token, `drafts` [B, K].  Returns (accepted [B], next token [B])."""
+        """One window per request: `last` [B] the newest token, `drafts` [B, K].  Returns (accepted [B], next token [B]); a request
+        that got no pages is not served: -1 accepted, and its newest token again."""
         B, K = self.B, self.K
         tokens = torch.cat([last[:, None], drafts], 1).reshape(-1)
         layout = self.cache.extend(B=B, n_new=K + 1)
@@ -106,8 +115,8 @@ class Server:
                                             draft_q=draft_probs.gather(1, flat.long()[:, None])[:, 0].contiguous(),
                                             uniforms=u).accept_len
         res = wisv.verify_residual(probs, flat, u, u_draw, B=B, K=K, draft_probs=draft_probs, accept_len=accepted)
-        self.cache.commit(self.cache.seq_len[:B] + res.accept_len + 1, B=B)
-        return res.accept_len, res.token
+        served = self.commit(layout, self.cache.seq_len[:B] + res.accept_len + 1)
+        return torch.where(served, res.accept_len, -1), torch.where(served, res.token, last)
 
     def close(self):
         self.verifier.close()
@@ -135,7 +144,8 @@ def serve(requests=4, rounds=6, drafts=5, seed=0, semantic=True, device="cuda:0"
         hidden = torch.randn((requests * drafts, 64), generator=g, device=device)
         accepted, token = server.round(last, draft, q, hidden, csi, rand(requests * drafts), rand(requests), semantic)
         for b in range(requests):                                  # (for the printout only: the cache does not need it)
-            text[b] = torch.cat([text[b], draft[b, :accepted[b]], token[b:b + 1]])
+            if accepted[b] >= 0:
+                text[b] = torch.cat([text[b], draft[b, :accepted[b]], token[b:b + 1]])
         last = token
         history.append(accepted.clone())
     return server, text, torch.stack(history)
@@ -148,7 +158,7 @@ def main():
     ap.add_argument("--drafts", type=int, default=5)
     a = ap.parse_args()
     server, text, accepted = serve(a.requests, a.rounds, a.drafts)
-    print("accepted drafts per round (rows) and request (columns):\n%s" % accepted.cpu())
+    print("accepted drafts per round (rows) and request (columns; -1: no pages):\n%s" % accepted.cpu())
     print("kept tokens %s, free pages %d of %d" % (server.cache.seq_len.tolist(), server.cache.n_free.item(),
                                                    server.cache.n_pages))
     for b, t in enumerate(text):

@@ -492,7 +492,9 @@ int wisv_cache_extend(wisv_cache* cache, const wisv_pages* pages, int32_t B, int
 
 /*
  * The lengths that the verdict leaves: seq_len[b] = new_len[b] (dev [B]), for instance seq_len + accept_len + 1, or 0 for
- * a finished request.  Pages behind the new length go back to the end of the free list, requests ascending, blocks
+ * a finished request.  A request that wisv_cache_extend gave no pages (WISV_ST_NO_PAGES, kv_len 0) has nothing of its window
+ * in the cache: commit its old length, seq_len, whatever the verdict on its rows says.  (No call can tell: the new
+ * length may still fit the pages that it held before.)  Pages behind the new length go back to the end of the free list, requests ascending, blocks
  * ascending, so that a round that is withdrawn entirely leaves the free list as it was.  A length that is negative or
  * longer than the pages held is clamped and flagged WISV_ST_BAD_LENGTH in status (dev [B], optional).
  */

@@ -242,7 +242,9 @@ class PagedCache:
         return out
 
     def commit(self, new_len, *, B: int, status=None, stream=None):
-        """wisv_cache_commit: the kept length of each request (int32 [B]); pages behind it go back.  Returns status."""
+        """wisv_cache_commit: the kept length of each request (int32 [B]); pages behind it go back.  Returns status.
+        A request that extend flagged (status WISV_ST_NO_PAGES, kv_len 0) keeps its old length, seq_len: nothing of its window
+        is cached."""
         i32 = self._torch.int32
         if status is None:
             status = _empty(self._torch, stream, B, i32, self.device)

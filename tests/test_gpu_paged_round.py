@@ -46,3 +46,29 @@ def test_rounds_agree_with_a_model_without_a_cache(semantic):
     if semantic:
         assert accepted.max() > 0                                  # the decision head keeps some drafts of random drafters
     server.close()
+
+
+def test_a_request_that_gets_no_pages_keeps_its_length():
+    """Rounds beyond what a request's row of the table can hold: it is not served, and nothing that was not cached is kept."""
+    from paged_round import serve
+    server, text, accepted = serve(requests=2, rounds=250, drafts=5)
+    cache, model = server.cache, server.model
+    most = cache.max_blocks * cache.page_size
+    assert (accepted < 0).any() and (accepted >= 0).any()          # a round that is not served is marked
+    for b, t in enumerate(text):
+        kept = len(t) - 1
+        assert cache.seq_len[b].item() == kept and most - 6 < kept <= most
+        assert len(t) == 7 + 9 * b + sum(a + 1 for a in accepted[:, b].tolist() if a >= 0)
+    # the keys of the first layer are those of the whole sequence
+    for b, t in enumerate(text):
+        rows = {}
+
+        def attention(i, q, k, v):
+            rows.setdefault(i, k)
+            return torch.zeros_like(q)
+        model.forward(t, attention)
+        pos = torch.arange(len(t) - 1, device=t.device)
+        got = server.pools[0][0][cache.block_table[b].long()[pos // 16], pos % 16]
+        # the same products of other batch sizes: a rounding of bf16 apart
+        assert (got.float() - rows[0][:-1].float()).abs().max() <= 2.0 ** -6 * rows[0].float().abs().max()
+    server.close()
