@@ -797,7 +797,9 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                         for (int i = 0; i < 4; ++i) mx[i] = max3_nan(mx[i], s[c + 2 * i], s[c + 2 * i + 1]);
                     }
                     const float mt = max3_nan(max3_nan(mx[0], mx[1], s[60]), max3_nan(mx[2], mx[3], s[61]), max3_nan(s[62], s[63], s[63])) * p.scale_log2;
-                    if (mt != mt) l = mt;                                            // a NaN score reaches the row's result
+                    // A score of NaN or +inf makes the row NaN, whichever way its exponential goes (the polynomial's clamp
+                    // would turn inf - inf into a small weight).
+                    if (!(mt < CUDART_INF_F)) l = CUDART_NAN_F;
                     const bool grow = valid && mt > m + 8.0f;
                     if (__any_sync(0xffffffffu, grow)) {
                         const float m_new = grow ? mt : m;
