@@ -164,21 +164,23 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of a pair by multiply-adds, for x <= 8 (below -126 as at -126): the nearest whole number goes to the exponent, the rest
-// r in [-1/2, 1/2] through the degree-4 polynomial with the least relative error there (2.6e-6; fitted by Remez's exchange).
+// 2^x of a pair by multiply-adds, for x <= 8: the nearest whole number goes to the exponent, the rest r in [-1/2, 1/2] through the
+// degree-4 polynomial that is 1 at r = 0 and has the least relative error there (2.8e-6; fitted by linear programming, 2.9e-6 in
+// fp32).  From x = -127 down it gives 0 exactly (the exponent of 1 less 127 is that of 0), as a masked score must; between -126 and
+// -127 something below 2^-126.
 // The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both matrix products;
 // kAttnPoly of every 8 pairs go this way instead (2048-row chunks under the power cap: 574, 566, 577, 592 us with 0 to 3).
 constexpr int kAttnPoly = 1;
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x)
 {
     const uint64_t magic = pair(12582912.0f, 12582912.0f), unmagic = pair(-12582912.0f, -12582912.0f);
-    x = pair(fmaxf(low(x), -126.0f), fmaxf(high(x), -126.0f));
+    x = pair(fmaxf(low(x), -127.0f), fmaxf(high(x), -127.0f));
     const uint64_t t = add2(x, magic);                       // the whole number in the low bits
     const uint64_t r = fma2(add2(t, unmagic), pair(-1.0f, -1.0f), x);
-    uint64_t y = fma2(r, pair(9.570102207e-3f, 9.570102207e-3f), pair(5.591785908e-2f, 5.591785908e-2f));
-    y = fma2(y, r, pair(2.402474433e-1f, 2.402474433e-1f));
-    y = fma2(y, r, pair(6.931217909e-1f, 6.931217909e-1f));
-    y = fma2(y, r, pair(9.999992847e-1f, 9.999992847e-1f));
+    uint64_t y = fma2(r, pair(9.585382417e-3f, 9.585382417e-3f), pair(5.590662733e-2f, 5.590662733e-2f));
+    y = fma2(y, r, pair(2.402403802e-1f, 2.402403802e-1f));
+    y = fma2(y, r, pair(6.931241751e-1f, 6.931241751e-1f));
+    y = fma2(y, r, pair(1.0f, 1.0f));
     const uint32_t a = static_cast<uint32_t>(t) * 0x800000u + static_cast<uint32_t>(y);
     const uint32_t b = static_cast<uint32_t>(t >> 32) * 0x800000u + static_cast<uint32_t>(y >> 32);
     return pair(__uint_as_float(a), __uint_as_float(b));
@@ -841,8 +843,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     fence_proxy_async();
                 }
                 if (warp_has_rows) {
-                    // A masked score's exponential is 0 from the special-function unit and 2^-126 from the polynomial, against
-                    // numerators of 2^-8 and more in any row that sees a key; a row that sees none is told by its maximum.
+                    // A masked score's exponential is 0 both ways, so that a finite value behind it adds nothing, however large.
                     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), base2 = pair(base_m, base_m);
                     uint64_t sum[2] = {0, 0};
 #pragma unroll

@@ -18,6 +18,21 @@ def place(cache, pool, b, key, head, column, value):
     pool[int(cache.block_table[b, key // page]), key % page, head, column] = value
 
 
+@pytest.mark.parametrize("n, L", [(40, 300), (9, 709), (300, 300)])
+def test_large_values_do_not_reach_rows_that_do_not_see_them(n, L):
+    """Values near the type's largest number: times anything but 0 they would show."""
+    H, kv, d = 8, 2, 128
+    cache, q, kp, vp, q_off = build(n_new=[n], kv_len=[L], H=H, kv=kv, d=d, page=16, dtype="bf16", seed=n)
+    ref = reference(q, kp.nan_to_num(0.0), vp.nan_to_num(0.0), cache.block_table, [L], q_off, d ** -0.5)
+    first = n // 3                                                 # new tokens from here on hold large values
+    for key in range(L - n + first, L):
+        place(cache, vp, 0, key, slice(None), slice(None), 3e38)
+    for hint in (n, 1):
+        out = cache.attend(q, kp, vp, dev([L]), B=1, max_new=hint, q_off=dev(q_off))
+        check(out[:first], None, [x[:first] for x in ref], "bf16", L)
+    cache.close()
+
+
 # n_new, kv_len, H, kv, d, dtype, the keys that get an infinite element
 SCORES = {
     "whole items": ([300], [300], 4, 2, 128, "bf16", [0, 1, 2, 16, 17, 33, 63, 64, 65, 80, 250, 299]),
