@@ -59,6 +59,7 @@ struct AttnParams {
     int32_t uniform;                             // rows per request where q_off is NULL
     const int32_t *q_off, *kv_len, *block_table;
     int64_t table_stride;
+    const void* v; int64_t vp, vt, vh;           // the value pool and its strides, for values that are infinite or NaN
     void* out; int64_t ot, oh;
     float* lse;
     float scale_log2, inv_group;
@@ -288,6 +289,7 @@ enum {
     kSegRows0, kSegRows1,                        // valid rows of its row tiles
     kSegReq,
     kSegFirst, kSegParts,                        // blocks that share the item: the first one, how many
+    kSegOdd,                                     // set by the softmax warps: infinite or NaN values were taken out of the stretch
     kSegLeft, kSegWords = 16                     // (units of the range before the stretch; the walking warp's own)
 };
 constexpr int kSegQueue = 4;
@@ -466,6 +468,32 @@ __device__ __forceinline__ void attn_merge(const AttnParams& p, const int* sg, i
     }
 }
 
+// Bits of the 16-bit elements of `w` that are infinite or NaN: all exponent bits set, to which one more at their low end carries
+// into the sign's place.
+template <typename E>
+__device__ __forceinline__ uint32_t odd_elements(uint32_t w)
+{
+    const uint32_t mask = is_bf16<E>::value ? 0x7f807f80u : 0x7c007c00u, one = is_bf16<E>::value ? 0x00800080u : 0x04000400u;
+    const uint32_t top = ((w & mask) + one) & 0x80008000u;
+    return (top >> 15) * 0xffffu;
+}
+// The infinite and NaN elements of 32 columns of one row of V, as they lie in the pool, added to a row's output
+template <typename E>
+__device__ __forceinline__ void add_odd_elements(const E* v, float (&x)[32])
+{
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(v) + i), odd = w & odd_elements<E>(w);
+        if (is_bf16<E>::value) {
+            x[2 * i] += __uint_as_float(odd << 16);
+            x[2 * i + 1] += __uint_as_float(odd & 0xffff0000u);
+        } else {
+            x[2 * i] += __half2float(__ushort_as_half(static_cast<unsigned short>(odd & 0xffffu)));
+            x[2 * i + 1] += __half2float(__ushort_as_half(static_cast<unsigned short>(odd >> 16)));
+        }
+    }
+}
+
 // Position in the ring of key and value tiles: tile g uses entries 2 g (keys) and 2 g + 1 (values).
 // The ring of key and value tiles, in turn.  A barrier's phase is one bit, so whoever waits for a fill (or a release) of a stage must know
 // that the one before it is past.  Here that hangs on S of a job being issued only after O of the slot's last job but one (s_free): the
@@ -617,7 +645,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const bool some = walk.next(p, s);
                 const int qi = item & (kSegQueue - 1);
                 if (some) {
-                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1;
+                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1; s[kSegOdd] = 0;
                     if (s[kSegT0] > 0 || s[kSegT1] < s[kSegTiles]) {                 // shared: whose ranges does the item reach?
                         auto block_of = [&](unsigned u) {
                             return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share;
@@ -774,6 +802,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             // columns of the job's keys past `cut` are masked for this row, rows of V from `have` on do not exist
             int cut = sg[kSegLimit] + attn_token(p, row) + (paired && slot ? p.tpt : 0) - key0;
             int have = sg[kSegKeys] - key0;
+            int common = sg[kSegLimit] - key0;       // last column that every row of the item sees
             float m = -CUDART_INF_F, l = 0.0f;
             for (int n = 0; n < J; n += 2) {
                 const uint32_t h = used & 1u;
@@ -826,22 +855,6 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     }
                     base_m = !valid ? -CUDART_INF_F : m == -CUDART_INF_F ? 0.0f : -m;
                 }
-                if (have < kAttnSub) {
-                    // Value rows behind the last key: their probabilities are 0, but 0 times what happens to lie there could be
-                    // NaN.  (Both slots of a paired item clear them: zeros over zeros.)  Row r of a tile lies in group r / 8
-                    // at 128 (r % 8), once per 64 columns.  The stage cannot be recycled before this job's second product.
-                    const int tile = tiles + (paired ? n >> 2 : n >> 1), sub = paired ? (n >> 1) & 1 : slot;
-                    const int e = 2 * tile + 1, st = e % kStages;
-                    ok = attn_wait_warp(full_bar(st), static_cast<uint32_t>(e / kStages) & 1u, flag);
-                    if (!ok) break;
-                    const int r0 = sub * kAttnSub + max(have, 0), r1 = sub * kAttnSub + kAttnSub;
-                    for (int i = row; i < (r1 - r0) * kHalves * 8; i += 128) {
-                        const int r = r0 + i / (kHalves * 8), c = i % (kHalves * 8);
-                        const uint32_t at = ring + st * kStage + (r >> 3) * kGroup + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16;
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at), "r"(0) : "memory");
-                    }
-                    fence_proxy_async();
-                }
                 if (warp_has_rows) {
                     // A masked score's exponential is 0 both ways, so that a finite value behind it adds nothing, however large.
                     const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), base2 = pair(base_m, base_m);
@@ -862,11 +875,44 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     l += low(both) + high(both);
                     tmem_wait_st();
                 }
+                if (common < kAttnSub - 1) {
+                    // Values that some row of the item does not see have weight 0 there, but 0 times an infinite value or NaN is NaN.
+                    // So rows of V behind the last key are cleared, and infinite and NaN elements of rows between taken out and
+                    // remembered; they are added at the end to the rows that see them.  Both slots of a paired item do this on
+                    // the same condition, whatever they see themselves: whoever comes second finds zeros.  Row r of a tile lies
+                    // in group r / 8 at 128 (r % 8), once per 64 columns.  The stage cannot be recycled before this job's
+                    // second product.
+                    const int tile = tiles + (paired ? n >> 2 : n >> 1), sub = paired ? (n >> 1) & 1 : slot;
+                    const int e = 2 * tile + 1, st = e % kStages;
+                    ok = attn_wait_warp(full_bar(st), static_cast<uint32_t>(e / kStages) & 1u, flag);
+                    if (!ok) break;
+                    const int r0 = max(common + 1, 0), dead = max(have, 0);
+                    for (int i = row + r0 * (kHalves * 8); i < kAttnSub * (kHalves * 8); i += 128) {
+                        const int r = i / (kHalves * 8), c = i % (kHalves * 8), at_row = sub * kAttnSub + r;
+                        const uint32_t at = ring + st * kStage + (at_row >> 3) * kGroup + (c >> 3) * 1024 + (at_row & 7) * 128 + (c & 7) * 16;
+                        uint32_t v[4] = {0, 0, 0, 0}, odd = 1;
+                        if (r < dead) {
+                            odd = 0;
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const uint32_t bad = odd_elements<E>(v[k]);
+                                odd |= bad;
+                                v[k] &= ~bad;
+                            }
+                            if (odd) *const_cast<volatile int*>(sg + kSegOdd) = 1;
+                        }
+                        if (odd)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+                    }
+                    fence_proxy_async();
+                }
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(2 * h + slot));
                 cut -= step;
                 have -= step;
+                common -= step;
                 ++used;
             }
             if (!ok) break;
@@ -900,6 +946,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 const int head = sg[kSegHead] * p.group + row - t * p.group;
                 const float inv = l == 0.0f ? 0.0f : attn_rcp(l);
                 if (whole) { wa *= inv; wb *= inv; }
+                const bool odd = valid && *const_cast<const volatile int*>(sg + kSegOdd) != 0;
                 const uint32_t aO_other = tO + (slot ^ 1) * 128 + lane_off;
                 for (int c = c0; c < c1; c += 32) {
                     uint32_t o[32];
@@ -913,6 +960,16 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) x[i] = fmaf(__uint_as_float(o[i]), wb, x[i]);
+                    }
+                    if (odd) {
+                        const int lo = max(max(sg[kSegLimit] + 1, 0), sg[kSegT0] * kAttnTile);
+                        const int hi = min(sg[kSegLimit] + tok - sg[kSegRow], sg[kSegT1] * kAttnTile - 1);       // the row's last key here
+                        for (int key = lo; key <= hi; ++key) {
+                            const int pg = __ldg(p.block_table + sg[kSegReq] * p.table_stride + (key >> p.page_shift));
+                            if (pg >= 0 && pg < p.n_pages)
+                                add_odd_elements<E>(static_cast<const E*>(p.v) + pg * p.vp + (key & ((1 << p.page_shift) - 1)) * p.vt +
+                                                        sg[kSegHead] * p.vh + c, x);
+                        }
                     }
                     if (valid && whole) {
                         E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + c;

@@ -380,6 +380,7 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
     p.uniform = a->max_new; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
     p.table_stride = a->table_stride;
+    p.v = a->v_pages; p.vp = s[7]; p.vt = s[8]; p.vh = s[9];
     p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;
     p.scale_log2 = (a->scale > 0.0f ? a->scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
     p.inv_group = 1.0f / (float)group;

@@ -1,7 +1,8 @@
 """Attention over the paged cache where masks and special values meet: what a row does not see does not reach it.
 
 Row i of a request sees keys 0 .. kv_len - n + i.  A weight is exp(score - max): a score of -inf gives 0, and one of +inf or NaN makes the
-row NaN, as it does in the softmax.  Finite entries are held to the tolerance derived in test_gpu_paged.py.
+row NaN, as it does in the softmax.  An infinite or NaN value reaches the rows that see its key, in its own column.  Finite entries are
+held to the tolerance derived in test_gpu_paged.py.
 """
 import pytest
 import torch
@@ -16,6 +17,58 @@ def place(cache, pool, b, key, head, column, value):
     """Writes one element of a request's key or value."""
     page = pool.shape[1]
     pool[int(cache.block_table[b, key // page]), key % page, head, column] = value
+
+
+def check_special(out, special, ref, dtype, keys):
+    """Entries where `special` (float64, 0 elsewhere) is infinite or NaN equal it, the others are within tolerance."""
+    odd = ~torch.isfinite(special)
+    o = out.double()
+    assert torch.equal(torch.isnan(o), torch.isnan(special))
+    inf = torch.isinf(special)
+    assert torch.equal(torch.isinf(o), inf) and torch.equal(o[inf], special[inf])
+    want, mag, _ = ref
+    check(torch.where(odd, torch.zeros_like(out), out), None, (torch.where(odd, 0.0, want), mag, None), dtype, keys)
+
+
+# n_new, kv_len, H, kv, d, page, dtype, and (request, key, key head, column, value) of the odd values
+VALUES = {
+    # one window of 9 rows, shared by several blocks; the third, fourth and last new token
+    "window": ([9], [709], 32, 8, 128, 16, "bf16", [(0, 702, 1, 5, NAN), (0, 703, 1, 6, INF), (0, 703, 0, 0, -INF), (0, 708, 7, 127, NAN)]),
+    # the boundary of two 64-key jobs and of two key tiles lies between the new tokens
+    "edges": ([20, 20], [138, 74], 8, 2, 64, 16, "fp16", [(0, 127, 0, 1, NAN), (0, 128, 1, 2, INF), (1, 63, 0, 3, -INF), (1, 64, 1, 4, NAN)]),
+    # a prompt chunk: pairs of row tiles share a key tile, the odd value is masked for one of them or for both
+    "chunk": ([300], [1000], 8, 2, 128, 64, "bf16", [(0, 700, 0, 0, NAN), (0, 731, 0, 1, INF), (0, 732, 1, 2, -INF), (0, 763, 1, 3, NAN),
+                                                   (0, 764, 0, 4, NAN), (0, 765, 0, 5, INF), (0, 899, 1, 6, NAN), (0, 999, 1, 7, NAN)]),
+    # infinities of both signs in one column: the rows that see one, then both (NaN)
+    "signs": ([40], [40], 4, 4, 64, 16, "bf16", [(0, 10, 2, 9, INF), (0, 20, 2, 9, -INF), (0, 12, 3, 9, -INF), (0, 22, 3, 9, -INF), (0, 0, 1, 63, INF)]),
+    # a cached value, which every row sees, beside new ones
+    "cached": ([5, 70], [400, 1500], 28, 4, 128, 32, "fp16", [(0, 17, 0, 7, INF), (1, 1429, 2, 8, NAN), (1, 1430, 3, 8, NAN), (1, 1470, 3, 9, -INF)]),
+    # more rows than keys: rows without a key stay zero
+    "fewer": ([6, 300], [3, 120], 8, 2, 128, 16, "bf16", [(0, 0, 0, 3, NAN), (0, 2, 1, 4, INF), (1, 0, 0, 5, NAN), (1, 64, 1, 6, -INF), (1, 119, 1, 7, NAN)]),
+    # 64 query heads to a key head: two tokens to a row tile
+    "group": ([7], [260], 64, 1, 64, 256, "bf16", [(0, 254, 0, 11, NAN), (0, 255, 0, 12, INF), (0, 256, 0, 13, -INF), (0, 259, 0, 14, NAN)]),
+}
+
+
+@pytest.mark.parametrize("name", VALUES)
+@pytest.mark.parametrize("heads_first", [False, True])
+def test_odd_values_reach_the_rows_that_see_them_and_no_others(name, heads_first):
+    n_new, kv_len, H, kv, d, page, dtype, odd = VALUES[name]
+    cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=H, kv=kv, d=d, page=page, dtype=dtype, heads_first=heads_first, seed=11)
+    special = torch.zeros(q.shape[0], H, d, dtype=torch.float64, device=DEV)
+    for b, key, head, column, _ in odd:                            # the finite part: the odd entries as zeros
+        place(cache, vp, b, key, head, column, 0.0)
+    ref = reference(q, kp.nan_to_num(0.0), vp.nan_to_num(0.0), cache.block_table, kv_len, q_off, d ** -0.5)
+    for b, key, head, column, value in odd:
+        place(cache, vp, b, key, head, column, value)
+        first = max(0, key - (kv_len[b] - n_new[b]))               # the first row of the request that sees the key
+        g = H // kv
+        special[q_off[b] + first:q_off[b + 1], head * g:(head + 1) * g, column] += value
+    for hint in (max(n_new), 1, 4 * max(n_new) + 3):
+        out = cache.attend(q, kp, vp, dev(kv_len), B=len(n_new), max_new=hint, q_off=dev(q_off))
+        check_special(out, special, ref, dtype, max(kv_len))
+    assert cache.device_error() == 0
+    cache.close()
 
 
 @pytest.mark.parametrize("n, L", [(40, 300), (9, 709), (300, 300)])
