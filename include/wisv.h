@@ -520,9 +520,11 @@ int wisv_cache_append(wisv_cache* cache, const wisv_append* a, void* cuda_stream
  * Attention of each request's new tokens over its cache.  Row i of request b (n_b = q_off[b+1] - q_off[b] rows, i from 0) sees
  * keys 0 .. kv_len[b] - n_b + i of the request: all that was cached before, and the new tokens up to itself (which
  * wisv_cache_append has written).  out = softmax(scale * q k^T) v per head; query head h reads key head h / (n_heads /
- * n_kv_heads).  A row that sees no key, or whose scores are all -inf, gives zero, and -inf in lse; a score of +inf (an overflow) or
- * NaN makes the row and its lse NaN.  An infinite or NaN value reaches the rows that see its key, in its own column, and no other.  Scores, maxima, sums and products are accumulated in fp32; the
- * probabilities are rounded to the cache's 16-bit type for the second product.
+ * n_kv_heads).  A row that sees no key, or whose scores are all -inf, gives zero, and -inf in lse; a score of +inf (an overflow)
+ * or NaN makes the row and its lse NaN.  An infinite or NaN value reaches the rows that see its key, in its own column, and no
+ * other.  Scores, maxima, sums and products are accumulated in fp32; the probabilities are rounded to the cache's 16-bit type
+ * for the second product.
+ * Rows of q that no window covers (before q_off[0], or from q_off[B] on) give zero and -inf likewise.
  * Keys and values past kv_len[b] (and whole pages that the table does not reach) may hold anything, NaN included; table entries
  * outside the pool read as zeros.
  */

@@ -551,6 +551,22 @@ __device__ __forceinline__ bool attn_load_tiles(const AttnParams& p, const CUten
     return true;
 }
 
+// Zeros (-inf in lse) for the rows of q that no window covers, those before the first offset and behind the last one: a batch padded
+// to a fixed number of rows carries them on into the next layer.  `w` of `all` warps.
+template <typename E, int D>
+__device__ __forceinline__ void attn_clear_rows(const AttnParams& p, int w, int all, int lane)
+{
+    if (!p.q_off) return;
+    const int head = min(max(__ldg(p.q_off), 0), p.T), tail = min(max(__ldg(p.q_off + p.B), head), p.T);
+    const int heads = p.n_kv * p.group;
+    for (int i = w; i < head + p.T - tail; i += all) {
+        const int64_t t = i < head ? i : tail + (i - head);
+        for (int x = lane; x < heads * (D / 8); x += 32)
+            *reinterpret_cast<uint4*>(static_cast<E*>(p.out) + t * p.ot + x / (D / 8) * p.oh + x % (D / 8) * 8) = make_uint4(0, 0, 0, 0);
+        for (int h = lane; p.lse && h < heads; h += 32) p.lse[t * heads + h] = -CUDART_INF_F;
+    }
+}
+
 template <typename E, int D>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
@@ -628,12 +644,14 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     const uint32_t tS = tmem, tO = tmem + 256;   // S of slot s at 128 s, P over its first half, O at 256 + 128 s
     int issued = 0, q_issued = 0;                // ring entries and query buffers filled (copying warps; read again before the end)
 
-    // Warps 0 and 4 idle: they share a scheduler with the softmax warps of rows 0 .. 31, the only ones at work where a row tile has
-    // few rows.  Warps 1, 2, 3, 5, 6, 7 are roles 0 .. 5.
+    // Warps 0 and 4 have next to nothing to do: they share a scheduler with the softmax warps of rows 0 .. 31, the only ones at
+    // work where a row tile has few rows.  Warps 1, 2, 3, 5, 6, 7 are roles 0 .. 5.
     const int role = warp > 7 || (warp & 3) == 0 ? -1 : warp < 4 ? warp - 1 : warp - 2;
     if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (role == 0) {
+        if (role < 0) {
+            attn_clear_rows<E, D>(p, static_cast<int>(me) * 2 + (warp >> 2), static_cast<int>(gridDim.x) * 2, lane);
+        } else if (role == 0) {
             // ------------------------------------------------------------ the work, and the TMA copies of queries and keys
             AttnWalk walk;
             unsigned share, more;

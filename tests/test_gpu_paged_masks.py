@@ -133,3 +133,28 @@ def test_infinite_scores(name):
               (torch.where(bad[:, :, None], zero, want), mag, torch.where(bad, zero, want_lse)), dtype, max(kv_len))
         assert cache.device_error() == 0
         cache.close()
+
+
+@pytest.mark.parametrize("H, kv, d, dtype", [(8, 2, 128, "bf16"), (14, 2, 64, "fp16")])
+def test_rows_outside_all_windows_are_zero(H, kv, d, dtype):
+    """A batch padded to a fixed number of rows: those before the first window and behind the last."""
+    n_new, kv_len = [4, 70], [100, 900]
+    cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=H, kv=kv, d=d, page=16, dtype=dtype, seed=2)
+    ref = reference(q, kp.nan_to_num(0.0), vp.nan_to_num(0.0), cache.block_table, kv_len, q_off, d ** -0.5)
+    for before, behind in ((0, 1), (3, 0), (2, 400)):
+        T = before + q.shape[0] + behind
+        wide = torch.full((T, H, d), NAN, dtype=q.dtype, device=DEV)
+        wide[before:before + q.shape[0]] = q
+        big = torch.full((T + 1, H + 1, d + 8), NAN, dtype=q.dtype, device=DEV)
+        lse = torch.full((T, H), NAN, dtype=torch.float32, device=DEV)
+        out = cache.attend(wide, kp, vp, dev(kv_len), B=2, max_new=70, q_off=dev(q_off) + before, out=big[:T, :H, :d], lse=lse)
+        inside = torch.zeros(T, dtype=torch.bool, device=DEV)
+        inside[before:before + q.shape[0]] = True
+        assert (out[~inside] == 0).all() and (lse[~inside] == -INF).all()
+        check(out[inside], lse[inside], ref, dtype, 900)
+        big[:T, :H, :d] = NAN
+        assert torch.isnan(big).all()                              # nothing beside the output was written
+    # no window has a row
+    out = cache.attend(q, kp, vp, dev(kv_len), B=2, max_new=1, q_off=dev([0, 0, 0]), out=torch.full_like(q, NAN))
+    assert (out == 0).all() and cache.device_error() == 0
+    cache.close()
