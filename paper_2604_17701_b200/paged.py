@@ -119,13 +119,25 @@ class WindowLayout:
     status: "object"
 
 
+def _owned_array(i):
+    """A cache's i-th bookkeeping array as an attribute that can be written in place (``+=`` included) but not replaced."""
+    def get(self):
+        return self._owned[i]
+
+    def put(self, value):
+        if value is not self._owned[i]:
+            raise AttributeError("the library holds this array's address: write into it (copy_) instead of replacing it")
+    return property(get, put)
+
+
 class PagedCache:
     """wisv_cache_* on torch CUDA tensors: the paged key/value cache of a target model.
 
     The bookkeeping tensors (``free_list``, ``n_free``, ``block_table``, ``n_blocks``, ``seq_len``) are ordinary int32
-    tensors of this object, with every page free at the start; the page pools of each layer are the caller's:
-    ``k_pages`` / ``v_pages`` of shape [n_pages, page_size, n_kv_heads, head_dim] with any strides that keep a
-    head's elements contiguous (a [n_pages, n_kv_heads, page_size, head_dim] pool is passed as ``.transpose(1, 2)``).
+    tensors of this object, with every page free at the start, to be written in place, not replaced.  The page pools of each
+    layer are the caller's: ``k_pages`` / ``v_pages`` of shape [n_pages, page_size, n_kv_heads, head_dim] with any strides
+    that keep a head's elements contiguous (a [n_pages, n_kv_heads, page_size, head_dim] pool is passed as
+    ``.transpose(1, 2)``).
     Request b of a call is row b of ``block_table``.  Calls are asynchronous on the current (or given) torch
     stream and must be ordered on it; they share the object's workspace.
     """
@@ -153,20 +165,18 @@ class PagedCache:
         self.page_size, self.n_pages, self.max_requests, self.max_blocks = page_size, n_pages, max_requests, max_blocks
         self.dtype = torch.bfloat16 if dtype == DT_BF16 else torch.float16
         i32 = dict(dtype=torch.int32, device=self.device)
-        self.free_list = torch.arange(n_pages - 1, -1, -1, **i32)
-        self.n_free = torch.full((1,), n_pages, **i32)
-        self.block_table = torch.full((max_requests, max_blocks), -1, **i32)
-        self.n_blocks = torch.zeros(max_requests, **i32)
-        self.seq_len = torch.zeros(max_requests, **i32)
-        self._pages = _Pages(*(t.data_ptr() for t in (self.free_list, self.n_free, self.block_table, self.n_blocks,
-                                                      self.seq_len)))
-        # the arrays whose addresses the block above holds
-        self._owned = (self.free_list, self.n_free, self.block_table, self.n_blocks, self.seq_len)
+        # every call works on these arrays: the block holds their addresses, and the attributes cannot be set
+        self._owned = (torch.arange(n_pages - 1, -1, -1, **i32), torch.full((1,), n_pages, **i32),
+                       torch.full((max_requests, max_blocks), -1, **i32), torch.zeros(max_requests, **i32),
+                       torch.zeros(max_requests, **i32))
+        self._pages = _Pages(*(t.data_ptr() for t in self._owned))
         self._pages_at = C.addressof(self._pages)
         self._index = self.device.index
         self._row = (n_kv_heads, head_dim)
         self._pool = (n_pages, page_size, n_kv_heads, head_dim)
         self._raw_stream, self._current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+    free_list, n_free, block_table, n_blocks, seq_len = (_owned_array(i) for i in range(5))
 
     def close(self):
         if getattr(self, "_h", None):
@@ -284,7 +294,7 @@ class PagedCache:
             raise ValueError("lse must be a contiguous float32 [T, n_heads] tensor")
         if scale is not None and not scale > 0:
             raise ValueError("scale must be positive")
-        table, blocks, step = self.block_table, self.max_blocks, self.max_blocks
+        table, blocks, step = self._owned[2], self.max_blocks, self.max_blocks
         if block_table is not None:
             table = block_table
             if table.dtype is not i32 or table.dim() != 2 or table.shape[0] < B or table.stride(1) != 1 or table.get_device() != dev:

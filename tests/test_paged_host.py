@@ -94,3 +94,14 @@ def test_verify_residual_refuses(lib, change, code):
 def test_binding_needs_a_cuda_device():
     with pytest.raises(ValueError):
         wisv.PagedCache(**{**GOOD, "device": "cpu"})
+
+
+@pytest.mark.parametrize("i, name", enumerate(n for n, _ in paged._Pages._fields_))
+def test_bookkeeping_arrays_cannot_be_replaced(i, name):
+    """The library holds their addresses: another tensor in the attribute would give the calls different tables."""
+    cache = object.__new__(wisv.PagedCache)
+    cache._owned = tuple(range(5))
+    assert getattr(cache, name) == i                               # the order of the block of addresses
+    setattr(cache, name, cache._owned[i])                          # as `+=` does after its work in place
+    with pytest.raises(AttributeError):
+        setattr(cache, name, None)
