@@ -548,6 +548,13 @@ typedef struct {
 } wisv_attend;
 int wisv_cache_attend(wisv_cache* cache, const wisv_attend* a, void* cuda_stream);
 
+/*
+ * Test hook for the failure path: in the calls of wisv_cache_attend that follow, waits give up after limit_cycles SM clocks (0: the
+ * usual 4e9), and the thread block `block` (-1: none) never copies values, so that waits of that block run out.  They set
+ * bit 0 of the error word that wisv_cache_error reports; rows that the block had a part in are not written.
+ */
+int wisv_debug_cache_waits(wisv_cache* cache, uint64_t limit_cycles, int32_t block);
+
 /* ------------------------------------------------------------------------------------------------------------------
  * Verification against the target's probabilities with a draw from the residual (Eqs. 1 and 2).
  *

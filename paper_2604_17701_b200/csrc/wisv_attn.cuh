@@ -50,7 +50,7 @@ constexpr int kAttnItemCost = 1;                 // key tiles that starting and 
 constexpr int kAttnSmem = 232448;                // all of an SM's shared memory that a block can have
 constexpr int kAttnSmall = 2816;                 // barriers, the queue of stretches, the slots' exchange of m and l
 constexpr int kAttnSlack = 256;                  // for aligning the tiles to 1024 bytes
-constexpr uint64_t kAttnWaitClocks = 4000000000ull;
+constexpr uint64_t kAttnWaitClocks = 4000000000ull;       // the limit of every wait, unless a test has set a shorter one
 
 struct AttnParams {
     int32_t B, T, max_new, n_kv, group, tpt, page_shift, n_pages, max_blocks;
@@ -64,6 +64,8 @@ struct AttnParams {
     float* lse;
     float scale_log2, inv_group;
     int32_t* err;
+    uint32_t wait_limit;                         // in 1024 clocks
+    int32_t stalled;                             // test hook: a block whose values are never copied; -1: none
     float* part_o;                               // [2 * blocks][D / 4][256 rows][4]: rows side by side, as the lanes that write and read them
     float2* part_ml;                             // [2 * blocks][256]
     int32_t* count;                              // [blocks]: arrivals at the item that starts in a block's range and ends in another's; 0 between calls
@@ -108,7 +110,7 @@ __device__ __forceinline__ float attn_ex2(float x)
     return y;
 }
 
-// Bounded wait; `flag` is the shared-memory address of the block's abort flag.  One inline try and everything else out of
+// Bounded wait; `flag` is the shared-memory address of the block's abort flag, three words before the limit.  One inline try and everything else out of
 // line: a try that is the condition of an inline loop costs some 370 clocks even where the barrier is complete.
 static __device__ __forceinline__ bool attn_wait_slow(uint32_t bar, uint32_t parity, uint32_t flag)
 {
@@ -116,10 +118,11 @@ static __device__ __forceinline__ bool attn_wait_slow(uint32_t bar, uint32_t par
     uint32_t n = 0;
     while (!mbar_try_wait(bar, parity)) {
         if ((++n & 0xFFu) == 0) {
-            uint32_t stop;
+            uint32_t stop, limit;
             asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(stop) : "r"(flag) : "memory");
             if (stop != 0) return false;
-            if (static_cast<uint64_t>(clock64() - t0) > kAttnWaitClocks) {
+            asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(limit) : "r"(flag + 12u) : "memory");
+            if (static_cast<uint64_t>(clock64() - t0) >> 10 > limit) {
                 asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(flag), "r"(1) : "memory");
                 return false;
             }
@@ -602,6 +605,8 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);       // [0] abort, [1] drain scratch
     const uint32_t flag = bars + 8u * (kBars + 9) + 4u;
     volatile int* came_last = reinterpret_cast<volatile int*>(tmem_slot + 3);        // whether this block was the last at a shared item
+    volatile uint32_t* wait_limit = tmem_slot + 4;                                   // [2]: three words behind either flag
+    volatile int* copies = reinterpret_cast<volatile int*>(tmem_slot + 6);           // key and value tiles copied, written at the end
     const unsigned me = blockIdx.x;
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
@@ -621,6 +626,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         for (int s = 0; s < kSegQueue; ++s) { mbar_init(seg_full(s), 1); mbar_init(seg_empty(s), 11); }
         mbar_init(o_full, 2); mbar_init(o_empty, 8); mbar_init(ml_full, 8); mbar_init(part_full, 8); mbar_init(last_full, 1); for (int s = 0; s < kAttnMmaWarps; ++s) mbar_init(drain + 8 * s, 1);
         abort_flag[0] = 0; abort_flag[1] = 0;
+        wait_limit[0] = wait_limit[1] = p.wait_limit;
         fence_barrier_init();
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmK);
@@ -702,7 +708,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
             // copies a tile, some 80 clocks each: one warp for both would be late)
             AttnRing rg;
             rg.step(kStages);
-            bool ok = true;
+            bool ok = static_cast<int>(me) != p.stalled;
             for (int item = 0; ok; ++item) {
                 const int qi = item & (kSegQueue - 1);
                 ok = attn_wait_warp(seg_full(qi), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
@@ -787,12 +793,6 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     if (last_use) { rg.step(kStages); rg.step(kStages); }
                 }
                 if (ok && second && lane == 0) mbar_arrive(seg_empty(qi));
-            }
-            if (!ok) {
-                const uint32_t mine = drain + 8 * (role - 1);
-                if (elect_one()) umma_commit(mine);
-                __syncwarp();
-                attn_wait(mine, 0, flag + 4);
             }
         }
     } else {
@@ -1041,16 +1041,28 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         }
     }
 
+    if (lane == 0 && role == 0) copies[0] = issued;
+    if (lane == 0 && role == 1 + kAttnMmaWarps) copies[1] = issued;
     __syncthreads();
-    if ((role == 0 || role == 1 + kAttnMmaWarps) && lane == 0 && abort_flag[0] != 0) {
-        // after a time-out: the copies still in flight have to land before this block's shared memory is given up
-        const int kind = role == 0 ? 0 : 1;
-        for (int i = issued > kStages ? issued - kStages : 0; i < issued; ++i) {
-            const int e = 2 * i + kind;
-            attn_wait(full_bar(e % kStages), static_cast<uint32_t>(e / kStages) & 1u, flag + 4);
+    if (abort_flag[0] != 0) {
+        // After a time-out: products and copies still in flight have to end before this block's TMEM and shared memory are given up,
+        // whoever issued them and however its own loop ended.
+        if (role > 0 && role <= kAttnMmaWarps) {
+            const uint32_t mine = drain + 8 * (role - 1);
+            if (elect_one()) umma_commit(mine);
+            __syncwarp();
+            attn_wait(mine, 0, flag + 4);
+        } else if (role == 0 && lane == 0) {
+            // the last fill of each stage: earlier ones were complete before the stage was filled again
+            const int n[2] = {copies[0], copies[1]}, end = 2 * max(n[0], n[1]);
+            for (int e = max(end - 4 * kStages, 0); e < end; ++e) {
+                const int again = e + kStages;
+                if ((e >> 1) < ((e & 1) ? n[1] : n[0]) && (again >> 1) >= ((again & 1) ? n[1] : n[0]))
+                    attn_wait(full_bar(e % kStages), static_cast<uint32_t>(e / kStages) & 1u, flag + 4);
+            }
+            for (int i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i)
+                attn_wait(q_full(i & 1), static_cast<uint32_t>((i >> 1) & 1), flag + 4);
         }
-        for (int i = q_issued > 2 ? q_issued - 2 : 0; i < q_issued; ++i)
-            attn_wait(q_full(i & 1), static_cast<uint32_t>((i >> 1) & 1), flag + 4);
     }
     tc_fence_before();
     __syncthreads();

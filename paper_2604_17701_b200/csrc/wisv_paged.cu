@@ -30,6 +30,8 @@ struct wisv_cache {
     float2* part_ml = nullptr;
     float* part_o = nullptr;
     EncodeTiledFn encode = nullptr;
+    uint64_t wait_clocks = kAttnWaitClocks;       // wisv_debug_cache_waits
+    int32_t stalled = -1;
 };
 
 namespace {
@@ -264,6 +266,14 @@ int wisv_cache_error(wisv_cache* c, void* cuda_stream, int32_t* flags)
     return WISV_OK;
 }
 
+int wisv_debug_cache_waits(wisv_cache* c, uint64_t limit_cycles, int32_t block)
+{
+    if (!c || limit_cycles > kAttnWaitClocks || block < -1) return WISV_EINVAL;
+    c->wait_clocks = limit_cycles ? limit_cycles : kAttnWaitClocks;
+    c->stalled = block;
+    return WISV_OK;
+}
+
 int wisv_cache_extend(wisv_cache* c, const wisv_pages* pages, int32_t B, int32_t T_total, const int32_t* n_new,
                       int32_t n_uniform, const wisv_layout* out, void* cuda_stream)
 {
@@ -384,6 +394,7 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;
     p.scale_log2 = (a->scale > 0.0f ? a->scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
     p.inv_group = 1.0f / (float)group;
+    p.wait_limit = (uint32_t)((c->wait_clocks + 1023) >> 10); p.stalled = c->stalled;
     p.err = c->err; p.part_o = c->part_o; p.part_ml = c->part_ml; p.count = c->count;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool bf = c->cfg.dtype == WISV_DT_BF16;

@@ -74,6 +74,7 @@ def _lib():
                            ("wisv_cache_error", [P, P, C.POINTER(I)]),
                            ("wisv_cache_extend", [P, P, I, I, P, I, P, P]), ("wisv_cache_commit", [P, P, I, P, P, P]),
                            ("wisv_cache_append", [P, P, P]), ("wisv_cache_attend", [P, P, P]),
+                           ("wisv_debug_cache_waits", [P, C.c_uint64, I]),
                            ("wisv_verify_residual", [P, P])):
             f = getattr(lib, name)
             f.restype, f.argtypes = C.c_int, args
@@ -312,6 +313,10 @@ class PagedCache:
         with self._torch.cuda.device(self.device):
             _check(self.lib.wisv_cache_error(self._h, self._raw_stream(self._index), C.byref(v)), "wisv_cache_error")
         return v.value
+
+    def debug_waits(self, limit_cycles: int = 0, block: int = -1):
+        """wisv_debug_cache_waits: a shorter limit for the waits of attend, and a block that never copies values."""
+        _check(self.lib.wisv_debug_cache_waits(self._h, limit_cycles, block), "wisv_debug_cache_waits")
 
     def launch_count(self) -> int:
         return int(self.lib.wisv_cache_launch_count(self._h))
