@@ -68,7 +68,10 @@ struct AttnParams {
     int32_t stalled;                             // test hook: a block whose values are never copied; -1: none
     float* part_o;                               // [2 * blocks][D / 4][256 rows][4]: rows side by side, as the lanes that write and read them
     float2* part_ml;                             // [2 * blocks][256]
-    int32_t* count;                              // [blocks]: arrivals at the item that starts in a block's range and ends in another's; 0 between calls
+    // [blocks]: arrivals at the item that starts in a block's range and ends in another's, in the half of the word that err[1] names.
+    // It is 0 when a call starts: the block that comes last clears it.  After a time-out the other half counts, and the next call
+    // clears what the failed one left.
+    int32_t* count;
 };
 
 template <typename E> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
@@ -282,7 +285,7 @@ __device__ __forceinline__ int attn_tiles(const AttnParams& p, const AttnReq& r,
     return last_key < 0 ? 1 : last_key / kAttnTile + 1;
 }
 
-// A stretch of one item's key tiles that this block works on, as the walking warp queues it for the others: 16 words
+// A stretch of one item's key tiles that this block works on, as the walking warp queues it for the others
 enum {
     kSegJobs,                                    // 0: the end
     kSegPaired, kSegT0, kSegT1, kSegTiles,       // key tiles [t0, t1) of the item's kSegTiles
@@ -293,7 +296,9 @@ enum {
     kSegReq,
     kSegFirst, kSegParts,                        // blocks that share the item: the first one, how many
     kSegOdd,                                     // set by the softmax warps: infinite or NaN values were taken out of the stretch
-    kSegLeft, kSegWords = 16                     // (units of the range before the stretch; the walking warp's own)
+    kSegShift,                                   // 16 times the half of the arrival counters that this call uses
+    kSegWords,
+    kSegLeft = kSegWords                         // (units of the range before the stretch; the walking warp's own)
 };
 constexpr int kSegQueue = 4;
 
@@ -301,7 +306,7 @@ struct AttnWalk {
     int b, kvh, it, pos, units;                  // position on the line of key tiles, and what is left of the range
     AttnReq r;
     // The next stretch; false at the end of the range.
-    __device__ __forceinline__ bool next(const AttnParams& p, int (&s)[kSegWords])
+    __device__ __forceinline__ bool next(const AttnParams& p, int (&s)[kSegWords + 1])
     {
         while (units > 0) {
             if (it >= r.items) {                 // (a request without rows)
@@ -607,10 +612,11 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     volatile int* came_last = reinterpret_cast<volatile int*>(tmem_slot + 3);        // whether this block was the last at a shared item
     volatile uint32_t* wait_limit = tmem_slot + 4;                                   // [2]: three words behind either flag
     volatile int* copies = reinterpret_cast<volatile int*>(tmem_slot + 6);           // key and value tiles copied, written at the end
+    volatile uint32_t* half_used = tmem_slot + 8;                                    // thread 0's: the half of the counters in use
     const unsigned me = blockIdx.x;
     int (*queue)[kSegWords] = reinterpret_cast<int (*)[kSegWords]>(small + kSegAt);  // [kSegQueue]
     float2* ml = reinterpret_cast<float2*>(small + kAttnSmall - 2048);               // [2][128]
-    static_assert(kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
+    static_assert(kSegWords == 16 && kSegAt + kSegQueue * kSegWords * 4 <= kAttnSmall - 2048, "shared memory");
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
     const int lane = threadIdx.x & 31;
@@ -656,20 +662,28 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
     if (warp < 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         if (role < 0) {
+            if (threadIdx.x == 0) {
+                const unsigned half = static_cast<unsigned>(__ldcg(p.err + 1)) & 1u;
+                *half_used = half;
+                const unsigned other = 0xffffu << (16u * (half ^ 1u));
+                if (static_cast<unsigned>(__ldcg(p.count + me)) & other) atomicAnd(p.count + me, static_cast<int>(~other));
+            }
+            __syncwarp();
             attn_clear_rows<E, D>(p, static_cast<int>(me) * 2 + (warp >> 2), static_cast<int>(gridDim.x) * 2, lane);
         } else if (role == 0) {
             // ------------------------------------------------------------ the work, and the TMA copies of queries and keys
+            const int half = __ldcg(p.err + 1) & 1;              // (on its way while the range is found: 0.5 us of a small call)
             AttnWalk walk;
             unsigned share, more;
             attn_range<D>(p, me, lane, walk, share, more);
-            int s[kSegWords];
+            int s[kSegWords + 1];
             AttnRing rg;
             bool ok = true;
             for (int item = 0; ok; ++item) {
                 const bool some = walk.next(p, s);
                 const int qi = item & (kSegQueue - 1);
                 if (some) {
-                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1; s[kSegOdd] = 0;
+                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1; s[kSegOdd] = 0; s[kSegShift] = 16 * half;
                     if (s[kSegT0] > 0 || s[kSegT1] < s[kSegTiles]) {                 // shared: whose ranges does the item reach?
                         auto block_of = [&](unsigned u) {
                             return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share;
@@ -683,7 +697,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                 if (!ok) break;
                 if (lane == 0) {
 #pragma unroll
-                    for (int i = 0; i < kSegLeft; ++i) queue[qi][i] = some ? s[i] : 0;
+                    for (int i = 0; i < kSegWords; ++i) queue[qi][i] = some ? s[i] : 0;
                     mbar_arrive(seg_full(qi));
                 }
                 __syncwarp();
@@ -1022,12 +1036,13 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                     ok = attn_wait_warp(part_full, splits & 1u, flag);
                     if (!ok) break;
                     if (lane == 0) {
+                        const int shift = sg[kSegShift];
                         __threadfence();
-                        const int before = atomicAdd(p.count + first_block, 1);
+                        const int before = static_cast<int>(static_cast<unsigned>(atomicAdd(p.count + first_block, 1 << shift)) >> shift & 0xffffu);
                         *came_last = before == parts - 1;
-                        if (before == parts - 1) p.count[first_block] = 0;
                         __threadfence();
                         mbar_arrive(last_full);
+                        if (before == parts - 1) p.count[first_block] = 0;               // (nobody counts in the other half)
                     }
                     __syncwarp();
                 }
@@ -1070,7 +1085,10 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    if (threadIdx.x == 0 && abort_flag[0] != 0) atomicOr(p.err, 1);
+    if (threadIdx.x == 0 && abort_flag[0] != 0) {
+        atomicOr(p.err, 1);
+        atomicExch(p.err + 1, static_cast<int>(*half_used ^ 1u));                    // (every block that gave up writes the same)
+    }
 }
 
 }  // namespace wisv

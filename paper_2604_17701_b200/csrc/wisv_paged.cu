@@ -23,7 +23,7 @@ struct wisv_cache {
     int sm_count = 0;
     int page_shift = 0;
     int64_t launches = 0;
-    // one allocation: [error word | arrival counters | partial maxima and sums | partial outputs]
+    // one allocation: [error word, half of the counters in use | arrival counters | partial maxima and sums | partial outputs]
     void* work = nullptr;         // NULL: the caller's
     int32_t* err = nullptr;
     int32_t* count = nullptr;
@@ -260,7 +260,6 @@ int wisv_cache_error(wisv_cache* c, void* cuda_stream, int32_t* flags)
     if (!c || !flags) return WISV_EINVAL;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     WISV_TRY_CUDA(cudaMemcpyAsync(flags, c->err, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
-    // (a kernel that gave up may leave arrival counters behind)
     WISV_TRY_CUDA(cudaMemsetAsync(c->err, 0, 256 + (size_t)c->sm_count * 4, st));
     WISV_TRY_CUDA(cudaStreamSynchronize(st));
     return WISV_OK;

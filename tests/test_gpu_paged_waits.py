@@ -21,9 +21,9 @@ SHAPES = {
 def setup(name):
     n_new, kv_len, H, kv, d, page, dtype, block = SHAPES[name]
     cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=H, kv=kv, d=d, page=page, dtype=dtype, seed=4)
-    args = (q, kp, vp, dev(kv_len))
+    args = (kp, vp, dev(kv_len))
     kw = dict(B=len(n_new), max_new=max(n_new), q_off=dev(q_off))
-    return cache, lambda: cache.attend(*args, **kw), block
+    return cache, lambda x=1.0: cache.attend(q * x, *args, **kw), block
 
 
 @pytest.mark.parametrize("name", SHAPES)
@@ -52,4 +52,23 @@ def test_refusals():
         with pytest.raises(wisv.WisvError) as e:
             cache.debug_waits(limit, block)
         assert e.value.code == -1
+    cache.close()
+
+
+@pytest.mark.parametrize("name", SHAPES)
+def test_calls_after_a_time_out_are_right_before_it_is_read(name):
+    """Graph replays cannot read the error word: arrivals that a failed call left behind must not count in the next ones."""
+    cache, attend, block = setup(name)
+    inputs = [1.0, -2.0, 0.5, 3.0]                                 # other queries every time, so that stale partials show
+    want = [attend(x) for x in inputs]
+    assert cache.device_error() == 0
+    for fails in (1, 2, 1):                                        # twice in a row as well
+        cache.debug_waits(2_000_000, block)
+        for _ in range(fails):
+            attend(1.5)
+        cache.debug_waits()
+        for x, y in zip(inputs, want):
+            assert torch.equal(attend(x), y), (fails, x)
+    assert cache.device_error() == 1                               # still reported
+    assert torch.equal(attend(2.0), attend(2.0)) and cache.device_error() == 0
     cache.close()
