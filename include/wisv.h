@@ -427,7 +427,8 @@ int wisv_debug_poison_static(void* cuda_stream);
  *
  * Lengths stay on the device throughout: nothing here reads them back or synchronises, and every call can be captured
  * in a CUDA graph.  The page pools (one pair of K and V arrays per layer) and the bookkeeping arrays belong to the caller.
- * Calls on one wisv_cache must be stream-ordered: they share its workspace.
+ * Calls on one wisv_cache must be stream-ordered: they share its workspace.  They are made with the device current on which it was
+ * created (WISV_EINVAL otherwise).
  */
 #define WISV_MAX_REQUESTS 4096
 #define WISV_MAX_GROUP    64        /* query heads per key head */

@@ -133,12 +133,20 @@ Workspace layout_of(const wisv_cache_config* cfg, int sms)
     return w;
 }
 
+// A cache's workspace and launch shapes are those of the device that it was created on.
+int check_device(const wisv_cache* c)
+{
+    int dev = 0;
+    WISV_TRY_CUDA(cudaGetDevice(&dev));
+    return dev == c->device ? WISV_OK : WISV_EINVAL;
+}
+
 int check_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B)
 {
     if (!c || !pg || !pg->free_list || !pg->n_free || !pg->block_table || !pg->n_blocks || !pg->seq_len) return WISV_EINVAL;
     if (B < 1) return WISV_ESHAPE;
     if (B > c->cfg.max_requests) return WISV_ECAPACITY;
-    return WISV_OK;
+    return check_device(c);
 }
 
 void fill_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B, PagesParams* p)
@@ -258,6 +266,8 @@ int64_t wisv_cache_launch_count(const wisv_cache* c) { return c ? c->launches : 
 int wisv_cache_error(wisv_cache* c, void* cuda_stream, int32_t* flags)
 {
     if (!c || !flags) return WISV_EINVAL;
+    const int rc = check_device(c);
+    if (rc != WISV_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     WISV_TRY_CUDA(cudaMemcpyAsync(flags, c->err, sizeof(int32_t), cudaMemcpyDeviceToHost, st));
     WISV_TRY_CUDA(cudaMemsetAsync(c->err, 0, 256 + (size_t)c->sm_count * 4, st));
@@ -328,6 +338,8 @@ int wisv_cache_append(wisv_cache* c, const wisv_append* a, void* cuda_stream)
     const int64_t s[] = {a->k_token_stride, a->k_head_stride, a->v_token_stride, a->v_head_stride, a->kp_page_stride,
                          a->kp_token_stride, a->kp_head_stride, a->vp_page_stride, a->vp_token_stride, a->vp_head_stride};
     for (int64_t x : s) if (x % 8) return WISV_EALIGN;
+    const int rc = check_device(c);
+    if (rc != WISV_OK) return rc;
     AppendParams p;
     p.T = a->T;
     p.vecs = c->cfg.n_kv_heads * c->cfg.head_dim / 8;
@@ -365,11 +377,13 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
                          a->kp_token_stride, a->kp_head_stride, a->vp_page_stride, a->vp_token_stride, a->vp_head_stride};
     for (int64_t x : s) if (x % 8 || x < 0) return WISV_EALIGN;
     if (!a->kp_token_stride || !a->vp_token_stride || a->kp_page_stride % (8 * a->kp_token_stride) || a->vp_page_stride % (8 * a->vp_token_stride)) return WISV_EALIGN;
+    int r = check_device(c);
+    if (r != WISV_OK) return r;
     const int group = c->cfg.n_heads / c->cfg.n_kv_heads, D = c->cfg.head_dim;
     AttnParams p;
     memset(&p, 0, sizeof p);
     CUtensorMap tmQ, tmK, tmV;
-    int r = encode_pool(c, &tmK, a->k_pages, s[4], s[5], s[6], &p.page_groups_k, &p.groups_k);
+    r = encode_pool(c, &tmK, a->k_pages, s[4], s[5], s[6], &p.page_groups_k, &p.groups_k);
     if (r == WISV_OK) r = encode_pool(c, &tmV, a->v_pages, s[7], s[8], s[9], &p.page_groups_v, &p.groups_v);
     if (r != WISV_OK) return r;
     p.tpt = kAttnTile / group < a->max_new ? kAttnTile / group : a->max_new;

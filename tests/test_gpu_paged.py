@@ -540,3 +540,26 @@ def test_batches_that_fill_memory_bandwidth(rows, d, dtype):
         assert torch.equal(o, outs[0])
     assert cache.device_error() == 0
     cache.close()
+
+
+def test_another_current_device_is_refused():
+    """The calls check the current device against the one at create; as a second device need not be there, the number kept
+    behind the configuration is changed instead."""
+    import ctypes as C
+    from paper_2604_17701_b200 import paged
+    cache = make_cache()
+    q = torch.zeros(4, 8, 64, dtype=torch.bfloat16, device=DEV)
+    kp = torch.zeros(64, 16, 2, 64, dtype=torch.bfloat16, device=DEV)
+    k, n, slots = q[:, :2], dev([4]), dev([0, 1, 2, 3], torch.int64)
+    calls = [lambda: cache.extend(B=1, n_new=1), lambda: cache.commit(dev([0]), B=1), lambda: cache.append(k, k, kp, kp, slots),
+             lambda: cache.attend(q, kp, kp, n, B=1, max_new=4), lambda: cache.device_error()]
+    kept = C.c_int32.from_address(cache._h.value + C.sizeof(paged._CacheConfig))
+    assert kept.value == torch.cuda.current_device()
+    for call in calls:
+        call()
+        kept.value += 1
+        with pytest.raises(wisv.WisvError) as e:
+            call()
+        kept.value -= 1
+        assert e.value.code == -1
+    cache.close()
