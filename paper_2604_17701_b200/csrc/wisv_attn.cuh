@@ -53,7 +53,7 @@ constexpr int kAttnSlack = 256;                  // for aligning the tiles to 10
 constexpr uint64_t kAttnWaitClocks = 4000000000ull;       // the limit of every wait, unless a test has set a shorter one
 
 struct AttnParams {
-    int32_t B, T, max_new, n_kv, group, tpt, page_shift, n_pages, max_blocks;
+    int32_t B, T, n_kv, group, tpt, page_shift, n_pages, max_blocks;
     int32_t page_groups_k, page_groups_v;        // 8-token groups from one page to the next
     int32_t groups_k, groups_v;                  // 8-token groups in the whole pool: the first coordinate out of range
     int32_t uniform;                             // rows per request where q_off is NULL

@@ -399,7 +399,7 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     // every key tile of every item has to count in 31 bits, whatever the lengths on the device say
     const int64_t items = (a->T + p.tpt - 1) / p.tpt + a->B, tiles = ((int64_t)a->max_blocks << c->page_shift) / kAttnTile + 2;
     if (items * tiles > 0x7ffe0000LL / c->cfg.n_kv_heads) return WISV_ESHAPE;
-    p.B = a->B; p.T = a->T; p.max_new = a->max_new; p.n_kv = c->cfg.n_kv_heads; p.group = group;
+    p.B = a->B; p.T = a->T; p.n_kv = c->cfg.n_kv_heads; p.group = group;
     p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
     p.uniform = a->max_new; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
     p.table_stride = a->table_stride;
