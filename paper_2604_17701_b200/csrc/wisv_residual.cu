@@ -38,8 +38,7 @@ constexpr int kResMaxCluster = 16;
 constexpr int kChunk = 512;                        // tokens whose weights a warp adds into one sum: 512 (2^23 - 1) < 2^32
 constexpr int kMaxChunks = WISV_STATIC_MAX_V / kChunk;
 constexpr int kChunksPerThread = kMaxChunks / kResThreads;
-constexpr int kResSms = 148;
-constexpr int kResResident = 8 * kResSms;          // blocks that run at once
+constexpr int kResPerSm = 8;                       // blocks that run on an SM at once
 constexpr float kFix = 17592186044416.0f;          // 2^44
 constexpr int kQuiet = 0, kDense = 1, kTop = 2;    // the drafter's distribution: one token, dense, a list
 
@@ -126,7 +125,7 @@ __device__ __forceinline__ void st_cluster_u64(uint32_t addr, u64 x)
 }
 
 template <typename TP, typename TQ, int kForm, bool kWide>
-__global__ void __launch_bounds__(kResThreads, 8) residual_kernel(const ResidualParams p)
+__global__ void __launch_bounds__(kResThreads, kResPerSm) residual_kernel(const ResidualParams p)
 {
     __shared__ u64 chunk_mass[kMaxChunks];
     __shared__ u64 warp_mass[kResWarps];
@@ -460,8 +459,9 @@ extern "C" int wisv_verify_residual(const wisv_residual* r, void* cuda_stream)
     const int ps = size_of(r->target_dtype), qs = dense ? size_of(r->draft_dtype) : 4;
     if (!rows_aligned(r->target_probs, 0, 1, ps) || (r->draft_probs && !rows_aligned(r->draft_probs, 0, 1, qs)))
         return WISV_EALIGN;
-    int dev = 0, major = 0;
+    int dev = 0, major = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) {
         (void)cudaGetLastError();
         return WISV_ECUDA;
@@ -473,8 +473,8 @@ extern "C" int wisv_verify_residual(const wisv_residual* r, void* cuda_stream)
     // Blocks per request: as many as can run at once, so that a small batch uses the whole chip and a large one pays for the
     // acceptance test and the exchange once per request; 16 only while every block has an SM to itself (one request: 7.0 us
     // against 8.5 with 8; 64 requests: 12.0 against 11.0).
-    p.cluster = r->B * kResMaxCluster <= kResSms ? kResMaxCluster : kResMaxCluster / 2;
-    while (p.cluster > 1 && (int64_t)p.B * p.cluster > kResResident) p.cluster >>= 1;
+    p.cluster = r->B * kResMaxCluster <= sms ? kResMaxCluster : kResMaxCluster / 2;
+    while (p.cluster > 1 && (int64_t)p.B * p.cluster > kResPerSm * sms) p.cluster >>= 1;
     p.k_off = r->k_off; p.P = r->target_probs; p.p_stride = r->target_stride;
     p.Q = r->draft_probs; p.q_stride = r->draft_stride; p.ids = r->draft_ids; p.tokens = r->draft_tokens;
     p.u = r->uniforms; p.u_draw = r->u_draw; p.accept_in = r->accept_in;
