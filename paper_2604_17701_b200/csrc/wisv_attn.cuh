@@ -45,8 +45,12 @@ constexpr int kAttnThreads = 512;
 constexpr int kAttnTile = 128;                   // rows of a row tile, keys of a key tile
 constexpr int kAttnSub = 64;                     // keys of a job
 constexpr int kAttnMaxStages = 12;
-constexpr int kAttnMinUnits = 2;                 // the smallest stretch worth a block of its own: shorter ones cost more to merge than they save
-constexpr int kAttnItemCost = 1;                 // key tiles that starting and finishing an item is worth
+// The smallest stretch worth a block of its own: shorter ones cost more to merge than they save.  (One window of 9 rows over 709 keys with
+// 1, 2, 3, 4: 13.7, 12.4, 15.3, 15.5 us.  Where blocks have more than that to do it does not matter.)
+constexpr int kAttnMinUnits = 2;
+// Key tiles that starting and finishing an item is worth: with 0, 1, 2 one window takes 12.5, 12.4, 12.6 us, 64 requests of one row over 258 k
+// keys 169.0, 165.5, 165.2, ragged windows over 141 k keys 113-117, 107-113, 108.
+constexpr int kAttnItemCost = 1;
 constexpr int kAttnSmem = 232448;                // all of an SM's shared memory that a block can have
 constexpr int kAttnSmall = 2816;                 // barriers, the queue of stretches, the slots' exchange of m and l
 constexpr int kAttnSlack = 256;                  // for aligning the tiles to 1024 bytes

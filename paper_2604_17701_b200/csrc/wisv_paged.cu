@@ -163,9 +163,12 @@ void fill_pages(const wisv_cache* c, const wisv_pages* pg, int32_t B, PagesParam
     p->seq_len = pg->seq_len;
 }
 
-// rounds with more rows than this are laid out by a cluster of eight blocks
-constexpr int kExtendOneBlockRows = 4096;
-constexpr int kCommitOneBlockRequests = 64;
+// One block, or a cluster of eight that repeats the scan and shares the rest.  extend: a row per thread at most for one block (one / eight:
+// 576 rows of 64 requests 4.15 / 4.23 us, 1088 rows 4.85 / 4.33, 4608 rows of 512 requests 8.1 / 4.6, 69632 of 4096 78 / 17).
+constexpr int kExtendOneBlockRows = 1024;
+// commit: the pages that go back are what the blocks share, and only the device knows how many (extend and commit with a commit of one
+// / eight: 512 requests of 9 rows 9.66 / 9.96 us, 1024 of 9 11.9 / 12.3, 2048 of 9 16.9 / 16.5, 4096 of 2 17.4 / 17.7, of 17 32.9 / 28.4).
+constexpr int kCommitOneBlockRequests = 1024;
 
 // Programmatic dependent launch: the block set-up (barriers, TMEM) runs while the kernel before it in the stream ends.
 template <typename E, int D>
