@@ -264,20 +264,21 @@ __device__ __forceinline__ uint32_t attn_idesc(uint32_t M, uint32_t N, bool b_mn
 }
 
 // ---------------------------------------------------------------- work items
-// One request as the kernel sees it; device-side lengths are clamped to what the arrays hold.
+// One request as the kernel sees it; device-side lengths are clamped to what the arrays hold.  (Offsets, lengths and tables may be
+// written by a kernel that still runs when this one's blocks start, so they are not read through the read-only path.)
 struct AttnReq { int q0, n, kv, items; };
 
 __device__ __forceinline__ AttnReq attn_request(const AttnParams& p, int b)
 {
     AttnReq r;
     if (p.q_off) {
-        r.q0 = min(max(__ldg(p.q_off + b), 0), p.T);
-        r.n = max(min(max(__ldg(p.q_off + b + 1), 0), p.T) - r.q0, 0);
+        r.q0 = min(max(p.q_off[b], 0), p.T);
+        r.n = max(min(max(p.q_off[b + 1], 0), p.T) - r.q0, 0);
     } else {
         r.q0 = b * p.uniform;
         r.n = p.uniform;
     }
-    r.kv = min(max(__ldg(p.kv_len + b), 0), p.max_blocks << p.page_shift);
+    r.kv = min(max(p.kv_len[b], 0), p.max_blocks << p.page_shift);
     r.items = ((r.n + p.tpt - 1) / p.tpt + 1) >> 1;
     return r;
 }
@@ -495,7 +496,7 @@ __device__ __forceinline__ void add_odd_elements(const E* v, float (&x)[32])
 {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(v) + i), odd = w & odd_elements<E>(w);
+        const uint32_t w = reinterpret_cast<const uint32_t*>(v)[i], odd = w & odd_elements<E>(w);
         if (is_bf16<E>::value) {
             x[2 * i] += __uint_as_float(odd << 16);
             x[2 * i + 1] += __uint_as_float(odd & 0xffff0000u);
@@ -528,7 +529,7 @@ template <int D> __host__ __device__ constexpr int attn_stages()
 __device__ __forceinline__ int attn_page(const AttnParams& p, int req, int t, int t1, int keys, int lane)
 {
     const int box_tok = min(1 << p.page_shift, kAttnTile), tok = t * kAttnTile + lane * box_tok;
-    return t < t1 && lane * box_tok < kAttnTile && tok < keys ? __ldg(p.block_table + req * p.table_stride + (tok >> p.page_shift)) : -1;
+    return t < t1 && lane * box_tok < kAttnTile && tok < keys ? p.block_table[req * p.table_stride + (tok >> p.page_shift)] : -1;
 }
 
 // The copies of key (or value) tiles t0 .. t1 - 1 of a request into every other entry of the ring, by one warp.  `pg`: attn_page
@@ -569,7 +570,7 @@ template <typename E, int D>
 __device__ __forceinline__ void attn_clear_rows(const AttnParams& p, int w, int all, int lane)
 {
     if (!p.q_off) return;
-    const int head = min(max(__ldg(p.q_off), 0), p.T), tail = min(max(__ldg(p.q_off + p.B), head), p.T);
+    const int head = min(max(p.q_off[0], 0), p.T), tail = min(max(p.q_off[p.B], head), p.T);
     const int heads = p.n_kv * p.group;
     for (int i = w; i < head + p.T - tail; i += all) {
         const int64_t t = i < head ? i : tail + (i - head);
@@ -1001,7 +1002,7 @@ attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUt
                         const int lo = max(max(sg[kSegLimit] + 1, 0), sg[kSegT0] * kAttnTile);
                         const int hi = min(sg[kSegLimit] + tok - sg[kSegRow], sg[kSegT1] * kAttnTile - 1);       // the row's last key here
                         for (int key = lo; key <= hi; ++key) {
-                            const int pg = __ldg(p.block_table + sg[kSegReq] * p.table_stride + (key >> p.page_shift));
+                            const int pg = p.block_table[sg[kSegReq] * p.table_stride + (key >> p.page_shift)];
                             if (pg >= 0 && pg < p.n_pages)
                                 add_odd_elements<E>(static_cast<const E*>(p.v) + pg * p.vp + (key & ((1 << p.page_shift) - 1)) * p.vt +
                                                         sg[kSegHead] * p.vh + c, x);

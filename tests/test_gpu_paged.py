@@ -563,3 +563,25 @@ def test_another_current_device_is_refused():
         kept.value -= 1
         assert e.value.code == -1
     cache.close()
+
+
+def test_attention_right_behind_the_call_that_lays_pages_out():
+    """extend hands out pages, commit takes them back, and attend reads the table in the next launch, with nothing between."""
+    B, page, H, kv, d = 96, 16, 8, 2, 64
+    cache = make_cache(n_heads=H, n_kv_heads=kv, head_dim=d, page_size=page, n_pages=B * 16, max_requests=B, max_blocks=16)
+    torch.manual_seed(0)
+    kp, vp = (torch.randn(B * 16, page, kv, d, device=DEV).bfloat16() for _ in range(2))
+    q = torch.randn(B * 20, H, d, device=DEV).bfloat16()
+    outs, layouts, tables = [], [], []
+    order = torch.randperm(B * 16, device=DEV).int()
+    for step in range(8):
+        cache.free_list.copy_(order.roll(step * 7))                # other pages every time
+        lay = cache.extend(B=B, n_new=20)
+        outs.append(cache.attend(q, kp, vp, lay.kv_len, B=B, max_new=20, q_off=lay.q_off))
+        layouts.append(lay.kv_len.clone())
+        tables.append(cache.block_table.clone())
+        cache.commit(torch.zeros(B, dtype=torch.int32, device=DEV) if step % 2 else lay.kv_len - 7, B=B)
+    off = [20 * b for b in range(B + 1)]
+    for out, kv_len, table in zip(outs, layouts, tables):
+        check(out, None, reference(q, kp, vp, table, kv_len.tolist(), off, d ** -0.5), "bf16", 256)
+    cache.close()
