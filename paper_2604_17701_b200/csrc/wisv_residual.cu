@@ -90,7 +90,7 @@ struct Piece {
             const int at = v + h * 256 + lane * 8;
             if (kWide && at + 8 <= V) {
 #pragma unroll
-                for (int i = 0; i < n; ++i) w[h * n + i] = __ldg(reinterpret_cast<const uint4*>(row + at) + i);
+                for (int i = 0; i < n; ++i) w[h * n + i] = reinterpret_cast<const uint4*>(row + at)[i];
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
