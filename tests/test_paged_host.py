@@ -96,7 +96,7 @@ def test_binding_needs_a_cuda_device():
         wisv.PagedCache(**{**GOOD, "device": "cpu"})
 
 
-@pytest.mark.parametrize("i, name", enumerate(n for n, _ in paged._Pages._fields_))
+@pytest.mark.parametrize("i, name", list(enumerate(n for n, _ in paged._Pages._fields_)))
 def test_bookkeeping_arrays_cannot_be_replaced(i, name):
     """The library holds their addresses: another tensor in the attribute would give the calls different tables."""
     cache = object.__new__(wisv.PagedCache)
