@@ -6,9 +6,17 @@
 // type because the second product takes 16-bit operands.  O is rescaled only when a row's maximum has grown by
 // more than 2^8 since its last rescaling: P then stays below 2^8, which loses nothing in a floating-point type.
 //
-// Measured (8B shape: 32 query heads, 8 key heads, D = 128): 64 requests of one row over 258 k keys in all 165 us, 6.4 TB/s, 0.98 of the
-// copy rate, 175-187 us back to back under the power cap; 2 x 2048 rows over 8 k keys 485-500 us, 1.1 PFLOP/s, 561-571 us under the
-// cap; one request of 9 rows over 709 keys 12.2 us.
+// (That rounding is most of the kernel's own error: relative to 64 bits 2.3e-3 in bf16 and 2.8e-4 in fp16, of which rounding the
+// result alone is 1.7e-3 and 2.1e-4.)
+//
+// A score of +inf or NaN makes its row NaN.  Masked scores have weight 0 exactly, and values are multiplied by it only where they are
+// finite: in the jobs that some row of an item does not see, infinite and NaN elements of V are taken out and added afterwards
+// to the rows that see them.
+//
+// Measured (8B shape: 32 query heads, 8 key heads, D = 128), back to back under the power cap and, in brackets, in runs of some
+// milliseconds: 64 requests of one row over 258 k keys in all 179 us, 5.9 TB/s, 0.91 of the copy rate (165 us); 2 x 2048 rows over
+// 8 k keys 553 us, 0.99 PFLOP/s (490-530 us); 8 requests of 65 rows over 120 k keys 152 us (128 us); one request of 9 rows over
+// 709 keys 12.4 us.  With D = 64: 110 us in short runs, 413 us, -, 10.4 us.
 //
 // What bounds it.  A window of K + 1 rows has group * (K + 1) rows per key head, so up to some 64 of them the kernel moves
 // 4 D bytes per key and does 4 D flops per row and key: bound by HBM as long as one 128-row MMA tile (1024 clocks for 128
@@ -16,8 +24,8 @@
 // rate).  Prompt chunks are bound by the MMAs and by the exponentials, 1024 clocks each per 128 x 128 tile.
 //
 // Roles.  One block per SM, persistent: a warp that walks the work and copies queries and keys by TMA, one that copies values, four
-// that issue the MMAs (S and O of each slot), and two sets of four softmax warps, each set ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either
-// "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
+// that issue the MMAs (S and O of each slot), two that only clear rows of no window, and two sets of four softmax warps, each set
+// ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
 // single row tile is left, "split": the slots take the key tiles in turn and are put together at the end.  Either way
 // the slots work at different 64-key jobs, and each has two S of 64 columns in turn: S of a job waits for O of the slot's last job but
 // one alone, so it is computed under the exponentials of the job before and under the other slot's products.
@@ -45,11 +53,11 @@ constexpr int kAttnThreads = 512;
 constexpr int kAttnTile = 128;                   // rows of a row tile, keys of a key tile
 constexpr int kAttnSub = 64;                     // keys of a job
 constexpr int kAttnMaxStages = 12;
-// The smallest stretch worth a block of its own: shorter ones cost more to merge than they save.  (One window of 9 rows over 709 keys with
-// 1, 2, 3, 4: 13.7, 12.4, 15.3, 15.5 us.  Where blocks have more than that to do it does not matter.)
+// The smallest stretch worth a block of its own: shorter ones cost more to merge than they save.  (One window of 9 rows over 709
+// keys with 1, 2, 3, 4: 13.7, 12.4, 15.3, 15.5 us.  Where blocks have more than that to do it does not matter.)
 constexpr int kAttnMinUnits = 2;
-// Key tiles that starting and finishing an item is worth: with 0, 1, 2 one window takes 12.5, 12.4, 12.6 us, 64 requests of one row over 258 k
-// keys 169.0, 165.5, 165.2, ragged windows over 141 k keys 113-117, 107-113, 108.
+// Key tiles that starting and finishing an item is worth: with 0, 1, 2 one window takes 12.5, 12.4, 12.6 us, 64 requests of one row
+// over 258 k keys 169.0, 165.5, 165.2, ragged windows over 141 k keys 113-117, 107-113, 108.
 constexpr int kAttnItemCost = 1;
 constexpr int kAttnSmem = 232448;                // all of an SM's shared memory that a block can have
 constexpr int kAttnSmall = 2816;                 // barriers, the queue of stretches, the slots' exchange of m and l
@@ -117,8 +125,8 @@ __device__ __forceinline__ float attn_ex2(float x)
     return y;
 }
 
-// Bounded wait; `flag` is the shared-memory address of the block's abort flag, three words before the limit.  One inline try and everything else out of
-// line: a try that is the condition of an inline loop costs some 370 clocks even where the barrier is complete.
+// Bounded wait; `flag` is the shared-memory address of the block's abort flag, three words before the limit.  One inline try and
+// everything else out of line: a try that is the condition of an inline loop costs some 370 clocks even where the barrier is complete.
 static __device__ __forceinline__ bool attn_wait_slow(uint32_t bar, uint32_t parity, uint32_t flag)
 {
     const long long t0 = clock64();
@@ -180,7 +188,8 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
 // fp32).  From x = -127 down it gives 0 exactly (the exponent of 1 less 127 is that of 0), as a masked score must; between -126 and
 // -127 something below 2^-126.
 // The special-function unit does 16 exponentials a clock, which for a 128 x 128 tile takes as long as both matrix products;
-// kAttnPoly of every 8 pairs go this way instead (2048-row chunks under the power cap: 574, 566, 577, 592 us with 0 to 3).
+// kAttnPoly of every 8 pairs go this way instead (2 x 2048 rows under the power cap with 0 to 3: 570, 553, 560, 564 us; D = 64:
+// 442, 413, 422, 430).
 constexpr int kAttnPoly = 1;
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x)
 {

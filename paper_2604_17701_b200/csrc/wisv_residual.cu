@@ -6,8 +6,11 @@
 // has to be read.  The row is cut into chunks of 512 tokens; a warp adds up the weights of a chunk and keeps the sum in shared
 // memory, the blocks exchange their totals through distributed shared memory, and the block whose chunks hold the
 // goal scans its sums and reads that one chunk again (from L2) to find the token.  So the row crosses HBM once, and that
-// is the bound: V (size(P) + size(Q)) bytes per request.  (512 requests, 152064 bf16 with 64 listed drafts: 37 us, of which the
-// row streams at 4.8 TB/s for 26; 64 requests with two bf16 rows of 128256 10.5 us; one with two fp32 rows 6.5 us.)
+// is the bound: V (size(P) + size(Q)) bytes per request.  (512 requests, 152064 bf16 with 64 listed drafts: 156 MB in 37 us, 4.2
+// TB/s; in the median block the acceptance test is done after 4.6 us and the row read after 36, 5.0 TB/s between, and the last
+// token is out 3 us behind the last row.  The same with a deterministic drafter 37 us; 64 requests with two bf16 rows of 128256
+// 10.4 us; one with two fp32 rows 6.6 us.  Rows that are not 16-byte aligned are read by elements: 512 requests of 152065 75 us, 64
+// of two rows of 128257 22 us.)
 //
 // Weights are integers (2^-44 units): addition is exact in any order, so the token depends neither on the number of
 // blocks nor on how the row was cut, and a row whose mass is spread over 2^18 tokens still leaves each token with
