@@ -527,7 +527,8 @@ int wisv_cache_append(wisv_cache* cache, const wisv_append* a, void* cuda_stream
  * or NaN makes the row and its lse NaN.  An infinite or NaN value reaches the rows that see its key, in its own column, and no
  * other.  Scores, maxima, sums and products are accumulated in fp32; the probabilities are rounded to the cache's 16-bit type
  * for the second product.
- * Rows of q that no window covers (before q_off[0], or from q_off[B] on) give zero and -inf likewise.
+ * Rows of q that no window covers (before q_off[0], or from q_off[B] on) are left as they are in out and lse, so that several
+ * calls can share them, or give zero and -inf where clear_rest says so (a batch padded to a fixed number of rows).
  * Keys and values past kv_len[b] (and whole pages that the table does not reach) may hold anything, NaN included; table entries
  * outside the pool read as zeros.
  */
@@ -548,6 +549,7 @@ typedef struct {
     int64_t o_token_stride, o_head_stride;
     float* lse;                          /* dev [T, n_heads], optional: natural log of the sum of exp(scale * q k^T) */
     float scale;                         /* 0: 1 / sqrt(head_dim) */
+    int32_t clear_rest;                  /* non-zero: rows that no window covers are written too */
 } wisv_attend;
 int wisv_cache_attend(wisv_cache* cache, const wisv_attend* a, void* cuda_stream);
 

@@ -24,7 +24,7 @@
 // rate).  Prompt chunks are bound by the MMAs and by the exponentials, 1024 clocks each per 128 x 128 tile.
 //
 // Roles.  One block per SM, persistent: a warp that walks the work and copies queries and keys by TMA, one that copies values, four
-// that issue the MMAs (S and O of each slot), two that only clear rows of no window, and two sets of four softmax warps, each set
+// that issue the MMAs (S and O of each slot), two that at most clear rows of no window, and two sets of four softmax warps, each set
 // ("slot") with its own S and O in TMEM (all 512 columns).  A work item is either "paired" - two row tiles of the same (request, key head), one per slot, sharing each tile of keys - or, where a
 // single row tile is left, "split": the slots take the key tiles in turn and are put together at the end.  Either way
 // the slots work at different 64-key jobs, and each has two S of 64 columns in turn: S of a job waits for O of the slot's last job but
@@ -69,6 +69,7 @@ struct AttnParams {
     int32_t page_groups_k, page_groups_v;        // 8-token groups from one page to the next
     int32_t groups_k, groups_v;                  // 8-token groups in the whole pool: the first coordinate out of range
     int32_t uniform;                             // rows per request where q_off is NULL
+    int32_t clear_rest;                          // rows of no window are written too
     const int32_t *q_off, *kv_len, *block_table;
     int64_t table_stride;
     const void* v; int64_t vp, vt, vh;           // the value pool and its strides, for values that are infinite or NaN
@@ -578,7 +579,7 @@ __device__ __forceinline__ bool attn_load_tiles(const AttnParams& p, const CUten
 template <typename E, int D>
 __device__ __forceinline__ void attn_clear_rows(const AttnParams& p, int w, int all, int lane)
 {
-    if (!p.q_off) return;
+    if (!p.q_off || !p.clear_rest) return;
     const int head = min(max(p.q_off[0], 0), p.T), tail = min(max(p.q_off[p.B], head), p.T);
     const int heads = p.n_kv * p.group;
     for (int i = w; i < head + p.T - tail; i += all) {

@@ -404,7 +404,7 @@ int wisv_cache_attend(wisv_cache* c, const wisv_attend* a, void* cuda_stream)
     if (items * tiles > 0x7ffe0000LL / c->cfg.n_kv_heads) return WISV_ESHAPE;
     p.B = a->B; p.T = a->T; p.n_kv = c->cfg.n_kv_heads; p.group = group;
     p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
-    p.uniform = a->max_new; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
+    p.uniform = a->max_new; p.clear_rest = a->clear_rest; p.q_off = a->q_off; p.kv_len = a->kv_len; p.block_table = a->block_table;
     p.table_stride = a->table_stride;
     p.v = a->v_pages; p.vp = s[7]; p.vt = s[8]; p.vh = s[9];
     p.out = a->out; p.ot = s[2]; p.oh = s[3]; p.lse = a->lse;

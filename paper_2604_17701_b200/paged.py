@@ -40,7 +40,7 @@ class _Attend(C.Structure):
                 ("kp_page_stride", C.c_int64), ("kp_token_stride", C.c_int64), ("kp_head_stride", C.c_int64),
                 ("vp_page_stride", C.c_int64), ("vp_token_stride", C.c_int64), ("vp_head_stride", C.c_int64),
                 ("out", C.c_void_p), ("o_token_stride", C.c_int64), ("o_head_stride", C.c_int64), ("lse", C.c_void_p),
-                ("scale", C.c_float)]
+                ("scale", C.c_float), ("clear_rest", C.c_int32)]
 
 
 class _Residual(C.Structure):
@@ -276,16 +276,19 @@ class PagedCache:
                                 _array("slot_map", slot_map, self._torch.int64, T, self._index)))
 
     def attend(self, q, k_pages, v_pages, kv_len, *, B: int, max_new: int, q_off=None, out=None, lse=None,
-               scale: Optional[float] = None, block_table=None, stream=None):
+               scale: Optional[float] = None, block_table=None, clear_rest: Optional[bool] = None, stream=None):
         """wisv_cache_attend: attention of the new rows q [T, n_heads, head_dim] over the cache, causal among
-        themselves.  kv_len: int32 [B], new tokens included; q_off: int32 [B+1], or None for max_new rows each."""
+        themselves.  kv_len: int32 [B], new tokens included; q_off: int32 [B+1], or None for max_new rows each.
+        Rows of q before q_off[0] or from q_off[B] on give zeros (-inf in lse) with clear_rest, which is the default where
+        the output is made here, and are left alone in an output that is given."""
         torch, dev = self._torch, self._index
         i32 = torch.int32
         H, D = self.n_heads, self.head_dim
         qp, qt, qh, T = self._rows("q", q, H)
         kpool, k0, k1, k2 = self._pages_of("k_pages", k_pages)
         vpool, v0, v1, v2 = self._pages_of("v_pages", v_pages)
-        if out is None:
+        made = out is None
+        if made:
             out = _empty(torch, stream, (T, H, D), self.dtype, self.device)
             op, ot, oh = out.data_ptr(), H * D, D
         else:
@@ -305,7 +308,7 @@ class PagedCache:
                    _pack_attend(B, T, max_new, 0 if q_off is None else _array("q_off", q_off, i32, B + 1, dev),
                                 _array("kv_len", kv_len, i32, B, dev), table.data_ptr(), step, blocks, qp, qt, qh,
                                 kpool, vpool, k0, k1, k2, v0, v1, v2, op, ot, oh, 0 if lse is None else lse.data_ptr(),
-                                0.0 if scale is None else scale))
+                                0.0 if scale is None else scale, made if clear_rest is None else bool(clear_rest)))
         return out
 
     def device_error(self) -> int:

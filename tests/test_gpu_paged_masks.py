@@ -147,14 +147,29 @@ def test_rows_outside_all_windows_are_zero(H, kv, d, dtype):
         wide[before:before + q.shape[0]] = q
         big = torch.full((T + 1, H + 1, d + 8), NAN, dtype=q.dtype, device=DEV)
         lse = torch.full((T, H), NAN, dtype=torch.float32, device=DEV)
-        out = cache.attend(wide, kp, vp, dev(kv_len), B=2, max_new=70, q_off=dev(q_off) + before, out=big[:T, :H, :d], lse=lse)
+        out = cache.attend(wide, kp, vp, dev(kv_len), B=2, max_new=70, q_off=dev(q_off) + before, out=big[:T, :H, :d], lse=lse,
+                           clear_rest=True)
         inside = torch.zeros(T, dtype=torch.bool, device=DEV)
         inside[before:before + q.shape[0]] = True
         assert (out[~inside] == 0).all() and (lse[~inside] == -INF).all()
         check(out[inside], lse[inside], ref, dtype, 900)
         big[:T, :H, :d] = NAN
         assert torch.isnan(big).all()                              # nothing beside the output was written
-    # no window has a row
-    out = cache.attend(q, kp, vp, dev(kv_len), B=2, max_new=1, q_off=dev([0, 0, 0]), out=torch.full_like(q, NAN))
+    # an output that the call makes is whole without being asked for; no window has a row
+    out = cache.attend(q, kp, vp, dev(kv_len), B=2, max_new=1, q_off=dev([0, 0, 0]))
     assert (out == 0).all() and cache.device_error() == 0
+    cache.close()
+
+
+def test_calls_that_share_an_output_leave_each_others_rows_alone():
+    """Two calls over parts of one packed batch, in either order, the offsets those of the whole."""
+    n_new, kv_len = [4, 70, 1, 9], [100, 900, 33, 40]
+    cache, q, kp, vp, q_off = build(n_new=n_new, kv_len=kv_len, H=8, kv=2, d=128, page=16, dtype="bf16", seed=6)
+    ref = reference(q, kp.nan_to_num(0.0), vp.nan_to_num(0.0), cache.block_table, kv_len, q_off, 128 ** -0.5)
+    for parts in (((0, 2), (2, 4)), ((2, 4), (0, 2)), ((1, 2), (0, 1), (2, 4))):
+        out, lse = torch.full_like(q, NAN), torch.full(q.shape[:2], NAN, dtype=torch.float32, device=DEV)
+        for lo, hi in parts:
+            cache.attend(q, kp, vp, dev(kv_len[lo:hi]), B=hi - lo, max_new=70, q_off=dev(q_off[lo:hi + 1]), out=out, lse=lse,
+                         block_table=cache.block_table[lo:hi])
+        check(out, lse, ref, "bf16", 900)
     cache.close()
