@@ -476,7 +476,7 @@ int wisv_cache_create(const wisv_cache_config* cfg, wisv_cache** out);
 int wisv_cache_destroy(wisv_cache* cache);          /* the caller must have synchronised */
 int64_t wisv_cache_launch_count(const wisv_cache* cache);
 /* Read (and clear) the device error word: bit 0 if a bounded wait inside a kernel gave up (the results of that call are not to be
- * used; calls after it are not affected), bit 2 if offsets that overlap made more work than a call can count (nothing was
+ * used; calls after it are not affected), bit 1 if shared memory did not start where the tiles need it (nothing was done), bit 2 if offsets that overlap made more work than a call can count (nothing was
  * done).  Synchronises the stream. */
 int wisv_cache_error(wisv_cache* cache, void* cuda_stream, int32_t* flags);
 
