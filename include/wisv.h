@@ -554,7 +554,82 @@ typedef struct {
 int wisv_cache_attend(wisv_cache* cache, const wisv_attend* a, void* cuda_stream);
 
 /*
- * Test hook for the failure path: in the calls of wisv_cache_attend that follow, waits give up after limit_cycles SM clocks (0: the
+ * The same cache in 8 bits: half the bytes to hold and to read.  A head of a token is head_dim e4m3 codes and one fp32 scale, for keys
+ * and values alike; the bookkeeping above (pages, tables, slots, lengths) is shared, and queries, new keys and values, and outputs have
+ * the cache's 16-bit type.  Pools belong to the caller.  Strides of codes are in bytes and multiples of 16, those of scales in floats and
+ * multiples of 4, bases 16-byte aligned; the codes of a head are contiguous, and so are the scales of a page's tokens for one head.  For
+ * wisv_cache_attend_q8 strides of codes are not negative and token strides not 0.
+ */
+typedef struct {
+    void *k, *v;                                                          /* dev e4m3 [n_pages, page_size, n_kv_heads, head_dim] */
+    int64_t k_page_stride, k_token_stride, k_head_stride, v_page_stride, v_token_stride, v_head_stride;
+    float *k_scale, *v_scale;                                             /* dev [n_pages, n_kv_heads, page_size] */
+    int64_t ks_page_stride, ks_head_stride, vs_page_stride, vs_head_stride;
+} wisv_q8_pages;
+
+/*
+ * Keys and values of one layer, quantised into their slots: per token and head, with t the largest |x| of its elements, scale = t / 448
+ * and code = 448 x / t rounded to the nearest e4m3 number, ties to even.  A head of zeros has scale 0; one with an infinite element or
+ * NaN has scale NaN and codes of 0, so that it makes NaN of what sees it, and of nothing else.  Strides of k and v, and slots, as in
+ * wisv_append.
+ */
+typedef struct {
+    int32_t T;                                                            /* rows */
+    const void *k, *v;                                                    /* dev [T, n_kv_heads, head_dim] */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int64_t* slot_map;                                              /* dev [T] */
+} wisv_q8_append;
+int wisv_cache_append_q8(wisv_cache* cache, const wisv_q8_pages* pages, const wisv_q8_append* a, void* cuda_stream);
+
+/*
+ * Tokens read back as 16-bit rows: row off[b] + i is token start[b] + i of request b, code * scale in fp32 rounded once.  A token that the
+ * table does not reach, or whose entry lies outside the pool, reads as zeros; what lies behind a request's length in a page it holds reads
+ * as it is.  Rows before off[0], or from off[B] on, are left as they are, or zero where clear_rest says so.
+ */
+typedef struct {
+    int32_t B;
+    int32_t T;                           /* rows of k and v */
+    int32_t n_uniform;                   /* tokens per request where off is NULL */
+    const int32_t* off;                  /* dev [B+1], ascending, or NULL */
+    const int32_t* start;                /* dev [B]: first token read of each request, or NULL: 0 */
+    const int32_t* block_table;          /* dev */
+    int64_t table_stride;                /* entries per row of the table */
+    int32_t max_blocks;                  /* entries of a row that may be read */
+    int32_t clear_rest;
+    void *k, *v;                         /* dev [T, n_kv_heads, head_dim], strides as in wisv_append */
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} wisv_q8_read;
+int wisv_cache_read_q8(wisv_cache* cache, const wisv_q8_pages* pages, const wisv_q8_read* r, void* cuda_stream);
+
+/*
+ * wisv_cache_attend over 8-bit pools: the same rows, masks, lse, rows without a key, rows of no window and work hint.  The codes are operands of
+ * the matrix products as they are and scales enter in fp32; queries and probabilities enter with the precision of the cache's
+ * type, down to 2^-18 of a query's (2^-16 of the probabilities') largest element.  A score of +inf or NaN makes its row and lse NaN, and so does a token
+ * whose scale is NaN, in the rows that see it.  Codes of the tokens that rows see are numbers (wisv_cache_append_q8 writes no other): the code of
+ * NaN in a window may reach each of its rows.  Codes and scales past kv_len[b], and pages that the table does not reach, may
+ * hold anything.  Scales of values count as at least 2^-100, and as 2^-40 of the largest among the 32 tokens around them.
+ */
+typedef struct {
+    int32_t B;
+    int32_t T;                           /* rows of q */
+    int32_t max_new;                     /* largest number of new tokens expected: a hint, as in wisv_attend */
+    const int32_t* q_off;                /* dev [B+1], or NULL: max_new rows per request */
+    const int32_t* kv_len;               /* dev [B]: cached tokens, the new ones included */
+    const int32_t* block_table;          /* dev */
+    int64_t table_stride;                /* entries per row of the table */
+    int32_t max_blocks;                  /* entries of a row that may be read */
+    const void* q;                       /* dev [T, n_heads, head_dim] */
+    int64_t q_token_stride, q_head_stride;
+    void* out;                           /* dev [T, n_heads, head_dim] */
+    int64_t o_token_stride, o_head_stride;
+    float* lse;                          /* dev [T, n_heads], optional */
+    float scale;                         /* 0: 1 / sqrt(head_dim) */
+    int32_t clear_rest;                  /* non-zero: rows that no window covers are written too */
+} wisv_q8_attend;
+int wisv_cache_attend_q8(wisv_cache* cache, const wisv_q8_pages* pages, const wisv_q8_attend* a, void* cuda_stream);
+
+/*
+ * Test hook for the failure path: in the calls of wisv_cache_attend and wisv_cache_attend_q8 that follow, waits give up after limit_cycles SM clocks (0: the
  * usual 4e9), and the thread block `block` (-1: none) never copies values, so that waits of that block run out.  They set
  * bit 0 of the error word that wisv_cache_error reports; rows that the block had a part in are not written.
  */

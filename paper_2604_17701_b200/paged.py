@@ -43,6 +43,34 @@ class _Attend(C.Structure):
                 ("scale", C.c_float), ("clear_rest", C.c_int32)]
 
 
+class _Q8Pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_page_stride", C.c_int64), ("k_token_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("v_page_stride", C.c_int64), ("v_token_stride", C.c_int64),
+                ("v_head_stride", C.c_int64), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("ks_page_stride", C.c_int64), ("ks_head_stride", C.c_int64), ("vs_page_stride", C.c_int64),
+                ("vs_head_stride", C.c_int64)]
+
+
+class _Q8Append(C.Structure):
+    _fields_ = [("T", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_token_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("slot_map", C.c_void_p)]
+
+
+class _Q8Read(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("n_uniform", C.c_int32), ("off", C.c_void_p), ("start", C.c_void_p),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("max_blocks", C.c_int32), ("clear_rest", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64)]
+
+
+class _Q8Attend(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("max_new", C.c_int32), ("q_off", C.c_void_p), ("kv_len", C.c_void_p),
+                ("block_table", C.c_void_p), ("table_stride", C.c_int64), ("max_blocks", C.c_int32), ("q", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("out", C.c_void_p), ("o_token_stride", C.c_int64),
+                ("o_head_stride", C.c_int64), ("lse", C.c_void_p), ("scale", C.c_float), ("clear_rest", C.c_int32)]
+
+
 class _Residual(C.Structure):
     _fields_ = [("B", C.c_int32), ("K", C.c_int32), ("k_off", C.c_void_p), ("T_total", C.c_int32), ("V", C.c_int32),
                 ("target_probs", C.c_void_p), ("target_stride", C.c_int64), ("target_dtype", C.c_int32),
@@ -61,6 +89,7 @@ def _packer(cls):
 
 
 _pack_layout, _pack_append, _pack_attend, _pack_residual = (_packer(c) for c in (_Layout, _Append, _Attend, _Residual))
+_pack_q8_pages, _pack_q8_append, _pack_q8_read, _pack_q8_attend = (_packer(c) for c in (_Q8Pages, _Q8Append, _Q8Read, _Q8Attend))
 _declared = False
 
 
@@ -74,6 +103,8 @@ def _lib():
                            ("wisv_cache_error", [P, P, C.POINTER(I)]),
                            ("wisv_cache_extend", [P, P, I, I, P, I, P, P]), ("wisv_cache_commit", [P, P, I, P, P, P]),
                            ("wisv_cache_append", [P, P, P]), ("wisv_cache_attend", [P, P, P]),
+                           ("wisv_cache_append_q8", [P, P, P, P]), ("wisv_cache_read_q8", [P, P, P, P]),
+                           ("wisv_cache_attend_q8", [P, P, P, P]),
                            ("wisv_debug_cache_waits", [P, C.c_uint64, I]),
                            ("wisv_verify_residual", [P, P])):
             f = getattr(lib, name)
@@ -118,6 +149,36 @@ class WindowLayout:
     slot_map: "object"
     positions: "object"
     status: "object"
+
+
+class QuantPages:
+    """One layer's pools of an 8-bit cache (wisv_q8_pages): codes ``k`` / ``v``, float8_e4m3fn of shape [n_pages, page_size, n_kv_heads,
+    head_dim] with any strides that are multiples of 16 and keep a head's codes contiguous, and scales ``k_scale`` / ``v_scale``, float32
+    [n_pages, page_size, n_kv_heads] with the tokens of a page and head side by side (a [n_pages, n_kv_heads, page_size] tensor, passed as
+    ``.transpose(1, 2)``).  A cached number is code * scale.  PagedCache.quant_pages makes them.
+    """
+
+    __slots__ = ("_tensors", "_shape", "_index", "_packed")
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        shape, index = k.shape, k.get_device()
+        if len(shape) != 4 or index < 0:
+            raise ValueError("codes must be 4-D CUDA tensors")
+        strides = []
+        for what, t in (("k", k), ("v", v)):
+            if t.dtype is not torch.float8_e4m3fn or t.shape != shape or t.get_device() != index or t.stride(3) != 1:
+                raise ValueError("%s must be float8_e4m3fn %s on cuda:%d with a head's codes contiguous" % (what, list(shape), index))
+            strides += [t.stride(i) if shape[i] > 1 else 0 for i in (0, 1, 2)]
+        for what, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if t.dtype is not torch.float32 or t.shape != shape[:3] or t.get_device() != index or (shape[1] > 1 and t.stride(1) != 1):
+                raise ValueError("%s must be float32 %s on cuda:%d with the tokens of a page and head side by side" %
+                                 (what, list(shape[:3]), index))
+            strides += [t.stride(i) if shape[i] > 1 else 0 for i in (0, 2)]
+        self._tensors, self._shape, self._index = (k, v, k_scale, v_scale), tuple(shape), index
+        self._packed = _pack_q8_pages(k.data_ptr(), v.data_ptr(), *strides[:6], k_scale.data_ptr(), v_scale.data_ptr(), *strides[6:])
+
+    k, v, k_scale, v_scale = (property(lambda self, i=i: self._tensors[i]) for i in range(4))
 
 
 def _owned_array(i):
@@ -309,6 +370,90 @@ class PagedCache:
                                 _array("kv_len", kv_len, i32, B, dev), table.data_ptr(), step, blocks, qp, qt, qh,
                                 kpool, vpool, k0, k1, k2, v0, v1, v2, op, ot, oh, 0 if lse is None else lse.data_ptr(),
                                 0.0 if scale is None else scale, made if clear_rest is None else bool(clear_rest)))
+        return out
+
+    # ------------------------------------------------------------------ the same in 8 bits
+    def quant_pages(self) -> QuantPages:
+        """Pools of one layer in 8 bits, all zero, each head's tokens of a page side by side."""
+        torch, (n, page, kv, d) = self._torch, self._pool
+
+        def codes():
+            return torch.zeros((n, kv, page, d), dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn).transpose(1, 2)
+
+        def scales():
+            return torch.zeros((n, kv, page), dtype=torch.float32, device=self.device).transpose(1, 2)
+        return QuantPages(codes(), codes(), scales(), scales())
+
+    def _q8(self, pages):
+        if pages._shape != self._pool or pages._index != self._index:
+            raise ValueError("pools must be [%d, %d, %d, %d] on %s" % (self._pool + (self.device,)))
+        return pages._packed
+
+    def _table(self, block_table, B):
+        """(address, row stride, entries of a row) of a block table, the cache's own where none is given."""
+        if block_table is None:
+            return self._owned[2].data_ptr(), self.max_blocks, self.max_blocks
+        t = block_table
+        if t.dtype is not self._torch.int32 or t.dim() != 2 or t.shape[0] < B or t.stride(1) != 1 or t.get_device() != self._index:
+            raise ValueError("block_table must be int32 [B, blocks] on %s" % self.device)
+        return t.data_ptr(), _row_stride(t), t.shape[1]
+
+    def append_q8(self, k, v, pages: QuantPages, slot_map, *, stream=None):
+        """wisv_cache_append_q8: one layer's new keys and values [T, n_kv_heads, head_dim], quantised into their slots."""
+        kp, kt, kh, T = self._rows("k", k, self.n_kv_heads)
+        vp, vt, vh, _ = self._rows("v", v, self.n_kv_heads, T)
+        self._call("wisv_cache_append_q8", stream, self._q8(pages),
+                   _pack_q8_append(T, kp, vp, kt, kh, vt, vh, _array("slot_map", slot_map, self._torch.int64, T, self._index)))
+
+    def read_q8(self, pages: QuantPages, *, B: int, n: Optional[int] = None, off=None, T: Optional[int] = None, start=None,
+                block_table=None, out=None, clear_rest: Optional[bool] = None, stream=None):
+        """wisv_cache_read_q8: tokens as rows (k, v) of [T, n_kv_heads, head_dim] in the cache's type: n tokens of each of B requests,
+        or off[b+1] - off[b] (int32 [B+1] on the device, with their sum T given), from token start[b] (int32 [B]; None: 0) on.
+        Rows that no request covers are zeros with clear_rest, which is the default where the rows are made here, and are left alone
+        in rows that are given (out = (k, v))."""
+        dev, i32, kv = self._index, self._torch.int32, self.n_kv_heads
+        if off is None:
+            if n is None:
+                raise ValueError("either n or off must be given")
+            if T is None:
+                T = B * n
+        elif T is None:
+            raise ValueError("T, the rows in all, must be given where off lives on the device")
+        made = out is None
+        if made:
+            both = _empty(self._torch, stream, (2, T, kv, self.head_dim), self.dtype, self.device)
+            out = tuple(both.unbind(0))
+        kp, kt, kh, _ = self._rows("out[0]", out[0], kv, T)
+        vp, vt, vh, _ = self._rows("out[1]", out[1], kv, T)
+        table, step, blocks = self._table(block_table, B)
+        self._call("wisv_cache_read_q8", stream, self._q8(pages),
+                   _pack_q8_read(B, T, 0 if n is None else n, 0 if off is None else _array("off", off, i32, B + 1, dev),
+                                 0 if start is None else _array("start", start, i32, B, dev), table, step, blocks,
+                                 made if clear_rest is None else bool(clear_rest), kp, vp, kt, kh, vt, vh))
+        return out
+
+    def attend_q8(self, q, pages: QuantPages, kv_len, *, B: int, max_new: int, q_off=None, out=None, lse=None,
+                  scale: Optional[float] = None, block_table=None, clear_rest: Optional[bool] = None, stream=None):
+        """wisv_cache_attend_q8: attend over 8-bit pools, with the arguments of attend."""
+        torch, dev, H, D = self._torch, self._index, self.n_heads, self.head_dim
+        qp, qt, qh, T = self._rows("q", q, H)
+        made = out is None
+        if made:
+            out = _empty(torch, stream, (T, H, D), self.dtype, self.device)
+            op, ot, oh = out.data_ptr(), H * D, D
+        else:
+            op, ot, oh, _ = self._rows("out", out, H, T)
+        if lse is not None and (lse.dtype is not torch.float32 or lse.shape != (T, H) or
+                                not lse.is_contiguous() or lse.get_device() != dev):
+            raise ValueError("lse must be a contiguous float32 [T, n_heads] tensor")
+        if scale is not None and not scale > 0:
+            raise ValueError("scale must be positive")
+        table, step, blocks = self._table(block_table, B)
+        self._call("wisv_cache_attend_q8", stream, self._q8(pages),
+                   _pack_q8_attend(B, T, max_new, 0 if q_off is None else _array("q_off", q_off, torch.int32, B + 1, dev),
+                                   _array("kv_len", kv_len, torch.int32, B, dev), table, step, blocks, qp, qt, qh, op, ot, oh,
+                                   0 if lse is None else lse.data_ptr(), 0.0 if scale is None else scale,
+                                   made if clear_rest is None else bool(clear_rest)))
         return out
 
     def device_error(self) -> int:
