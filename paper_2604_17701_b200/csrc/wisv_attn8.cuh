@@ -10,22 +10,23 @@
 //
 // 8-bit operands without a loss.  The codes are operands of the products as they are.  The other operand is cut into e4m3 parts: a number's
 // nearest e4m3 number, the nearest to what is left, and so on; each part takes 4 bits and the sign of the rest one more, so two parts carry
-// the 8 bits of a bf16 and three the 11 of an fp16 number, above a floor: with queries scaled by a power of two to a largest element in
-// [128, 256) and P to a largest value of 64 or more, what is lost is at most 2^-10 (2^-18 of a query row's largest
-// element, 2^-16 of a column's largest P).  The products are exact, sums are fp32.  (P is rounded to fp16 on the way, then to 9 bits where
-// queries are bf16: half the error of a bf16 P.)  The parts lie side by side as columns, [part][column], so that a tile of K or V is
-// read once for all of them.
+// the 8 bits of a bf16 and three the 11 of an fp16 number, above a floor.  Queries are scaled by a power of two to a largest element in
+// [128, 256); a last part's half step of 2^-10 is 2^-17 of a row's largest element at most.  Each further part of P is scaled up by 16 (its
+// sums are kept apart until the end), so that with a largest P of 4 or more the half step is 2^-16 of it, 2^-20 with three parts.  The
+// products are exact, sums are fp32.  (P is rounded to fp16 on the way, then to 9 bits where queries are bf16: half the error of a bf16 P.)  The
+// parts lie side by side as columns, [part][column], so that a tile of K or V is read once for all of them.
 //
 // References.  m grows only when a column's x passes 8.75 (P must stay below 448, the largest e4m3 number), then to the column's largest
-// minus 6; l and O are scaled with it.  One vote of the four warps a tile says whether any column has to.
+// minus 2; l and O are scaled with it.  One vote of a slot's warps per tile says whether any column has to.
 //
 // What does not reach a column.  Masked keys have x = -inf and P = 0 exactly.  V behind the last key of a request is cleared in shared memory,
 // since 0 times a code of NaN is NaN.  A scale of NaN (a token with infinite or NaN elements) makes x, and so the columns that see
-// the token, NaN.  Values with a scale of 0 (or below 2^-40 of the largest of the 32 keys around them) count as that small:
-// their l needs a b that can be divided by.
+// the token, NaN.  Values with a scale of 0 (or below 2^-40 of the largest of the tile) count as that small: their l needs a b that can be
+// divided by.
 //
-// Roles.  One block per SM, persistent: a warp that walks the work and copies keys, one that copies values, one that copies scales, one that
-// cuts queries, four that issue the MMAs (S and O of each slot), and two sets of four softmax warps ("slots"), a thread per key.  A
+// Roles.  One block per SM, persistent: a warp that walks the work and copies keys, one that copies values, one that copies scales and
+// prepares them, four that issue the MMAs (S and O of each slot), one that at most clears rows of no window, and two sets of eight
+// softmax warps ("slots"), a thread per key and half of the columns, which also cut the queries.  A
 // work item is "paired" - two tiles of columns of the same (request, key head), one per slot, sharing every tile of keys - or, where one
 // tile of columns is left, "split": the slots take the key tiles in turn and are put together at the end.  The line of key tiles, its cut
 // over the blocks and the joining of shared items are those of the 16-bit cache (wisv_attn.cuh).
@@ -39,10 +40,14 @@ namespace wisv {
 
 constexpr int kA8Cols = 64;                      // columns of a tile
 constexpr int kA8Stages = 12;                    // at most, of keys and of values
-constexpr int kA8Scales = 8;                     // tiles of scales in flight
+constexpr int kA8Scales = 6;                     // tiles of scales in flight
+constexpr int kA8ScaleBytes = 3 * 4 * kAttnTile; // of a tile: a, log2 b and 1 / b
 constexpr int kA8Small = 9 * 1024;               // barriers, queue, tables of columns
 constexpr int kA8Slack = 1024;
-constexpr float kA8Grow = 8.75f, kA8Room = 6.0f;
+constexpr int kA8SoftWarps = 16;                 // eight per slot
+constexpr int kA8Threads = 256 + 32 * kA8SoftWarps;
+constexpr float kA8Grow = 8.75f, kA8Room = 2.0f;
+constexpr float kA8Step = 16.0f;                 // from one part of P to the next
 
 struct Attn8Params : AttnParams {
     const void* q; int64_t qt, qh;               // in elements
@@ -55,12 +60,12 @@ struct Attn8Params : AttnParams {
 
 template <typename E> struct a8_parts { static constexpr int n = is_bf16<E>::value ? 2 : 3; };
 
-// TMEM: 256 columns a slot, S (at most 64 columns for each part) from the first, O behind it, with a column for each part where that fits:
-// V then is read once for all parts (a product whose operand has to be turned takes 73 clocks whatever its columns, 16 to 128).
-template <typename E> __host__ __device__ constexpr int a8_o_at() { return kA8Cols * a8_parts<E>::n; }
-template <typename E> __host__ __device__ constexpr bool a8_stacked(int cols) { return a8_parts<E>::n * cols <= 256 - a8_o_at<E>(); }
+// TMEM: 256 columns a slot, O behind S.  O has columns for each part, so that V is read once for all of them (a product whose operand has to be
+// turned takes 73 clocks whatever its columns, 16 to 64) and that the parts can have scales of their own; S too where that fits.
+template <typename E> __host__ __device__ constexpr int a8_o_at() { return 256 - kA8Cols * a8_parts<E>::n; }
+template <typename E> __host__ __device__ constexpr bool a8_s_stacked(int cols) { return a8_parts<E>::n * cols <= a8_o_at<E>(); }
 // bytes of a slot's P: 64 columns of 128 keys in a piece
-template <typename E> __host__ __device__ constexpr int a8_p_bytes(int cols) { return (a8_stacked<E>(cols) ? (a8_parts<E>::n * cols + 63) / 64 : a8_parts<E>::n) * 8192; }
+template <typename E> __host__ __device__ constexpr int a8_p_bytes(int cols) { return (a8_parts<E>::n * cols + 63) / 64 * 8192; }
 
 // D[tmem] (+)= A[smem] * B[smem], e4m3 operands
 __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -74,7 +79,7 @@ __device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t a_desc, uint64
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// kind::f8f6f4, e4m3 operands, fp32 accumulator; `mn`: both operands MN-major
+// kind::f8f6f4, e4m3 operands, fp32 sums; `mn`: both operands MN-major
 __device__ __forceinline__ uint32_t a8_idesc(uint32_t M, uint32_t N, bool mn)
 {
     return (1u << 4) | (mn ? 3u << 15 : 0u) | ((N >> 3) << 17) | ((M >> 4) << 24);
@@ -102,11 +107,6 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-// an arrival on `bar` when the thread's copies so far are done
-__device__ __forceinline__ void cp_async_arrive(uint32_t bar)
-{
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-}
 __device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 {
@@ -121,14 +121,21 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
                  : "r"(taddr)
                  : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
 __device__ __forceinline__ float warp_max_nan(float x)
 {
     float r;
     asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-// Two numbers below 448 in NP e4m3 parts each, largest first; codes in pairs, the first number in the low byte
-template <int NP>
+// Two numbers below 448 in NP e4m3 parts each, largest first, each further part 16 times what is left where `kScaled`; codes in pairs, the
+// first number in the low byte
+template <int NP, bool kScaled>
 __device__ __forceinline__ void a8_cut(float lo, float hi, uint32_t (&c)[NP])
 {
     uint32_t h;
@@ -142,8 +149,21 @@ __device__ __forceinline__ void a8_cut(float lo, float hi, uint32_t (&c)[NP])
             uint32_t back;
             asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(e));
             asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(h) : "r"(back));
+            if (kScaled) asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h) : "r"(0x4c004c00u));           // 16
         }
     }
+}
+
+template <typename E> __device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi);
+template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, float& lo, float& hi)
+{
+    lo = __uint_as_float(w << 16);
+    hi = __uint_as_float(w & 0xffff0000u);
+}
+template <> __device__ __forceinline__ void unpack2<__half>(uint32_t w, float& lo, float& hi)
+{
+    lo = __half2float(__ushort_as_half(static_cast<unsigned short>(w & 0xffffu)));
+    hi = __half2float(__ushort_as_half(static_cast<unsigned short>(w >> 16)));
 }
 
 template <typename E> __device__ __forceinline__ E a8_round(float x);
@@ -169,9 +189,8 @@ struct A8Ring {
 struct A8Small {
     uint64_t k_full[kA8Stages], k_empty[kA8Stages], v_full[kA8Stages], v_empty[kA8Stages];
     uint64_t sc_full[kA8Scales], sc_empty[kA8Scales];
-    uint64_t q_full[2], q_empty[2];              // query buffers
-    uint64_t s_full[2], s_free[2], p_full[2], pv_done[2], vote[2];          // slots
-    uint64_t seg_full[kSegQueue], seg_empty[kSegQueue], rs_full[kSegQueue];
+    uint64_t q_full[2], s_full[2], s_free[2], p_full[2], pv_done[2], vote[2];                        // slots
+    uint64_t seg_full[kSegQueue], seg_empty[kSegQueue];
     uint64_t o_full, o_empty, ml_full, fin_full, part_full, last_full, drain[4];
     uint32_t tmem;
     uint32_t abort[2];                           // [1] is for the waits after a time-out
@@ -179,13 +198,14 @@ struct A8Small {
     uint32_t limit[2];                           // three words behind either flag
     int32_t came_last;
     uint32_t half;
-    int32_t queue[kSegQueue][kSegWords];
-    float rs[kSegQueue][2][kA8Cols];             // c over a query column's power of two
-    float m[2][kA8Cols];                         // references
-    float a[2][kA8Cols];                         // factors when they grow; at the end those of a slot's own O
-    float b[2][kA8Cols];                         // at the end: of the other slot's O
-    float mx[2][4][kA8Cols];                     // maxima of the warps; at the end their l
-    int32_t grow[2][2][4];
+    alignas(16) int32_t queue[kSegQueue][kSegWords];
+    alignas(16) int32_t grow[2][2][8];
+    alignas(16) float rs[2][kA8Cols];            // c over a query column's power of two
+    alignas(16) float m[2][kA8Cols];             // references
+    alignas(16) float a[2][kA8Cols];             // factors when they grow; at the end those of a slot's own O
+    alignas(16) float b[2][kA8Cols];             // at the end: of the other slot's O
+    alignas(16) float mx[2][4][kA8Cols];         // maxima of the warps; at the end their l
+    int64_t at[2][kA8Cols];                      // at the end: where a column's output lies
 };
 static_assert(sizeof(A8Small) <= kA8Small, "shared memory");
 static_assert(offsetof(A8Small, limit) - offsetof(A8Small, abort) == 12, "attn_wait");
@@ -221,69 +241,62 @@ __device__ __forceinline__ bool a8_load_tiles(const Attn8Params& p, const CUtens
     return true;
 }
 
-// A tile of queries cut into parts, by one warp: D / 16 lanes to a row of 16 elements each.
+// Rows w, w + 8, ... of a tile of queries (in groups of 32 / (D / 16) rows), cut into parts by one warp: D / 16 lanes to a row of 16 elements
+// each.
 template <typename E, int D>
-__device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, int head, int rows, int cols, uint32_t dst, float* rs, int lane)
+__device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, int head, int rows, int cols, uint32_t dst, float* rs, int w, int lane)
 {
-    constexpr int NP = a8_parts<E>::n, L = D / 16, R = 32 / L;
+    constexpr int NP = a8_parts<E>::n, L = D / 16, R = 32 / L, U = 16 / R;           // U groups cover 64 columns in two rounds of 8 warps
     const int c = lane % L;
-    for (int r0 = 0; r0 < cols; r0 += 4 * R) {
-        uint4 w[4][2];
+    uint4 v[U / 2][2];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int r = r0 + u * R + lane / L;
-            w[u][0] = w[u][1] = make_uint4(0, 0, 0, 0);
-            if (r < rows) {
-                const int t = attn_token(p, r);
-                const uint4* src = reinterpret_cast<const uint4*>(static_cast<const E*>(p.q) + (row0 + t) * p.qt + (head * p.group + r - t * p.group) * p.qh) + 2 * c;
-                w[u][0] = src[0];
-                w[u][1] = src[1];
-            }
+    for (int u = 0; u < U / 2; ++u) {
+        const int r = (u * 8 + w) * R + lane / L;
+        v[u][0] = v[u][1] = make_uint4(0, 0, 0, 0);
+        if (r < rows) {
+            const int t = attn_token(p, r);
+            const uint4* src = reinterpret_cast<const uint4*>(static_cast<const E*>(p.q) + (row0 + t) * p.qt + (head * p.group + r - t * p.group) * p.qh) + 2 * c;
+            v[u][0] = src[0];
+            v[u][1] = src[1];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U / 2; ++u) {
+        const int r = (u * 8 + w) * R + lane / L;
+        if ((u * 8 + w) * R >= cols) break;                          // (the warp as one)
+        const uint32_t* d = reinterpret_cast<const uint32_t*>(v[u]);
+        float x[16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            unpack2<E>(d[i], x[2 * i], x[2 * i + 1]);
+            top = max(top, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int r = r0 + u * R + lane / L;
-            if (R == 8 && r0 + u * R >= cols) break;                                 // (16 columns: the warp as one)
-            const uint32_t* v = reinterpret_cast<const uint32_t*>(w[u]);
-            float x[16];
-            uint32_t top = 0;
+        for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool fine = top < 0x7f800000u;
+        const uint32_t e = max(top >> 23, 8u);                       // (0 and what is below 2^-119 are scaled alike)
+        const float up = __uint_as_float((261u - (fine ? e : 8u)) << 23);            // largest element to [128, 256)
+        uint32_t out[NP][4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (is_bf16<E>::value) {
-                    x[2 * i] = __uint_as_float(v[i] << 16);
-                    x[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
-                } else {
-                    x[2 * i] = __half2float(__ushort_as_half(static_cast<unsigned short>(v[i] & 0xffffu)));
-                    x[2 * i + 1] = __half2float(__ushort_as_half(static_cast<unsigned short>(v[i] >> 16)));
-                }
-                top = max(top, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
-            }
+        for (int i = 0; i < 4; ++i) {
+            uint32_t f[NP], g[NP];
+            a8_cut<NP, false>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, f);
+            a8_cut<NP, false>(fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, g);
 #pragma unroll
-            for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const bool fine = top < 0x7f800000u;
-            const uint32_t e = max(top >> 23, 8u);                                   // (0 and what is below 2^-119 are scaled alike)
-            const float up = fine ? __uint_as_float((261u - e) << 23) : 0.0f;        // largest element to [128, 256)
-            uint32_t out[NP][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t a[NP], b[NP];
-                a8_cut<NP>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, a);
-                a8_cut<NP>(fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, b);
-#pragma unroll
-                for (int q = 0; q < NP; ++q) out[q][i] = a[q] | b[q] << 16;
-            }
-#pragma unroll
-            for (int q = 0; q < NP; ++q) {
-                const int row = q * cols + r;
-                const uint32_t at = dst + row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][2]), "r"(out[q][3]) : "memory");
-            }
-            if (c == 0) rs[r] = r >= rows ? 0.0f : fine ? p.scale_log2 * __uint_as_float((e - 7u) << 23) : CUDART_NAN_F;
+            for (int q = 0; q < NP; ++q) out[q][i] = f[q] | g[q] << 16;
         }
+#pragma unroll
+        for (int q = 0; q < NP; ++q) {
+            const int row = q * cols + r;
+            const uint32_t at = dst + row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][2]), "r"(out[q][3]) : "memory");
+        }
+        if (c == 0) rs[r] = r >= rows ? 0.0f : fine ? p.scale_log2 * __uint_as_float((e - 7u) << 23) : CUDART_NAN_F;
     }
 }
 
-// The merge of an item's partials by the eight softmax warps of the block that came last: a warp takes a column at a time, its lanes
+// The merge of an item's partials by the softmax warps of the block that came last: a warp takes a column at a time, its lanes
 // the D elements; four partials are loaded together and added in block order.  Reads go past L1, which other blocks'
 // writes do not reach.
 template <typename E, int D>
@@ -293,7 +306,7 @@ __device__ __forceinline__ void a8_merge(const Attn8Params& p, const int* sg, in
     const int parts = __shfl_sync(0xffffffffu, sg[kSegParts], 0);
     const int rows0 = __shfl_sync(0xffffffffu, sg[kSegRows0], 0), rows = rows0 + __shfl_sync(0xffffffffu, sg[kSegRows1], 0);
     const int first = sg[kSegFirst];
-    for (int r = w; r < rows; r += 8) {
+    for (int r = w; r < rows; r += kA8SoftWarps) {
         const bool second = r >= rows0;
         const int in = second ? r - rows0 : r, at = in + (second ? kA8Cols : 0);
         float m = -CUDART_INF_F, l = 0.0f, acc[V];
@@ -345,46 +358,221 @@ __device__ __forceinline__ void a8_merge(const Attn8Params& p, const int* sg, in
     }
 }
 
-// columns of the tiles of an item with so many rows in its larger tile
-__device__ __forceinline__ int a8_cols(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : kA8Cols; }
+// columns that a tile of so many rows is computed with
+__host__ __device__ __forceinline__ int a8_cols(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 ? 48 : kA8Cols; }
+
+constexpr float kA8None = -3.402823466e38f;      // the reference of a column that has seen no key
+
+// ---- the work: as in the 16-bit kernel, with tiles of paired items weighing two units, since their two slots have a product each
+__device__ __forceinline__ int a8_weight(const Attn8Params& p, const AttnReq& r, int it) { return r.n - it * 2 * p.tpt > p.tpt ? 2 : 1; }
+__device__ __forceinline__ unsigned a8_units(const Attn8Params& p, const AttnReq& r, int it)
+{
+    return a8_weight(p, r, it) * attn_tiles(p, r, it) + kAttnItemCost;
+}
+
+struct A8Walk {
+    int b, kvh, it, pos, units;                  // position on the line of units, and what is left of the range
+    AttnReq r;
+    // The next stretch; false at the end of the range.  A tile belongs to the range that its first unit lies in.
+    __device__ __forceinline__ bool next(const Attn8Params& p, int (&s)[kSegWords + 1])
+    {
+        while (units > 0) {
+            if (it >= r.items) {                 // (a request without rows)
+                if (++b >= p.B) return false;
+                kvh = it = pos = 0;
+                r = attn_request(p, b);
+                continue;
+            }
+            const int nt = attn_tiles(p, r, it), wt = a8_weight(p, r, it), all = wt * nt + kAttnItemCost;
+            const int take = min(units, all - pos);
+            const int t0 = min(nt, (pos + wt - 1) / wt), t1 = min(nt, (pos + take + wt - 1) / wt);
+            if (t1 > t0) {
+                const int tok0 = it * 2 * p.tpt, left = r.n - tok0;
+                s[kSegJobs] = t1 - t0;
+                s[kSegPaired] = wt == 2; s[kSegT0] = t0; s[kSegT1] = t1; s[kSegTiles] = nt;
+                s[kSegKeys] = r.kv; s[kSegLimit] = r.kv - r.n + tok0;
+                s[kSegRow] = r.q0 + tok0; s[kSegHead] = kvh; s[kSegReq] = b;
+                s[kSegLeft] = units + pos;       // (from the item's first unit to the end of the range)
+                s[kSegRows0] = min(left, p.tpt) * p.group;
+                s[kSegRows1] = wt == 2 ? min(left - p.tpt, p.tpt) * p.group : 0;
+            }
+            units -= take;
+            pos += take;
+            if (pos == all) {
+                pos = 0;
+                if (++it == r.items) {
+                    it = 0;
+                    if (++kvh == p.n_kv) {
+                        kvh = 0;
+                        if (++b < p.B) r = attn_request(p, b);
+                        else units = 0;
+                    }
+                }
+            }
+            if (t1 > t0) return true;
+        }
+        return false;
+    }
+};
+
+// This block's range of the line of units, found by one warp (see attn_range).
+__device__ __forceinline__ void a8_range(const Attn8Params& p, unsigned me, int lane, A8Walk& w, unsigned& share, unsigned& more)
+{
+    const int per = (p.B + 31) >> 5, b0 = min(lane * per, p.B), b1 = min(b0 + per, p.B);
+    auto units_of = [&](const AttnReq& r) {
+        unsigned u = 0;
+        for (int i = 0; i < r.items; ++i) u += a8_units(p, r, i);
+        return u;
+    };
+    unsigned long long sum = 0;
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b) sum += static_cast<unsigned long long>(units_of(attn_request(p, b))) * p.n_kv;
+    const unsigned mine = static_cast<unsigned>(sum);
+    const unsigned high = __reduce_add_sync(0xffffffffu, static_cast<unsigned>(min(sum >> 16, 1ull << 20)));
+    unsigned upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned x = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += x;
+    }
+    unsigned total = __shfl_sync(0xffffffffu, upto, 31);
+    if (high >= 0x7fffu) {
+        total = upto = 0;
+        if (lane == 0) atomicOr(p.err, 4);
+    }
+    const unsigned blocks = min(gridDim.x, max(total / kAttnMinUnits, 1u));
+    share = total / blocks;
+    more = total - share * blocks;
+    const unsigned lo = me * share + min(me, more);
+    w.b = w.kvh = w.it = w.pos = w.units = 0;
+    const bool mine_starts = me < blocks && lo < upto && lo >= upto - mine;          // one lane's requests hold the start
+    if (mine_starts) {
+        unsigned x = lo - (upto - mine);
+        for (int b = b0; b < b1; ++b) {
+            const AttnReq r = attn_request(p, b);
+            const unsigned one = units_of(r);
+            if (x >= one * p.n_kv) { x -= one * p.n_kv; continue; }
+            const unsigned h = x / one;
+            x -= h * one;
+            int it = 0;
+            for (; ; ++it) {
+                const unsigned u = a8_units(p, r, it);
+                if (x < u) break;
+                x -= u;
+            }
+            w.b = b; w.kvh = h; w.it = it; w.pos = x;
+            break;
+        }
+    }
+    const unsigned who = __ballot_sync(0xffffffffu, mine_starts);
+    const int src = who ? __ffs(who) - 1 : 0;
+    w.b = __shfl_sync(0xffffffffu, w.b, src);
+    w.kvh = __shfl_sync(0xffffffffu, w.kvh, src);
+    w.it = __shfl_sync(0xffffffffu, w.it, src);
+    w.pos = __shfl_sync(0xffffffffu, w.pos, src);
+    w.units = who ? share + (me < more ? 1 : 0) : 0;
+    if (who) w.r = attn_request(p, w.b);
+}
+
+// The scales of key tiles t0 .. t1 - 1 into their ring, by one warp, four tokens to a lane: copied four tiles ahead, then turned in place into
+// a, log2 b and 1 / b.  A lane works on what it has copied itself.
+__device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int head, int t0, int t1, int keys, uint32_t ring, A8Small* sm, uint32_t flag,
+                                          int lane, A8Ring& at, A8Ring& done)
+{
+    constexpr int kAhead = 4;
+    const int mask = (1 << p.page_shift) - 1;
+    auto page = [&](int t) {
+        const int tok = t * kAttnTile + 4 * lane;
+        return t < t1 && tok < keys ? p.block_table[req * p.table_stride + (tok >> p.page_shift)] : -1;
+    };
+    int pg = page(t0);
+    for (int t = t0; t < t1 + kAhead; ++t) {
+        if (t < t1) {
+            const bool in = pg >= 0 && pg < p.n_pages;
+            const int o = in ? (t * kAttnTile + 4 * lane) & mask : 0, from = in ? pg : 0;
+            pg = page(t + 1);
+            if (!attn_wait_warp(smem_u32(&sm->sc_empty[at.s]), at.ph ^ 1u, flag)) return false;
+            const uint32_t dst = ring + at.s * kA8ScaleBytes + lane * 16;
+            cp_async16(dst, p.ks + from * p.ksp + head * p.ksh + o, in ? 16 : 0);
+            cp_async16(dst + 512, p.vs + from * p.vsp + head * p.vsh + o, in ? 16 : 0);
+            at.step(kA8Scales, 1);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (t < t0 + kAhead) continue;
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+        const uint32_t src = ring + done.s * kA8ScaleBytes + lane * 16;
+        float a[4], b[4], lb[4];
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]) : "r"(src) : "memory");
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]) : "r"(src + 512) : "memory");
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if ((t - kAhead) * kAttnTile + 4 * lane + i >= keys) a[i] = b[i] = 0.0f;                // (behind the last key: anything)
+            if (b[i] > 0.0f && b[i] < CUDART_INF_F) top = max(top, __float_as_uint(b[i]));
+        }
+        const float least = fmaxf(__uint_as_float(__reduce_max_sync(0xffffffffu, top)) * 9.094947e-13f, 7.888609e-31f);          // 2^-40 of the largest, 2^-100
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float be = fmaxf(b[i], least);
+            lb[i] = b[i] == b[i] ? attn_lg2(be) : CUDART_NAN_F;
+            b[i] = attn_rcp(be);
+        }
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(src), "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]) : "memory");
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(src + 512), "f"(lb[0]), "f"(lb[1]), "f"(lb[2]), "f"(lb[3]) : "memory");
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(src + 1024), "f"(b[0]), "f"(b[1]), "f"(b[2]), "f"(b[3]) : "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sm->sc_full[done.s]));
+        done.step(kA8Scales, 1);
+    }
+    return true;
+}
 
 // What a softmax warp carries from stretch to stretch
 struct A8Soft {
-    int slot, quad, lane, row;                   // row: of the tile of keys
-    uint32_t lane_off, tmem, p_smem, ring_v, ring_sc, flag;
+    int slot, half, quad, lane, row;             // half: of the columns; row: of the tile of keys
+    uint32_t lane_off, tmem, q_smem, p_smem, ring_v, ring_sc, flag;
     uint32_t jobs = 0, votes = 0;                // of this slot so far
     uint32_t tiles = 0;                          // of the block so far
     A8Ring v, sc;                                // the place of tile number `tiles`
 };
 
-constexpr float kA8None = -3.402823466e38f;      // the reference of a column that has seen no key
+// 8 or 16 columns of TMEM, and 8 or 16 bytes of an operand
+template <int W> __device__ __forceinline__ void a8_tmem_ld(uint32_t at, uint32_t (&r)[W]);
+template <> __device__ __forceinline__ void a8_tmem_ld<8>(uint32_t at, uint32_t (&r)[8]) { tmem_ld8(at, r); }
+template <> __device__ __forceinline__ void a8_tmem_ld<16>(uint32_t at, uint32_t (&r)[16]) { tmem_ld16(at, r); }
 
-// A stretch of an item's tiles with at most 16 NC columns, up to and including its outputs or partials.  false: a wait ran out.
-template <typename E, int D, int NC>
-__device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8Soft& w, const int* sg, int qi, uint32_t item)
+// A stretch of an item's tiles with at most 2 C columns, up to and including its outputs or partials.  false: a wait ran out.
+template <typename E, int D, int C>
+__device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8Soft& w, const int* sg, uint32_t item)
 {
-    constexpr int NP = a8_parts<E>::n, N = 16 * NC;
-    constexpr bool kStacked = a8_stacked<E>(N);                      // O has a column per part
-    constexpr int kOAt = a8_o_at<E>(), kOParts = kStacked ? NP : 1;
-    const int slot = w.slot;
+    constexpr int NP = a8_parts<E>::n, N = 2 * C, W = C % 16 ? 8 : 16;               // W: columns at a time
+    constexpr int kSParts = a8_s_stacked<E>(N) ? NP : 1;
+    const int slot = w.slot, col0 = w.half * C, ts = w.half * 128 + w.row;
     const bool paired = sg[kSegPaired];
     const int nt = sg[kSegT1] - sg[kSegT0], keys = sg[kSegKeys];
     const int limit = sg[kSegLimit] + (paired && slot ? p.tpt : 0);  // last key that the tile's first token sees
-    const uint32_t aS = w.tmem + static_cast<uint32_t>(slot) * 256 + w.lane_off, aO = aS + kOAt;
-    const float* const rs = sm->rs[qi][paired ? slot : 0];
+    const int rows = paired && slot ? sg[kSegRows1] : sg[kSegRows0];
+    const int tok0 = sg[kSegRow] + (paired && slot ? p.tpt : 0);
+    const uint32_t aS = w.tmem + static_cast<uint32_t>(slot) * 256 + w.lane_off, aO = aS + a8_o_at<E>();
+    const float* const rs = sm->rs[slot] + col0;
     float* const m = sm->m[slot];
-    auto vote = [&]() {                                              // the slot's four warps meet
+    auto vote = [&]() {                                              // the slot's warps meet
         __syncwarp();
         if (w.lane == 0) mbar_arrive(smem_u32(&sm->vote[slot]));
         const bool ok = attn_wait_warp(smem_u32(&sm->vote[slot]), w.votes & 1u, w.flag);
         ++w.votes;
         return ok;
     };
-    if (w.row < N) m[w.row] = kA8None;
-    if (!attn_wait_warp(smem_u32(&sm->rs_full[qi]), static_cast<uint32_t>(item / kSegQueue) & 1u, w.flag)) return false;
-    uint64_t l[N / 2];
+    // ---- queries (the products that read the last ones are complete: their S has been waited for)
+    a8_cut_queries<E, D>(p, tok0, sg[kSegHead], rows, N, w.q_smem, sm->rs[slot], w.half * 4 + w.quad, w.lane);
+    fence_proxy_async();
+    __syncwarp();
+    if (w.lane == 0) mbar_arrive(smem_u32(&sm->q_full[slot]));
+    if (ts < N) m[ts] = kA8None;
+    if (!vote()) return false;
+    uint64_t l[C / 2];
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) l[i] = 0;
+    for (int i = 0; i < C / 2; ++i) l[i] = 0;
 
     const int i0 = paired ? 0 : static_cast<int>((w.tiles ^ static_cast<uint32_t>(slot)) & 1u), step = paired ? 1 : 2;
     A8Ring rv = w.v, rsc = w.sc;
@@ -393,54 +581,41 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         const int key0 = (sg[kSegT0] + i) * kAttnTile, key = key0 + w.row;
         // ---- the scales of this thread's key
         if (!attn_wait_warp(smem_u32(&sm->sc_full[rsc.s]), rsc.ph, w.flag)) return false;
-        float ka, vb;
+        float ka, lb, rb;
         {
-            const uint32_t at = w.ring_sc + rsc.s * 1024 + w.row * 4;
+            const uint32_t at = w.ring_sc + rsc.s * kA8ScaleBytes + w.row * 4;
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ka) : "r"(at) : "memory");
-            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vb) : "r"(at + 512) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lb) : "r"(at + 512) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rb) : "r"(at + 1024) : "memory");
         }
-        __syncwarp();
-        if (w.lane == 0) {
-            mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
-            if (!paired) mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
-        }
-        rsc.step(kA8Scales, step);
-        if (key >= keys) { ka = 0.0f; vb = 0.0f; }
-        const uint32_t top = __reduce_max_sync(0xffffffffu, vb > 0.0f && vb < CUDART_INF_F ? __float_as_uint(vb) : 0u);
-        const float be = fmaxf(vb, fmaxf(__uint_as_float(top) * 9.094947e-13f, 7.888609e-31f));     // 2^-40 of the largest, 2^-100
-        const float lb = vb == vb ? attn_lg2(be) : CUDART_NAN_F, rb = attn_rcp(be);
-        const uint64_t ka2 = pair(ka, ka), lb2 = pair(lb, lb), rb2 = pair(rb, rb);
+        const uint64_t ka2 = pair(ka, ka), lb2 = pair(lb, lb);
         // columns from `vis` on see this key
         const bool masked = key0 + kAttnTile - 1 > limit;
-        const int vis = key >= keys ? 1 << 20 : min(max(key - limit, 0), kA8Cols + 1) * p.group;
+        const int vis = (key >= keys ? 1 << 20 : min(max(key - limit, 0), kA8Cols + 1) * p.group) - col0;
 
         if (!attn_wait_warp(smem_u32(&sm->s_full[slot]), w.jobs & 1u, w.flag)) return false;
         tc_fence_after();
-        float x[N];
+        float x[C];
         // Pass 0 finds x with the references as they are; where a column outgrows its own, pass 1 finds x + m for its maximum and pass 2 x
         // with the new references.  (The first tile of a stretch has none yet.)
         for (int pass = i == i0 ? 1 : 0; ; ++pass) {
-            constexpr int W = N < 32 ? N : 32;
             const float neg = pass == 1 ? 0.0f : -1.0f;
             const uint64_t neg2 = pair(neg, neg);
 #pragma unroll
-            for (int c = 0; c < N; c += W) {
-                uint32_t s[NP][W];
+            for (int c = 0; c < C; c += W) {
+                uint32_t s[kSParts][W];
 #pragma unroll
-                for (int q = 0; q < NP; ++q) {
-                    if (W == 32) tmem_ld32(aS + q * N + c, s[q]);
-                    else tmem_ld16(aS + q * N + c, *reinterpret_cast<uint32_t (*)[16]>(s[q]));
-                }
+                for (int q = 0; q < kSParts; ++q) a8_tmem_ld<W>(aS + q * N + col0 + c, s[q]);
                 tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < W; j += 4) {
-                    const float4 r4 = *reinterpret_cast<const float4*>(rs + c + j), m4 = *reinterpret_cast<const float4*>(m + c + j);
+                    const float4 r4 = *reinterpret_cast<const float4*>(rs + c + j), m4 = *reinterpret_cast<const float4*>(m + col0 + c + j);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int k = j + 2 * h;
                         uint64_t v = pair(__uint_as_float(s[0][k]), __uint_as_float(s[0][k + 1]));
 #pragma unroll
-                        for (int q = 1; q < NP; ++q) v = add2(v, pair(__uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1])));
+                        for (int q = 1; q < kSParts; ++q) v = add2(v, pair(__uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1])));
                         v = fma2(mul2(v, h ? pair(r4.z, r4.w) : pair(r4.x, r4.y)), ka2, lb2);
                         v = fma2(h ? pair(m4.z, m4.w) : pair(m4.x, m4.y), neg2, v);
                         x[c + k] = low(v);
@@ -450,65 +625,71 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             }
             if (masked) {
 #pragma unroll
-                for (int n = 0; n < N; ++n) x[n] = n >= vis ? x[n] : -CUDART_INF_F;
+                for (int n = 0; n < C; ++n) x[n] = n >= vis ? x[n] : -CUDART_INF_F;
             }
             if (pass == 2) break;
             if (pass == 0) {
                 float worst[2] = {-CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
-                for (int n = 0; n < N; n += 4) {
+                for (int n = 0; n < C; n += 4) {
                     worst[0] = max3_nan(worst[0], x[n], x[n + 1]);
                     worst[1] = max3_nan(worst[1], x[n + 2], x[n + 3]);
                 }
                 const bool mine = __any_sync(0xffffffffu, !(worst[0] <= kA8Grow && worst[1] <= kA8Grow));
                 volatile int32_t* const grow = sm->grow[slot][w.votes & 1u];
-                if (w.lane == 0) grow[w.quad] = mine;
+                if (w.lane == 0) grow[w.half * 4 + w.quad] = mine;
                 if (!vote()) return false;
-                if (!(grow[0] | grow[1] | grow[2] | grow[3])) break;
+                if (!__any_sync(0xffffffffu, grow[w.lane & 7] != 0)) break;
                 continue;
             }
             // ---- the references grow
+            float keep = 0.0f;
 #pragma unroll
-            for (int c = 0; c < N; c += W) {
-                float keep = 0.0f;
-#pragma unroll
-                for (int n = 0; n < W; ++n) {
-                    const float r = warp_max_nan(x[c + n]);
-                    if (n == w.lane) keep = r;
-                }
-                if (w.lane < W) sm->mx[slot][w.quad][c + w.lane] = keep;
+            for (int n = 0; n < C; ++n) {
+                const float r = warp_max_nan(x[n]);
+                if (n == w.lane) keep = r;
             }
+            if (w.lane < C) sm->mx[slot][w.quad][col0 + w.lane] = keep;
             if (!vote()) return false;
-            if (w.row < N) {
+            if (ts < N) {
                 const float (&mx)[4][kA8Cols] = sm->mx[slot];
-                const float big = max3_nan(max3_nan(mx[0][w.row], mx[1][w.row], mx[2][w.row]), mx[3][w.row], mx[3][w.row]);
-                const float old = m[w.row];
+                const float big = max3_nan(max3_nan(mx[0][ts], mx[1][ts], mx[2][ts]), mx[3][ts], mx[3][ts]);
+                const float old = m[ts];
                 const bool grows = !(big - old <= kA8Grow), bad = !(big < CUDART_INF_F);             // (a score of NaN or +inf)
                 const float now = !grows ? old : !bad ? big - kA8Room : old == kA8None ? 0.0f : old;
-                sm->a[slot][w.row] = !grows ? 1.0f : bad ? CUDART_NAN_F : attn_ex2(old - now);
-                m[w.row] = now;
+                sm->a[slot][ts] = !grows ? 1.0f : bad ? CUDART_NAN_F : attn_ex2(old - now);
+                m[ts] = now;
             }
             if (!vote()) return false;
+            const float* const a = sm->a[slot];
             if (i != i0) {
                 if (!attn_wait_warp(smem_u32(&sm->pv_done[slot]), (w.jobs - 1) & 1u, w.flag)) return false;
                 tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < kOParts * N; c += 16) {
-                    uint32_t o[16];
-                    tmem_ld16(aO + c, o);
-                    tmem_wait_ld();
+                for (int q = 0; q < NP; ++q) {
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * sm->a[slot][c % N + j]);
-                    tmem_st16(aO + c, o);
+                    for (int c = 0; c < C; c += 8) {
+                        uint32_t o[8];
+                        tmem_ld8(aO + q * N + col0 + c, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) o[j] = __float_as_uint(__uint_as_float(o[j]) * a[col0 + c + j]);
+                        tmem_st8(aO + q * N + col0 + c, o);
+                    }
                 }
                 tmem_wait_st();
             }
 #pragma unroll
-            for (int n = 0; n < N; n += 2) l[n / 2] = mul2(l[n / 2], pair(sm->a[slot][n], sm->a[slot][n + 1]));
+            for (int n = 0; n < C; n += 2) l[n / 2] = mul2(l[n / 2], pair(a[col0 + n], a[col0 + n + 1]));
         }
         tc_fence_before();
         __syncwarp();
-        if (w.lane == 0) mbar_arrive(smem_u32(&sm->s_free[slot]));
+        if (w.lane == 0) {
+            mbar_arrive(smem_u32(&sm->s_free[slot]));
+            mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
+            if (!paired) mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
+        }
+        rsc.step(kA8Scales, step);
 
         // ---- P, once the product before has read the last one
         if (w.jobs) {
@@ -518,33 +699,37 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             // (both slots of a paired item clear: whoever comes second writes zeros over zeros)
             if (!attn_wait_warp(smem_u32(&sm->v_full[rv.s]), rv.ph, w.flag)) return false;
             if (key >= keys) {
-                const uint32_t at = w.ring_v + rv.s * a8_tile_bytes<D>() + w.row * D;
+                const uint32_t at = w.ring_v + rv.s * a8_tile_bytes<D>() + w.row * D + w.half * (D / 2);
 #pragma unroll
-                for (int c = 0; c < D; c += 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + c), "r"(0) : "memory");
+                for (int c = 0; c < D / 2; c += 16) asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + c), "r"(0) : "memory");
             }
         }
         rv.step(p.v_stages, step);
+        const uint64_t rb2 = pair(rb, rb);
 #pragma unroll
-        for (int c = 0; c < N; c += 16) {
-            uint32_t out[NP][4];
+        for (int c = 0; c < C; c += W) {
+            uint32_t out[NP][W / 4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < W / 4; ++j) {
                 uint32_t e[2][NP];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int n = c + 4 * j + 2 * h;
                     const float e0 = attn_ex2(x[n]), e1 = attn_ex2(x[n + 1]);
                     l[n / 2] = fma2(pair(e0, e1), rb2, l[n / 2]);
-                    a8_cut<NP>(e0, e1, e[h]);
+                    a8_cut<NP, true>(e0, e1, e[h]);
                 }
 #pragma unroll
                 for (int q = 0; q < NP; ++q) out[q][j] = e[0][q] | e[1][q] << 16;
             }
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
-                const int n = q * (kStacked ? N : kA8Cols) + c;      // column of the operand; rows of 64 bytes, swizzled
-                const uint32_t at = w.p_smem + (n >> 6) * 8192 + w.row * 64 + ((((n >> 4) & 3) ^ ((w.row >> 1) & 3)) << 4);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][2]), "r"(out[q][3]) : "memory");
+                const int n = q * N + col0 + c;                      // column of the operand; rows of 64 bytes, swizzled
+                const uint32_t at = w.p_smem + (n >> 6) * 8192 + w.row * 64 + ((((n >> 4) & 3) ^ ((w.row >> 1) & 3)) << 4) + (n & 8);
+                if (W == 16)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][W / 4 - 2]), "r"(out[q][W / 4 - 1]) : "memory");
+                else
+                    asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]) : "memory");
             }
         }
         fence_proxy_async();
@@ -554,48 +739,48 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         ++w.jobs;
     }
 
-    // ---- sums over the keys: lanes first (a lane ends with N / 32 columns, or two lanes with one), then warps, then slots
-    if (!attn_wait_warp(smem_u32(&sm->o_full), item & 1u, w.flag)) return false;
-    tc_fence_after();
+    // ---- sums over the keys: lanes first (a lane, or several, end with one column), then warps, then slots
     {
-        float v[N];
+        float v[C];
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i) { v[2 * i] = low(l[i]); v[2 * i + 1] = high(l[i]); }
-        int len = N;
+        for (int i = 0; i < C / 2; ++i) { v[2 * i] = low(l[i]); v[2 * i + 1] = high(l[i]); }
+        // halve the columns that a lane keeps while they are even in number; what is left (1, or 3 of 24) is added over the other lanes
+        int len = C;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
-            if (len > 1) {
+            if (len % 2 == 0) {
                 len >>= 1;
                 const bool up = (w.lane & o) != 0;
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) {
+                for (int i = 0; i < C / 2; ++i) {
                     if (i < len) {
                         const float keep = up ? v[i + len] : v[i], send = up ? v[i] : v[i + len];
                         v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
                     }
                 }
             } else {
-                v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    if (i < len) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+                }
             }
         }
-        float* const mine = sm->mx[slot][w.quad];
-        if (NC == 4) { mine[2 * w.lane] = v[0]; mine[2 * w.lane + 1] = v[1]; }
-        else if (NC == 2) mine[w.lane] = v[0];
-        else if ((w.lane & 1) == 0) mine[w.lane >> 1] = v[0];
+        constexpr int kLeft = C == 24 ? 3 : 1, kLanes = 32 * kLeft / C;              // columns a lane ends with, lanes that share them
+        if (w.lane % kLanes == 0) {
+#pragma unroll
+            for (int i = 0; i < kLeft; ++i) sm->mx[slot][w.quad][col0 + w.lane / kLanes * kLeft + i] = v[i];
+        }
     }
     __syncwarp();
     if (w.lane == 0) mbar_arrive(smem_u32(&sm->ml_full));
     if (!attn_wait_warp(smem_u32(&sm->ml_full), item & 1u, w.flag)) return false;
-    const int rows = paired && slot ? sg[kSegRows1] : sg[kSegRows0];
     const bool first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
     const int part = static_cast<int>(blockIdx.x) * 2 + (first ? 1 : 0), part_row = paired ? slot * kA8Cols : 0;
-    const int tok0 = sg[kSegRow] + (paired && slot ? p.tpt : 0), head0 = sg[kSegHead] * p.group;
-    if (w.row < N) {
-        const int n = w.row;
-        auto sum = [&](int s) { return (sm->mx[s][0][n] + sm->mx[s][1][n]) + (sm->mx[s][2][n] + sm->mx[s][3][n]); };
-        float mm = m[n], ll = sum(slot), wa = 1.0f, wb = 0.0f;
+    if (ts < N) {
+        auto sum = [&](int s) { return (sm->mx[s][0][ts] + sm->mx[s][1][ts]) + (sm->mx[s][2][ts] + sm->mx[s][3][ts]); };
+        float mm = m[ts], ll = sum(slot), wa = 1.0f, wb = 0.0f;
         if (!paired) {
-            const float other = sm->m[slot ^ 1][n], top = fmaxf(mm, other);
+            const float other = sm->m[slot ^ 1][ts], top = fmaxf(mm, other);
             wa = mm == kA8None ? 0.0f : attn_ex2(mm - top);
             wb = other == kA8None ? 0.0f : attn_ex2(other - top);
             ll = ll * wa + sum(slot ^ 1) * wb;
@@ -607,56 +792,52 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             wa *= inv;
             wb *= inv;
         }
-        sm->a[slot][n] = wa;
-        sm->b[slot][n] = wb;
-        if (n < rows && (paired || slot == 0)) {
-            if (!whole) p.part_ml[part * (2 * kA8Cols) + part_row + n] = make_float2(mm, ll);
-            else if (p.lse) {
-                const int t = attn_token(p, n);
-                p.lse[static_cast<int64_t>(tok0 + t) * (p.n_kv * p.group) + head0 + n - t * p.group] =
-                    ll == 0.0f ? -CUDART_INF_F : (mm + attn_lg2(ll)) * 0.6931471805599453f;
-            }
+        sm->a[slot][ts] = wa;
+        sm->b[slot][ts] = wb;
+        const int t = attn_token(p, ts), head = sg[kSegHead] * p.group + ts - t * p.group;
+        sm->at[slot][ts] = (tok0 + t) * p.ot + head * p.oh;
+        if (ts < rows && (paired || slot == 0)) {
+            if (!whole) p.part_ml[part * (2 * kA8Cols) + part_row + ts] = make_float2(mm, ll);
+            else if (p.lse)
+                p.lse[static_cast<int64_t>(tok0 + t) * (p.n_kv * p.group) + head] = ll == 0.0f ? -CUDART_INF_F : (mm + attn_lg2(ll)) * 0.6931471805599453f;
         }
     }
     __syncwarp();
     if (w.lane == 0) mbar_arrive(smem_u32(&sm->fin_full));
     if (!attn_wait_warp(smem_u32(&sm->fin_full), item & 1u, w.flag)) return false;
+    if (!attn_wait_warp(smem_u32(&sm->o_full), item & 1u, w.flag)) return false;
+    tc_fence_after();
 
     // ---- outputs: a thread has one element of every column; split: each slot does half of the columns, from both accumulators
     const int d = D == 128 ? w.row : w.quad * 16 + w.lane;
     const bool has = D == 128 || w.lane < 16;
     const uint32_t other = slot ? aO - 256 : aO + 256;
-    const int c0 = paired ? 0 : slot * (N / 2), c1 = min(paired ? N : c0 + N / 2, rows);
-    for (int c = c0; c < c1; c += 8) {
+    // chunks of 8 columns, dealt out to the warps that share the lanes: two in a paired item, the four of both slots in a split one
+    for (int c = 8 * (paired ? w.half : 2 * slot + w.half); c < rows; c += paired ? 16 : 32) {
         float y[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = 0.0f;
 #pragma unroll
         for (int side = 0; side < 2; ++side) {
             if (side && paired) break;
-            uint32_t o[kOParts][8];
+            uint32_t o[NP][8];
 #pragma unroll
-            for (int q = 0; q < kOParts; ++q) tmem_ld8((side ? other : aO) + q * N + c, o[q]);
+            for (int q = 0; q < NP; ++q) tmem_ld8((side ? other : aO) + q * N + c, o[q]);
             tmem_wait_ld();
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const float f = side ? sm->b[slot][c + j] : sm->a[slot][c + j];
-                float v = __uint_as_float(o[0][j]);
+                float v = __uint_as_float(o[NP - 1][j]);
 #pragma unroll
-                for (int q = 1; q < kOParts; ++q) v += __uint_as_float(o[q][j]);
+                for (int q = NP - 2; q >= 0; --q) v = fmaf(v, 1.0f / kA8Step, __uint_as_float(o[q][j]));
                 if (f != 0.0f) y[j] = fmaf(v, f, y[j]);              // (an accumulator without a job may hold anything)
             }
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int n = c + j;
-            if (n >= rows || !has) continue;
-            if (whole) {
-                const int t = attn_token(p, n);
-                static_cast<E*>(p.out)[(tok0 + t) * p.ot + (head0 + n - t * p.group) * p.oh + d] = a8_round<E>(y[j]);
-            } else {
-                p.part_o[(static_cast<size_t>(part) * (2 * kA8Cols) + part_row + n) * D + d] = y[j];
-            }
+            if (c + j >= rows || !has) continue;
+            if (whole) static_cast<E*>(p.out)[sm->at[slot][c + j] + d] = a8_round<E>(y[j]);
+            else p.part_o[(static_cast<size_t>(part) * (2 * kA8Cols) + part_row + c + j) * D + d] = y[j];
         }
     }
     w.tiles += static_cast<uint32_t>(nt);
@@ -666,7 +847,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
 }
 
 template <typename E, int D>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(kA8Threads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Attn8Params p)
 {
     constexpr int NP = a8_parts<E>::n;
@@ -677,7 +858,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const uint32_t pad = ((raw_addr + 1023u) & ~1023u) - raw_addr;
     const uint32_t q_buf = raw_addr + pad, p_buf = q_buf + 2 * p.q_bytes, ring_k = p_buf + 2 * p.p_bytes;
     const uint32_t ring_v = ring_k + p.k_stages * kTile, ring_sc = ring_v + p.v_stages * kTile;
-    const uint32_t small_off = ring_sc + kA8Scales * 1024 - raw_addr;
+    const uint32_t small_off = ring_sc + kA8Scales * kA8ScaleBytes - raw_addr;
     A8Small* const sm = reinterpret_cast<A8Small*>(smem_raw + small_off);
     auto bar = [](const uint64_t& b) { return smem_u32(&b); };
     const unsigned me = blockIdx.x;
@@ -692,16 +873,16 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     if (threadIdx.x == 0) {
         for (int s = 0; s < p.k_stages; ++s) { mbar_init(bar(sm->k_full[s]), 1); mbar_init(bar(sm->k_empty[s]), 2); }
         for (int s = 0; s < p.v_stages; ++s) { mbar_init(bar(sm->v_full[s]), 1); mbar_init(bar(sm->v_empty[s]), 2); }
-        for (int s = 0; s < kA8Scales; ++s) { mbar_init(bar(sm->sc_full[s]), 32); mbar_init(bar(sm->sc_empty[s]), 8); }
+        for (int s = 0; s < kA8Scales; ++s) { mbar_init(bar(sm->sc_full[s]), 1); mbar_init(bar(sm->sc_empty[s]), kA8SoftWarps); }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(bar(sm->q_full[s]), 1); mbar_init(bar(sm->q_empty[s]), 2);
-            mbar_init(bar(sm->s_full[s]), 1); mbar_init(bar(sm->s_free[s]), 4);
-            mbar_init(bar(sm->p_full[s]), 4); mbar_init(bar(sm->pv_done[s]), 1);
-            mbar_init(bar(sm->vote[s]), 4);
+            mbar_init(bar(sm->q_full[s]), 8);
+            mbar_init(bar(sm->s_full[s]), 1); mbar_init(bar(sm->s_free[s]), 8);
+            mbar_init(bar(sm->p_full[s]), 8); mbar_init(bar(sm->pv_done[s]), 1);
+            mbar_init(bar(sm->vote[s]), 8);
         }
-        for (int s = 0; s < kSegQueue; ++s) { mbar_init(bar(sm->seg_full[s]), 1); mbar_init(bar(sm->seg_empty[s]), 15); mbar_init(bar(sm->rs_full[s]), 1); }
-        mbar_init(bar(sm->o_full), 2); mbar_init(bar(sm->o_empty), 8); mbar_init(bar(sm->ml_full), 8); mbar_init(bar(sm->fin_full), 8);
-        mbar_init(bar(sm->part_full), 8); mbar_init(bar(sm->last_full), 1);
+        for (int s = 0; s < kSegQueue; ++s) { mbar_init(bar(sm->seg_full[s]), 1); mbar_init(bar(sm->seg_empty[s]), 6 + kA8SoftWarps); }
+        mbar_init(bar(sm->o_full), 2); mbar_init(bar(sm->o_empty), kA8SoftWarps); mbar_init(bar(sm->ml_full), kA8SoftWarps);
+        mbar_init(bar(sm->fin_full), kA8SoftWarps); mbar_init(bar(sm->part_full), kA8SoftWarps); mbar_init(bar(sm->last_full), 1);
         for (int s = 0; s < 4; ++s) mbar_init(bar(sm->drain[s]), 1);
         sm->abort[0] = 0; sm->abort[1] = 0;
         sm->limit[0] = sm->limit[1] = p.wait_limit;
@@ -721,14 +902,24 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const uint32_t tmem = __shfl_sync(0xffffffffu, sm->tmem, 0);
     int issued = 0;                              // tiles copied (copying warps; read again before the end)
 
-    // warps 0: queries; 1: the walk and keys; 2, 3: S of the slots; 4: scales; 5, 6: O of the slots; 7: values
+    // warps 0: rows of no window; 1: the walk and keys; 2, 3: S of the slots; 4: scales; 5, 6: O of the slots; 7: values.  (The block starts with
+    // 80 registers a thread: 8 warps at 32 and 16 at 104 take the same.)
     if (warp < 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-        if (warp == 1) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+        if (warp == 0) {
+            if (lane == 0) {
+                const unsigned half = static_cast<unsigned>(__ldcg(p.err + 1)) & 1u;
+                sm->half = half;
+                const unsigned other = 0xffffu << (16u * (half ^ 1u));
+                if (static_cast<unsigned>(__ldcg(p.count + me)) & other) atomicAnd(p.count + me, static_cast<int>(~other));
+            }
+            __syncwarp();
+            attn_clear_rows<E, D>(p, static_cast<int>(me), static_cast<int>(gridDim.x), lane);
+        } else if (warp == 1) {
             const int half = __ldcg(p.err + 1) & 1;
-            AttnWalk walk;
+            A8Walk walk;
             unsigned share, more;
-            attn_range<D>(p, me, lane, walk, share, more);
+            a8_range(p, me, lane, walk, share, more);
             int s[kSegWords + 1];
             A8Ring rg;
             bool ok = true;
@@ -741,8 +932,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                         auto block_of = [&](unsigned u) {
                             return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share;
                         };
-                        const unsigned unit0 = (me + 1) * share + min(me + 1, more) - s[kSegLeft] - s[kSegT0];
-                        const unsigned first = block_of(unit0), last = block_of(unit0 + s[kSegTiles] - 1);
+                        const unsigned unit0 = (me + 1) * share + min(me + 1, more) - s[kSegLeft];
+                        const unsigned first = block_of(unit0), last = block_of(unit0 + (s[kSegTiles] - 1) * (s[kSegPaired] ? 2 : 1));
                         s[kSegFirst] = first; s[kSegParts] = last - first + 1;
                     }
                 }
@@ -759,17 +950,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                                       s[kSegKeys], s[kSegHead], ring_k, bar(sm->k_full[0]), bar(sm->k_empty[0]), p.k_stages, flag, lane, rg, issued);
             }
         } else {
-            if (threadIdx.x == 0) {
-                const unsigned half = static_cast<unsigned>(__ldcg(p.err + 1)) & 1u;
-                sm->half = half;
-                const unsigned other = 0xffffu << (16u * (half ^ 1u));
-                if (static_cast<unsigned>(__ldcg(p.count + me)) & other) atomicAnd(p.count + me, static_cast<int>(~other));
-            }
-            __syncwarp();
             const int slot = warp == 3 || warp == 6 ? 1 : 0;
-            A8Ring rg;
+            A8Ring rg, done;
             uint32_t tiles = 0, jobs = 0;        // of the block, of the slot
-            int q_used = 0;
             bool ok = warp != 7 || static_cast<int>(me) != p.stalled;
             for (int item = 0; ok; ++item) {
                 const int qi = item & (kSegQueue - 1);
@@ -779,59 +962,21 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                 if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;           // (the compiler then knows it uniform)
                 const bool paired = __shfl_sync(0xffffffffu, sg[kSegPaired], 0) != 0;
                 const int t0 = __shfl_sync(0xffffffffu, sg[kSegT0], 0), t1 = __shfl_sync(0xffffffffu, sg[kSegT1], 0), nt = t1 - t0;
-                const int rows0 = __shfl_sync(0xffffffffu, sg[kSegRows0], 0), rows1 = __shfl_sync(0xffffffffu, sg[kSegRows1], 0);
-                const int cols = a8_cols(max(rows0, rows1));
-                const int req = sg[kSegReq], keys = sg[kSegKeys], head = sg[kSegHead];
                 if (warp == 7) {
                     // ------------------------------------------------ values
-                    ok = a8_load_tiles<D>(p, &tmV, req, attn_page(p, req, t0, t1, keys, lane), t0, t1, keys, head, ring_v, bar(sm->v_full[0]),
-                                          bar(sm->v_empty[0]), p.v_stages, flag, lane, rg, issued);
+                    ok = a8_load_tiles<D>(p, &tmV, sg[kSegReq], attn_page(p, sg[kSegReq], t0, t1, sg[kSegKeys], lane), t0, t1, sg[kSegKeys], sg[kSegHead],
+                                          ring_v, bar(sm->v_full[0]), bar(sm->v_empty[0]), p.v_stages, flag, lane, rg, issued);
                 } else if (warp == 4) {
-                    // ------------------------------------------------ scales: a lane copies those of four tokens
-                    const int mask = (1 << p.page_shift) - 1;
-                    auto page = [&](int t) {
-                        const int tok = t * kAttnTile + 4 * lane;
-                        return t < t1 && tok < keys ? p.block_table[req * p.table_stride + (tok >> p.page_shift)] : -1;
-                    };
-                    int pg = page(t0);
-                    for (int t = t0; t < t1; ++t) {
-                        const bool in = pg >= 0 && pg < p.n_pages;
-                        const int at = in ? (t * kAttnTile + 4 * lane) & mask : 0, from = in ? pg : 0;
-                        pg = page(t + 1);
-                        ok = attn_wait_warp(bar(sm->sc_empty[rg.s]), rg.ph ^ 1u, flag);
-                        if (!ok) break;
-                        const uint32_t dst = ring_sc + rg.s * 1024 + lane * 16;
-                        cp_async16(dst, p.ks + from * p.ksp + head * p.ksh + at, in ? 16 : 0);
-                        cp_async16(dst + 512, p.vs + from * p.vsp + head * p.vsh + at, in ? 16 : 0);
-                        cp_async_arrive(bar(sm->sc_full[rg.s]));
-                        rg.step(kA8Scales, 1);
-                    }
-                } else if (warp == 0) {
-                    // ------------------------------------------------ queries
-                    for (int t = 0; ok && t < (paired ? 2 : 1); ++t, ++q_used) {
-                        const int qb = q_used & 1;
-                        ok = attn_wait_warp(bar(sm->q_empty[qb]), ((q_used >> 1) & 1u) ^ 1u, flag);
-                        if (!ok) break;
-                        a8_cut_queries<E, D>(p, sg[kSegRow] + t * p.tpt, head, t ? rows1 : rows0, cols, q_buf + qb * p.q_bytes, sm->rs[qi][t], lane);
-                        fence_proxy_async();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bar(sm->q_full[qb]));
-                    }
-                    if (ok && lane == 0) mbar_arrive(bar(sm->rs_full[qi]));
+                    ok = a8_scales(p, sg[kSegReq], sg[kSegHead], t0, t1, sg[kSegKeys], ring_sc, sm, flag, lane, rg, done);
                 } else {
                     // ------------------------------------------------ MMA: a warp per slot and product
                     const bool second = warp > 4;
-                    const int qb = (q_used + (paired ? slot : 0)) & 1, stages = second ? p.v_stages : p.k_stages;
-                    const bool stacked = a8_stacked<E>(cols);
+                    const int cols = __shfl_sync(0xffffffffu, a8_cols(paired && slot ? sg[kSegRows1] : sg[kSegRows0]), 0);
+                    const int stages = second ? p.v_stages : p.k_stages, s_parts = a8_s_stacked<E>(cols) ? 1 : NP;
                     const uint32_t sS = tmem + slot * 256, sO = sS + a8_o_at<E>();
-                    const uint32_t idesc = second ? a8_idesc(D, stacked ? NP * cols : cols, true) : a8_idesc(kAttnTile, NP * cols, false);
-                    if (!second) {
-                        // (a paired item's other buffer too, so that no warp skips a phase)
-                        for (const int end = q_used + (paired ? 2 : 1); ok && q_used < end; ++q_used)
-                            ok = attn_wait_warp(bar(sm->q_full[q_used & 1]), static_cast<uint32_t>(q_used >> 1) & 1u, flag);
-                    } else if (item > 0) {
-                        ok = attn_wait_warp(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag);   // the previous O has been read
-                    }
+                    const uint32_t idesc = second ? a8_idesc(D, NP * cols, true) : a8_idesc(kAttnTile, s_parts == 1 ? NP * cols : cols, false);
+                    ok = second ? item == 0 || attn_wait_warp(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
+                                : attn_wait_warp(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
                     const int i0 = paired ? 0 : static_cast<int>((tiles ^ static_cast<uint32_t>(slot)) & 1u), step = paired ? 1 : 2;
                     A8Ring r = rg;
                     if (i0) r.step(stages, 1);
@@ -842,9 +987,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
-                                const uint64_t a0 = a8_desc(ring_k + r.s * kTile, D, 16), b0 = a8_desc(q_buf + qb * p.q_bytes, D, 16);
+                                const uint64_t a0 = a8_desc(ring_k + r.s * kTile, D, 16), b0 = a8_desc(q_buf + slot * p.q_bytes, D, 16);
+                                for (int q = 0; q < s_parts; ++q) {
 #pragma unroll
-                                for (int k = 0; k < D / 32; ++k) umma_f8(sS, a0 + 2 * k, b0 + 2 * k, idesc, k != 0);
+                                    for (int k = 0; k < D / 32; ++k) umma_f8(sS, a0 + 2 * k, b0 + 2 * k + q * (cols * D / 16), idesc, q != 0 || k != 0);
+                                }
                                 umma_commit(bar(sm->s_full[slot]));
                                 umma_commit(bar(sm->k_empty[r.s]));
                                 if (!paired) umma_commit(bar(sm->k_empty[r.s]));
@@ -856,12 +1003,9 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                             tc_fence_after();
                             if (elect_one()) {
                                 const uint64_t a0 = a8_desc(ring_v + r.s * kTile, D, 8192), b0 = a8_desc(p_buf + slot * p.p_bytes, 64, 8192);
-                                for (int q = 0; q < (stacked ? 1 : NP); ++q) {
 #pragma unroll
-                                    for (int k = 0; k < kAttnTile / 32; ++k)
-                                        umma_f8(sO, a0 + k * (32 * D / 16), b0 + k * (32 * 64 / 16) + q * (8192 / 16), idesc,
-                                                (i != i0 || q != 0 || k != 0) ? 1u : 0u);            // a slot's first tile overwrites O
-                                }
+                                for (int k = 0; k < kAttnTile / 32; ++k)
+                                    umma_f8(sO, a0 + k * (32 * D / 16), b0 + k * (32 * 64 / 16), idesc, i != i0 || k != 0);      // a slot's first tile overwrites O
                                 umma_commit(bar(sm->pv_done[slot]));
                                 umma_commit(bar(sm->v_empty[r.s]));
                                 if (!paired) umma_commit(bar(sm->v_empty[r.s]));
@@ -870,14 +1014,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                         __syncwarp();
                         r.step(stages, step);
                     }
-                    if (ok && elect_one()) {
-                        if (second) {
-                            umma_commit(bar(sm->o_full));
-                        } else {
-                            umma_commit(bar(sm->q_empty[qb]));
-                            if (paired) umma_commit(bar(sm->q_empty[qb]));           // (a split item's buffer hears from both warps)
-                        }
-                    }
+                    if (ok && second && elect_one()) umma_commit(bar(sm->o_full));
                     __syncwarp();
                     tiles += static_cast<uint32_t>(nt);
                     rg.jump(stages, nt);
@@ -885,29 +1022,27 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                 __syncwarp();
                 if (ok && lane == 0) mbar_arrive(bar(sm->seg_empty[qi]));
             }
-            if (warp == 4) {
-                cp_async_wait_all();
-                attn_clear_rows<E, D>(p, static_cast<int>(me), static_cast<int>(gridDim.x), lane);
-            }
+            if (warp == 4) cp_async_wait_all();
         }
     } else {
-        // ---------------------------------------------------------------- softmax: four warps per slot, a thread per key
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+        // ---------------------------------------------------------------- softmax: a thread per key and half of the columns
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
         A8Soft w;
-        w.slot = (warp - 8) >> 2; w.quad = warp & 3; w.lane = lane; w.row = w.quad * 32 + lane;
+        w.slot = (warp - 8) >> 3; w.half = ((warp - 8) >> 2) & 1; w.quad = warp & 3; w.lane = lane; w.row = w.quad * 32 + lane;
         w.lane_off = static_cast<uint32_t>(w.quad * 32) << 16;
-        w.tmem = tmem; w.p_smem = p_buf + w.slot * p.p_bytes; w.ring_v = ring_v; w.ring_sc = ring_sc; w.flag = flag;
+        w.tmem = tmem; w.q_smem = q_buf + w.slot * p.q_bytes; w.p_smem = p_buf + w.slot * p.p_bytes; w.ring_v = ring_v; w.ring_sc = ring_sc; w.flag = flag;
         uint32_t splits = 0;                     // stretches of shared items so far
         for (uint32_t item = 0; ; ++item) {
             const int qi = item & (kSegQueue - 1);
             const int* const sg = sm->queue[qi];
             if (!attn_wait_warp(bar(sm->seg_full[qi]), (item / kSegQueue) & 1u, flag)) break;
             if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;
-            const int cols = __shfl_sync(0xffffffffu, a8_cols(max(sg[kSegRows0], sg[kSegRows1])), 0);
+            const int cols = __shfl_sync(0xffffffffu, a8_cols(sg[kSegPaired] && w.slot ? sg[kSegRows1] : sg[kSegRows0]), 0);
             bool ok;
-            if (cols == 16) ok = a8_stretch<E, D, 1>(p, sm, w, sg, qi, item);
-            else if (cols == 32) ok = a8_stretch<E, D, 2>(p, sm, w, sg, qi, item);
-            else ok = a8_stretch<E, D, 4>(p, sm, w, sg, qi, item);
+            if (cols == 16) ok = a8_stretch<E, D, 8>(p, sm, w, sg, item);
+            else if (cols == 32) ok = a8_stretch<E, D, 16>(p, sm, w, sg, item);
+            else if (cols == 48) ok = a8_stretch<E, D, 24>(p, sm, w, sg, item);
+            else ok = a8_stretch<E, D, 32>(p, sm, w, sg, item);
             if (!ok) break;
             tc_fence_before();
             __syncwarp();

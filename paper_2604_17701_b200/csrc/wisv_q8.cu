@@ -71,11 +71,11 @@ template <typename E, int D>
 int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap& tmV, Attn8Params& p, cudaStream_t st)
 {
     const int rows = p.tpt * p.group;
-    p.cols = rows <= 16 ? 16 : rows <= 32 ? 32 : kA8Cols;
+    p.cols = a8_cols(rows);
     p.q_bytes = (uint32_t)(a8_parts<E>::n * p.cols * D);
     p.p_bytes = (uint32_t)a8_p_bytes<E>(p.cols);
     // what is left of shared memory: stages of keys and values in even numbers; a value stage is held longer (behind the exponentials)
-    const int left = kAttnSmem - kA8Slack - kA8Small - kA8Scales * 1024 - 2 * (int)(p.q_bytes + p.p_bytes);
+    const int left = kAttnSmem - kA8Slack - kA8Small - kA8Scales * kA8ScaleBytes - 2 * (int)(p.q_bytes + p.p_bytes);
     const int stages = left / (int)a8_tile_bytes<D>(), v = (stages + 2) / 4 * 2, k = (stages - (v < kA8Stages ? v : kA8Stages)) / 2 * 2;
     p.v_stages = v < kA8Stages ? v : kA8Stages;
     p.k_stages = k < kA8Stages ? k : kA8Stages;
@@ -88,7 +88,7 @@ int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap&
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3((unsigned)c->sm_count);
-    cfg.blockDim = dim3(kAttnThreads);
+    cfg.blockDim = dim3(kA8Threads);
     cfg.dynamicSmemBytes = kAttnSmem;
     WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
     return WISV_OK;

@@ -33,18 +33,6 @@ struct Q8AppendParams {
     const int64_t* slot_map;
 };
 
-template <typename E> __device__ __forceinline__ void unpack2(uint32_t w, float& lo, float& hi);
-template <> __device__ __forceinline__ void unpack2<__nv_bfloat16>(uint32_t w, float& lo, float& hi)
-{
-    lo = __uint_as_float(w << 16);
-    hi = __uint_as_float(w & 0xffff0000u);
-}
-template <> __device__ __forceinline__ void unpack2<__half>(uint32_t w, float& lo, float& hi)
-{
-    lo = __half2float(__ushort_as_half(static_cast<unsigned short>(w & 0xffffu)));
-    hi = __half2float(__ushort_as_half(static_cast<unsigned short>(w >> 16)));
-}
-
 // 16 elements of a head that L lanes hold: their codes; returns the scale.  A head with an infinite element or NaN has the scale NaN and
 // codes of 0.
 template <typename E, int L>
