@@ -46,7 +46,8 @@ constexpr int kA8Small = 9 * 1024;               // barriers, queue, tables of c
 constexpr int kA8Slack = 1024;
 constexpr int kA8SoftWarps = 16;                 // eight per slot
 constexpr int kA8Threads = 256 + 32 * kA8SoftWarps;
-constexpr float kA8Grow = 8.75f, kA8Room = 2.0f;
+constexpr float kA8Grow = 8.75f;
+template <typename E> __host__ __device__ constexpr float a8_room() { return is_bf16<E>::value ? 0.0f : -1.0f; }
 constexpr float kA8Step = 16.0f;                 // from one part of P to the next
 
 struct Attn8Params : AttnParams {
@@ -655,8 +656,9 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                 const float (&mx)[4][kA8Cols] = sm->mx[slot];
                 const float big = max3_nan(max3_nan(mx[0][ts], mx[1][ts], mx[2][ts]), mx[3][ts], mx[3][ts]);
                 const float old = m[ts];
-                const bool grows = !(big - old <= kA8Grow), bad = !(big < CUDART_INF_F);             // (a score of NaN or +inf)
-                const float now = !grows ? old : !bad ? big - kA8Room : old == kA8None ? 0.0f : old;
+                // (once any column has to, those that have doubled follow)
+                const bool grows = !(big - old <= a8_room<E>() + 1.0f), bad = !(big < CUDART_INF_F);             // (a score of NaN or +inf)
+                const float now = !grows ? old : !bad ? big - a8_room<E>() : old == kA8None ? 0.0f : old;
                 sm->a[slot][ts] = !grows ? 1.0f : bad ? CUDART_NAN_F : attn_ex2(old - now);
                 m[ts] = now;
             }
