@@ -134,23 +134,41 @@ __device__ __forceinline__ float warp_max_nan(float x)
     asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
-// Two numbers below 448 in NP e4m3 parts each, largest first, each further part 16 times what is left where `kScaled`; codes in pairs, the
-// first number in the low byte
+// Four numbers below 448 in NP e4m3 parts each, largest first, each further part 16 times what is left where `kScaled`: a word of four codes,
+// the first number in the low byte, for each part
 template <int NP, bool kScaled>
-__device__ __forceinline__ void a8_cut(float lo, float hi, uint32_t (&c)[NP])
+__device__ __forceinline__ void a8_cut(float x0, float x1, float x2, float x3, uint32_t (&c)[NP])
 {
-    uint32_t h;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h) : "f"(hi), "f"(lo));
+    uint32_t h0, h1;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(x1), "f"(x0));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(x3), "f"(x2));
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-        uint16_t e;
-        asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(e) : "r"(h));
-        c[p] = e;
         if (p + 1 < NP) {
-            uint32_t back;
-            asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(e));
-            asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(h) : "r"(back));
-            if (kScaled) asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h) : "r"(0x4c004c00u));           // 16
+            uint32_t b0, b1;
+            asm("{\n\t"
+                ".reg .b16 e0, e1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 e0, %3;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 e1, %4;\n\t"
+                "mov.b32 %0, {e0, e1};\n\t"
+                "cvt.rn.f16x2.e4m3x2 %1, e0;\n\t"
+                "cvt.rn.f16x2.e4m3x2 %2, e1;\n\t"
+                "}"
+                : "=r"(c[p]), "=r"(b0), "=r"(b1) : "r"(h0), "r"(h1));
+            asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(h0) : "r"(b0));
+            asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(h1) : "r"(b1));
+            if (kScaled) {
+                asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h0) : "r"(0x4c004c00u));           // 16
+                asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h1) : "r"(0x4c004c00u));
+            }
+        } else {
+            asm("{\n\t"
+                ".reg .b16 e0, e1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 e0, %1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f16x2 e1, %2;\n\t"
+                "mov.b32 %0, {e0, e1};\n\t"
+                "}"
+                : "=r"(c[p]) : "r"(h0), "r"(h1));
         }
     }
 }
@@ -200,7 +218,7 @@ struct A8Small {
     int32_t came_last;
     uint32_t half;
     alignas(16) int32_t queue[kSegQueue][kSegWords];
-    alignas(16) int32_t grow[2][2][8];
+    uint32_t grow[2][2];
     alignas(16) float rs[2][kA8Cols];            // c over a query column's power of two
     alignas(16) float m[2][kA8Cols];             // references
     alignas(16) float a[2][kA8Cols];             // factors when they grow; at the end those of a slot's own O
@@ -281,11 +299,10 @@ __device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, i
         uint32_t out[NP][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t f[NP], g[NP];
-            a8_cut<NP, false>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, f);
-            a8_cut<NP, false>(fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, g);
+            uint32_t f[NP];
+            a8_cut<NP, false>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, f);
 #pragma unroll
-            for (int q = 0; q < NP; ++q) out[q][i] = f[q] | g[q] << 16;
+            for (int q = 0; q < NP; ++q) out[q][i] = f[q];
         }
 #pragma unroll
         for (int q = 0; q < NP; ++q) {
@@ -528,10 +545,40 @@ __device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int hea
     return true;
 }
 
+// Waits and arrivals of the softmax warps, on a barrier OFF bytes behind `base`.  A wait for a barrier that is complete is a try, a vote and a branch
+// that the warp takes as one; an arrival is one predicated instruction.  (They were two fifths of a tile's instructions as calls of the general forms.)
+template <int OFF>
+__device__ __forceinline__ bool a8_wait(uint32_t base, uint32_t parity, uint32_t flag)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1 + %3], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}\n"
+        : "=r"(ok) : "r"(base), "r"(parity), "n"(OFF) : "memory");
+    if (__all_sync(0xffffffffu, ok)) return true;
+    return __all_sync(0xffffffffu, attn_wait_slow(base + OFF, parity, flag));
+}
+template <int OFF>
+__device__ __forceinline__ void a8_arrive(uint32_t base, int lane)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.eq.s32 p, %1, 0;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0 + %2];\n\t"
+        "}\n"
+        ::"r"(base), "r"(lane), "n"(OFF) : "memory");
+}
+#define A8_AT(member) static_cast<int>(offsetof(A8Small, member))
+
 // What a softmax warp carries from stretch to stretch
 struct A8Soft {
     int slot, half, quad, lane, row;             // half: of the columns; row: of the tile of keys
     uint32_t lane_off, tmem, q_smem, p_smem, ring_v, ring_sc, flag;
+    uint32_t small, bars;                        // A8Small, and its barriers of this slot
     uint32_t jobs = 0, votes = 0;                // of this slot so far
     uint32_t tiles = 0;                          // of the block so far
     A8Ring v, sc;                                // the place of tile number `tiles`
@@ -559,8 +606,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
     float* const m = sm->m[slot];
     auto vote = [&]() {                                              // the slot's warps meet
         __syncwarp();
-        if (w.lane == 0) mbar_arrive(smem_u32(&sm->vote[slot]));
-        const bool ok = attn_wait_warp(smem_u32(&sm->vote[slot]), w.votes & 1u, w.flag);
+        a8_arrive<A8_AT(vote)>(w.bars, w.lane);
+        const bool ok = a8_wait<A8_AT(vote)>(w.bars, w.votes & 1u, w.flag);
         ++w.votes;
         return ok;
     };
@@ -568,7 +615,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
     a8_cut_queries<E, D>(p, tok0, sg[kSegHead], rows, N, w.q_smem, sm->rs[slot], w.half * 4 + w.quad, w.lane);
     fence_proxy_async();
     __syncwarp();
-    if (w.lane == 0) mbar_arrive(smem_u32(&sm->q_full[slot]));
+    a8_arrive<A8_AT(q_full)>(w.bars, w.lane);
     if (ts < N) m[ts] = kA8None;
     if (!vote()) return false;
     uint64_t l[C / 2];
@@ -581,7 +628,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
     for (int i = i0; i < nt; i += step) {
         const int key0 = (sg[kSegT0] + i) * kAttnTile, key = key0 + w.row;
         // ---- the scales of this thread's key
-        if (!attn_wait_warp(smem_u32(&sm->sc_full[rsc.s]), rsc.ph, w.flag)) return false;
+        if (!a8_wait<A8_AT(sc_full)>(w.small + 8 * rsc.s, rsc.ph, w.flag)) return false;
         float ka, lb, rb;
         {
             const uint32_t at = w.ring_sc + rsc.s * kA8ScaleBytes + w.row * 4;
@@ -590,11 +637,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rb) : "r"(at + 1024) : "memory");
         }
         const uint64_t ka2 = pair(ka, ka), lb2 = pair(lb, lb);
-        // columns from `vis` on see this key
         const bool masked = key0 + kAttnTile - 1 > limit;
-        const int vis = (key >= keys ? 1 << 20 : min(max(key - limit, 0), kA8Cols + 1) * p.group) - col0;
-
-        if (!attn_wait_warp(smem_u32(&sm->s_full[slot]), w.jobs & 1u, w.flag)) return false;
+        if (!a8_wait<A8_AT(s_full)>(w.bars, w.jobs & 1u, w.flag)) return false;
         tc_fence_after();
         float x[C];
         // Pass 0 finds x with the references as they are; where a column outgrows its own, pass 1 finds x + m for its maximum and pass 2 x
@@ -625,6 +669,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                 }
             }
             if (masked) {
+                // columns from `vis` on see this key
+                const int vis = (key >= keys ? 1 << 20 : min(max(key - limit, 0), kA8Cols + 1) * p.group) - col0;
 #pragma unroll
                 for (int n = 0; n < C; ++n) x[n] = n >= vis ? x[n] : -CUDART_INF_F;
             }
@@ -636,11 +682,12 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                     worst[0] = max3_nan(worst[0], x[n], x[n + 1]);
                     worst[1] = max3_nan(worst[1], x[n + 2], x[n + 3]);
                 }
-                const bool mine = __any_sync(0xffffffffu, !(worst[0] <= kA8Grow && worst[1] <= kA8Grow));
-                volatile int32_t* const grow = sm->grow[slot][w.votes & 1u];
-                if (w.lane == 0) grow[w.half * 4 + w.quad] = mine;
+                // (whoever has such a column writes the number of the vote: two places in turn, and nothing to clear)
+                volatile uint32_t* const grow = &sm->grow[slot][w.votes & 1u];
+                const uint32_t number = w.votes;
+                if (!(worst[0] <= kA8Grow && worst[1] <= kA8Grow)) *grow = number;
                 if (!vote()) return false;
-                if (!__any_sync(0xffffffffu, grow[w.lane & 7] != 0)) break;
+                if (__all_sync(0xffffffffu, *grow != number)) break;
                 continue;
             }
             // ---- the references grow
@@ -665,7 +712,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             if (!vote()) return false;
             const float* const a = sm->a[slot];
             if (i != i0) {
-                if (!attn_wait_warp(smem_u32(&sm->pv_done[slot]), (w.jobs - 1) & 1u, w.flag)) return false;
+                if (!a8_wait<A8_AT(pv_done)>(w.bars, (w.jobs - 1) & 1u, w.flag)) return false;
                 tc_fence_after();
 #pragma unroll
                 for (int q = 0; q < NP; ++q) {
@@ -686,20 +733,18 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         }
         tc_fence_before();
         __syncwarp();
-        if (w.lane == 0) {
-            mbar_arrive(smem_u32(&sm->s_free[slot]));
-            mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
-            if (!paired) mbar_arrive(smem_u32(&sm->sc_empty[rsc.s]));
-        }
+        a8_arrive<A8_AT(s_free)>(w.bars, w.lane);
+        a8_arrive<A8_AT(sc_empty)>(w.small + 8 * rsc.s, w.lane);
+        if (!paired) a8_arrive<A8_AT(sc_empty)>(w.small + 8 * rsc.s, w.lane);
         rsc.step(kA8Scales, step);
 
         // ---- P, once the product before has read the last one
         if (w.jobs) {
-            if (!attn_wait_warp(smem_u32(&sm->pv_done[slot]), (w.jobs - 1) & 1u, w.flag)) return false;
+            if (!a8_wait<A8_AT(pv_done)>(w.bars, (w.jobs - 1) & 1u, w.flag)) return false;
         }
         if (key0 + kAttnTile > keys) {
             // (both slots of a paired item clear: whoever comes second writes zeros over zeros)
-            if (!attn_wait_warp(smem_u32(&sm->v_full[rv.s]), rv.ph, w.flag)) return false;
+            if (!a8_wait<A8_AT(v_full)>(w.small + 8 * rv.s, rv.ph, w.flag)) return false;
             if (key >= keys) {
                 const uint32_t at = w.ring_v + rv.s * a8_tile_bytes<D>() + w.row * D + w.half * (D / 2);
 #pragma unroll
@@ -708,26 +753,27 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         }
         rv.step(p.v_stages, step);
         const uint64_t rb2 = pair(rb, rb);
+        const uint32_t p_row = w.p_smem ^ (C % 16 ? 0 : col0);
 #pragma unroll
         for (int c = 0; c < C; c += W) {
             uint32_t out[NP][W / 4];
 #pragma unroll
             for (int j = 0; j < W / 4; ++j) {
-                uint32_t e[2][NP];
+                const int n = c + 4 * j;
+                const float e0 = attn_ex2(x[n]), e1 = attn_ex2(x[n + 1]), e2 = attn_ex2(x[n + 2]), e3 = attn_ex2(x[n + 3]);
+                l[n / 2] = fma2(pair(e0, e1), rb2, l[n / 2]);
+                l[n / 2 + 1] = fma2(pair(e2, e3), rb2, l[n / 2 + 1]);
+                uint32_t e[NP];
+                a8_cut<NP, true>(e0, e1, e2, e3, e);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int n = c + 4 * j + 2 * h;
-                    const float e0 = attn_ex2(x[n]), e1 = attn_ex2(x[n + 1]);
-                    l[n / 2] = fma2(pair(e0, e1), rb2, l[n / 2]);
-                    a8_cut<NP, true>(e0, e1, e[h]);
-                }
-#pragma unroll
-                for (int q = 0; q < NP; ++q) out[q][j] = e[0][q] | e[1][q] << 16;
+                for (int q = 0; q < NP; ++q) out[q][j] = e[q];
             }
 #pragma unroll
             for (int q = 0; q < NP; ++q) {
-                const int n = q * N + col0 + c;                      // column of the operand; rows of 64 bytes, swizzled
-                const uint32_t at = w.p_smem + (n >> 6) * 8192 + w.row * 64 + ((((n >> 4) & 3) ^ ((w.row >> 1) & 3)) << 4) + (n & 8);
+                // column n of the operand, in rows of 64 bytes, swizzled.  (w.p_smem is the row's place with the swizzle of piece 0; where
+                // a half's columns make whole pieces, its own bits do not carry into the others'.)
+                const int n = q * N + c + (C % 16 ? col0 : 0);
+                const uint32_t at = ((C % 16 ? w.p_smem : p_row) ^ (((n >> 4) & 3) << 4)) + (n >> 6) * 8192 + (n & 8);
                 if (W == 16)
                     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][W / 4 - 2]), "r"(out[q][W / 4 - 1]) : "memory");
                 else
@@ -737,7 +783,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
-        if (w.lane == 0) mbar_arrive(smem_u32(&sm->p_full[slot]));
+        a8_arrive<A8_AT(p_full)>(w.bars, w.lane);
         ++w.jobs;
     }
 
@@ -774,8 +820,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         }
     }
     __syncwarp();
-    if (w.lane == 0) mbar_arrive(smem_u32(&sm->ml_full));
-    if (!attn_wait_warp(smem_u32(&sm->ml_full), item & 1u, w.flag)) return false;
+    a8_arrive<A8_AT(ml_full)>(w.small, w.lane);
+    if (!a8_wait<A8_AT(ml_full)>(w.small, item & 1u, w.flag)) return false;
     const bool first = sg[kSegT0] == 0, whole = first && sg[kSegT1] == sg[kSegTiles];
     const int part = static_cast<int>(blockIdx.x) * 2 + (first ? 1 : 0), part_row = paired ? slot * kA8Cols : 0;
     if (ts < N) {
@@ -805,9 +851,9 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         }
     }
     __syncwarp();
-    if (w.lane == 0) mbar_arrive(smem_u32(&sm->fin_full));
-    if (!attn_wait_warp(smem_u32(&sm->fin_full), item & 1u, w.flag)) return false;
-    if (!attn_wait_warp(smem_u32(&sm->o_full), item & 1u, w.flag)) return false;
+    a8_arrive<A8_AT(fin_full)>(w.small, w.lane);
+    if (!a8_wait<A8_AT(fin_full)>(w.small, item & 1u, w.flag)) return false;
+    if (!a8_wait<A8_AT(o_full)>(w.small, item & 1u, w.flag)) return false;
     tc_fence_after();
 
     // ---- outputs: a thread has one element of every column; split: each slot does half of the columns, from both accumulators
@@ -887,6 +933,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         mbar_init(bar(sm->fin_full), kA8SoftWarps); mbar_init(bar(sm->part_full), kA8SoftWarps); mbar_init(bar(sm->last_full), 1);
         for (int s = 0; s < 4; ++s) mbar_init(bar(sm->drain[s]), 1);
         sm->abort[0] = 0; sm->abort[1] = 0;
+        sm->grow[0][0] = sm->grow[0][1] = sm->grow[1][0] = sm->grow[1][1] = 0xffffffffu;
         sm->limit[0] = sm->limit[1] = p.wait_limit;
         fence_barrier_init();
         tma_prefetch_desc(&tmK);
@@ -1032,7 +1079,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         A8Soft w;
         w.slot = (warp - 8) >> 3; w.half = ((warp - 8) >> 2) & 1; w.quad = warp & 3; w.lane = lane; w.row = w.quad * 32 + lane;
         w.lane_off = static_cast<uint32_t>(w.quad * 32) << 16;
-        w.tmem = tmem; w.q_smem = q_buf + w.slot * p.q_bytes; w.p_smem = p_buf + w.slot * p.p_bytes; w.ring_v = ring_v; w.ring_sc = ring_sc; w.flag = flag;
+        w.small = smem_u32(sm); w.bars = w.small + 8 * w.slot;
+        w.tmem = tmem; w.q_smem = q_buf + w.slot * p.q_bytes; w.p_smem = p_buf + w.slot * p.p_bytes + w.row * 64 + (((w.row >> 1) & 3) << 4); w.ring_v = ring_v; w.ring_sc = ring_sc; w.flag = flag;
         uint32_t splits = 0;                     // stretches of shared items so far
         for (uint32_t item = 0; ; ++item) {
             const int qi = item & (kSegQueue - 1);
