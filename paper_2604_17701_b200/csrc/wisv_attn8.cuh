@@ -48,7 +48,7 @@ constexpr int kA8SoftWarps = 16;                 // eight per slot
 constexpr int kA8Threads = 256 + 32 * kA8SoftWarps;
 constexpr float kA8Grow = 8.75f;
 template <typename E> __host__ __device__ constexpr float a8_room() { return is_bf16<E>::value ? 0.0f : -1.0f; }
-constexpr float kA8Step = 16.0f;                 // from one part of P to the next
+constexpr float kA8Step = 16.0f;                 // from one part to the next
 
 struct Attn8Params : AttnParams {
     const void* q; int64_t qt, qh;               // in elements
@@ -219,7 +219,8 @@ struct A8Small {
     uint32_t half;
     alignas(16) int32_t queue[kSegQueue][kSegWords];
     uint32_t grow[2][2];
-    alignas(16) float rs[2][kA8Cols];            // c over a query column's power of two
+    uint32_t top[2][2];                          // largest query element of a slot's tile, for even and odd items
+    alignas(16) float rs[2][kA8Cols];            // of query columns: c over a column's power of two; with a common one 0, or NaN where the row is
     alignas(16) float m[2][kA8Cols];             // references
     alignas(16) float a[2][kA8Cols];             // factors when they grow; at the end those of a slot's own O
     alignas(16) float b[2][kA8Cols];             // at the end: of the other slot's O
@@ -260,16 +261,20 @@ __device__ __forceinline__ bool a8_load_tiles(const Attn8Params& p, const CUtens
     return true;
 }
 
-// Rows w, w + 8, ... of a tile of queries (in groups of 32 / (D / 16) rows), cut into parts by one warp: D / 16 lanes to a row of 16 elements
-// each.
-template <typename E, int D>
-__device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, int head, int rows, int cols, uint32_t dst, float* rs, int w, int lane)
+// A slot's tile of queries, cut into parts by its eight warps: D / 16 lanes to a row of 16 elements, rows in groups of 32 / (D / 16).  Where the
+// parts lie side by side (kCommon) the tile has one power of two, from its largest finite element, and each further part 16 times
+// what is left, so that the half step is at most 2^-21 of that element; else every row has its own, and the step is 2^-17 of the row's
+// largest.  Returns c over the common power of two.
+template <typename E, int D, bool kCommon, typename Vote>
+__device__ __forceinline__ bool a8_cut_queries(const Attn8Params& p, A8Small* sm, int slot, uint32_t item, int row0, int head, int rows, int cols, uint32_t dst,
+                                               int w, int lane, Vote vote, float& common)
 {
-    constexpr int NP = a8_parts<E>::n, L = D / 16, R = 32 / L, U = 16 / R;           // U groups cover 64 columns in two rounds of 8 warps
+    constexpr int NP = a8_parts<E>::n, L = D / 16, R = 32 / L, U = 8 / R;            // U groups a warp: 64 columns by eight warps
     const int c = lane % L;
-    uint4 v[U / 2][2];
+    uint4 v[U][2];
+    uint32_t top[U], most = 0;
 #pragma unroll
-    for (int u = 0; u < U / 2; ++u) {
+    for (int u = 0; u < U; ++u) {
         const int r = (u * 8 + w) * R + lane / L;
         v[u][0] = v[u][1] = make_uint4(0, 0, 0, 0);
         if (r < rows) {
@@ -280,27 +285,47 @@ __device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, i
         }
     }
 #pragma unroll
-    for (int u = 0; u < U / 2; ++u) {
+    for (int u = 0; u < U; ++u) {
+        const uint32_t* d = reinterpret_cast<const uint32_t*>(v[u]);
+        top[u] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float a, b;
+            unpack2<E>(d[i], a, b);
+            top[u] = max(top[u], max(__float_as_uint(a) & 0x7fffffffu, __float_as_uint(b) & 0x7fffffffu));
+        }
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) top[u] = max(top[u], __shfl_xor_sync(0xffffffffu, top[u], o));
+        if (top[u] < 0x7f800000u) most = max(most, top[u]);
+    }
+    if (kCommon) {
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) atomicMax(&sm->top[slot][item & 1u], most);
+        if (!vote()) return false;
+        most = *const_cast<volatile uint32_t*>(&sm->top[slot][item & 1u]);
+        if (w == 0 && lane == 0) *const_cast<volatile uint32_t*>(&sm->top[slot][(item + 1) & 1u]) = 0;
+    }
+    // (0 and what is below 2^-119 are scaled alike)
+    const uint32_t ec = max(most >> 23, 8u);
+    common = p.scale_log2 * __uint_as_float((ec - 7u) << 23);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
         const int r = (u * 8 + w) * R + lane / L;
         if ((u * 8 + w) * R >= cols) break;                          // (the warp as one)
         const uint32_t* d = reinterpret_cast<const uint32_t*>(v[u]);
-        float x[16];
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            unpack2<E>(d[i], x[2 * i], x[2 * i + 1]);
-            top = max(top, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
-        }
-#pragma unroll
-        for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const bool fine = top < 0x7f800000u;
-        const uint32_t e = max(top >> 23, 8u);                       // (0 and what is below 2^-119 are scaled alike)
-        const float up = __uint_as_float((261u - (fine ? e : 8u)) << 23);            // largest element to [128, 256)
+        const bool fine = top[u] < 0x7f800000u;
+        const uint32_t e = kCommon ? ec : fine ? max(top[u] >> 23, 8u) : 8u;
+        const float up = __uint_as_float((261u - e) << 23);          // largest element to [128, 256)
         uint32_t out[NP][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
+            float x[4];
+            unpack2<E>(d[2 * i], x[0], x[1]);
+            unpack2<E>(d[2 * i + 1], x[2], x[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
             uint32_t f[NP];
-            a8_cut<NP, false>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, f);
+            a8_cut<NP, kCommon>(x[0], x[1], x[2], x[3], f);
 #pragma unroll
             for (int q = 0; q < NP; ++q) out[q][i] = f[q];
         }
@@ -310,8 +335,9 @@ __device__ __forceinline__ void a8_cut_queries(const Attn8Params& p, int row0, i
             const uint32_t at = dst + row * D + ((D == 128 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4);
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(out[q][0]), "r"(out[q][1]), "r"(out[q][2]), "r"(out[q][3]) : "memory");
         }
-        if (c == 0) rs[r] = r >= rows ? 0.0f : fine ? p.scale_log2 * __uint_as_float((e - 7u) << 23) : CUDART_NAN_F;
+        if (c == 0) sm->rs[slot][r] = kCommon ? (fine ? 0.0f : CUDART_NAN_F) : r >= rows ? 0.0f : fine ? p.scale_log2 * __uint_as_float((e - 7u) << 23) : CUDART_NAN_F;
     }
+    return true;
 }
 
 // The merge of an item's partials by the softmax warps of the block that came last: a warp takes a column at a time, its lanes
@@ -594,7 +620,8 @@ template <typename E, int D, int C>
 __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8Soft& w, const int* sg, uint32_t item)
 {
     constexpr int NP = a8_parts<E>::n, N = 2 * C, W = C % 16 ? 8 : 16;               // W: columns at a time
-    constexpr int kSParts = a8_s_stacked<E>(N) ? NP : 1;
+    constexpr bool kCommon = a8_s_stacked<E>(N);                     // S has columns for each part, and the queries one power of two
+    constexpr int kSParts = kCommon ? NP : 1;
     const int slot = w.slot, col0 = w.half * C, ts = w.half * 128 + w.row;
     const bool paired = sg[kSegPaired];
     const int nt = sg[kSegT1] - sg[kSegT0], keys = sg[kSegKeys];
@@ -612,7 +639,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
         return ok;
     };
     // ---- queries (the products that read the last ones are complete: their S has been waited for)
-    a8_cut_queries<E, D>(p, tok0, sg[kSegHead], rows, N, w.q_smem, sm->rs[slot], w.half * 4 + w.quad, w.lane);
+    float common;
+    if (!a8_cut_queries<E, D, kCommon>(p, sm, slot, item, tok0, sg[kSegHead], rows, N, w.q_smem, w.half * 4 + w.quad, w.lane, vote, common)) return false;
     fence_proxy_async();
     __syncwarp();
     a8_arrive<A8_AT(q_full)>(w.bars, w.lane);
@@ -636,6 +664,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lb) : "r"(at + 512) : "memory");
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rb) : "r"(at + 1024) : "memory");
         }
+        if (kCommon) ka *= common;
         const uint64_t ka2 = pair(ka, ka), lb2 = pair(lb, lb);
         const bool masked = key0 + kAttnTile - 1 > limit;
         if (!a8_wait<A8_AT(s_full)>(w.bars, w.jobs & 1u, w.flag)) return false;
@@ -654,15 +683,18 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                 tmem_wait_ld();
 #pragma unroll
                 for (int j = 0; j < W; j += 4) {
-                    const float4 r4 = *reinterpret_cast<const float4*>(rs + c + j), m4 = *reinterpret_cast<const float4*>(m + col0 + c + j);
+                    const float4 m4 = *reinterpret_cast<const float4*>(m + col0 + c + j);
+                    float4 r4 = make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+                    if (!kCommon) r4 = *reinterpret_cast<const float4*>(rs + c + j);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int k = j + 2 * h;
-                        uint64_t v = pair(__uint_as_float(s[0][k]), __uint_as_float(s[0][k + 1]));
+                        uint64_t v = pair(__uint_as_float(s[kSParts - 1][k]), __uint_as_float(s[kSParts - 1][k + 1]));
 #pragma unroll
-                        for (int q = 1; q < kSParts; ++q) v = add2(v, pair(__uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1])));
-                        v = fma2(mul2(v, h ? pair(r4.z, r4.w) : pair(r4.x, r4.y)), ka2, lb2);
-                        v = fma2(h ? pair(m4.z, m4.w) : pair(m4.x, m4.y), neg2, v);
+                        for (int q = kSParts - 2; q >= 0; --q)
+                            v = fma2(v, pair(1.0f / kA8Step, 1.0f / kA8Step), pair(__uint_as_float(s[q][k]), __uint_as_float(s[q][k + 1])));
+                        if (!kCommon) v = mul2(v, h ? pair(r4.z, r4.w) : pair(r4.x, r4.y));
+                        v = fma2(v, ka2, fma2(h ? pair(m4.z, m4.w) : pair(m4.x, m4.y), neg2, lb2));
                         x[c + k] = low(v);
                         x[c + k + 1] = high(v);
                     }
@@ -760,11 +792,15 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
 #pragma unroll
             for (int j = 0; j < W / 4; ++j) {
                 const int n = c + 4 * j;
-                const float e0 = attn_ex2(x[n]), e1 = attn_ex2(x[n + 1]), e2 = attn_ex2(x[n + 2]), e3 = attn_ex2(x[n + 3]);
-                l[n / 2] = fma2(pair(e0, e1), rb2, l[n / 2]);
-                l[n / 2 + 1] = fma2(pair(e2, e3), rb2, l[n / 2 + 1]);
+                uint64_t y[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int k = n + 2 * h;
+                    y[h] = pair(attn_ex2(x[k]), attn_ex2(x[k + 1]));
+                    l[k / 2] = fma2(y[h], rb2, l[k / 2]);
+                }
                 uint32_t e[NP];
-                a8_cut<NP, true>(e0, e1, e2, e3, e);
+                a8_cut<NP, true>(low(y[0]), high(y[0]), low(y[1]), high(y[1]), e);
 #pragma unroll
                 for (int q = 0; q < NP; ++q) out[q][j] = e[q];
             }
@@ -835,6 +871,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             mm = top;
         }
         if (mm == kA8None) { mm = -CUDART_INF_F; wa = 0.0f; }
+        else if (kCommon) ll += sm->rs[slot][ts];
         if (whole) {
             const float inv = ll == 0.0f ? 0.0f : attn_rcp(ll);
             wa *= inv;
@@ -933,6 +970,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         mbar_init(bar(sm->fin_full), kA8SoftWarps); mbar_init(bar(sm->part_full), kA8SoftWarps); mbar_init(bar(sm->last_full), 1);
         for (int s = 0; s < 4; ++s) mbar_init(bar(sm->drain[s]), 1);
         sm->abort[0] = 0; sm->abort[1] = 0;
+        sm->top[0][0] = sm->top[0][1] = sm->top[1][0] = sm->top[1][1] = 0;
         sm->grow[0][0] = sm->grow[0][1] = sm->grow[1][0] = sm->grow[1][1] = 0xffffffffu;
         sm->limit[0] = sm->limit[1] = p.wait_limit;
         fence_barrier_init();
