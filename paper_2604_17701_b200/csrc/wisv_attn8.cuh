@@ -46,6 +46,7 @@ constexpr int kA8Small = 9 * 1024;               // barriers, queue, tables of c
 constexpr int kA8Slack = 1024;
 constexpr int kA8SoftWarps = 16;                 // eight per slot
 constexpr int kA8Threads = 256 + 32 * kA8SoftWarps;
+constexpr int kA8ItemCost = 8;                   // (see kAttnItemCost) key tiles that starting and finishing an item is worth
 constexpr float kA8Grow = 8.75f;
 template <typename E> __host__ __device__ constexpr float a8_room() { return is_bf16<E>::value ? 0.0f : -1.0f; }
 constexpr float kA8Step = 16.0f;                 // from one part to the next
@@ -340,6 +341,8 @@ __device__ __forceinline__ bool a8_cut_queries(const Attn8Params& p, A8Small* sm
     return true;
 }
 
+constexpr int kA8Tok1 = kSegOdd;                 // in a stretch: tokens of a paired item's first tile
+
 // The merge of an item's partials by the softmax warps of the block that came last: a warp takes a column at a time, its lanes
 // the D elements; four partials are loaded together and added in block order.  Reads go past L1, which other blocks'
 // writes do not reach.
@@ -391,7 +394,7 @@ __device__ __forceinline__ void a8_merge(const Attn8Params& p, const int* sg, in
             m = mm;
         }
         const float inv = l == 0.0f ? 0.0f : attn_rcp(l);
-        const int t = attn_token(p, in), tok = sg[kSegRow] + t + (second ? p.tpt : 0), head = sg[kSegHead] * p.group + in - t * p.group;
+        const int t = attn_token(p, in), tok = sg[kSegRow] + t + (second ? sg[kA8Tok1] : 0), head = sg[kSegHead] * p.group + in - t * p.group;
         E* const dst = static_cast<E*>(p.out) + tok * p.ot + head * p.oh + lane * V;
         if (V == 4)
             *reinterpret_cast<uint2*>(dst) = make_uint2(pack2<E>(acc[0] * inv, acc[1] * inv), pack2<E>(acc[V - 2] * inv, acc[V - 1] * inv));
@@ -407,11 +410,12 @@ __host__ __device__ __forceinline__ int a8_cols(int rows) { return rows <= 16 ? 
 
 constexpr float kA8None = -3.402823466e38f;      // the reference of a column that has seen no key
 
-// ---- the work: as in the 16-bit kernel, with tiles of paired items weighing two units, since their two slots have a product each
+// ---- the work: as in the 16-bit kernel, with tiles of paired items weighing two units, since their two slots have a product each.  A paired item's
+// tokens are halved, so that neither tile has columns to spare.
 __device__ __forceinline__ int a8_weight(const Attn8Params& p, const AttnReq& r, int it) { return r.n - it * 2 * p.tpt > p.tpt ? 2 : 1; }
 __device__ __forceinline__ unsigned a8_units(const Attn8Params& p, const AttnReq& r, int it)
 {
-    return a8_weight(p, r, it) * attn_tiles(p, r, it) + kAttnItemCost;
+    return a8_weight(p, r, it) * attn_tiles(p, r, it) + kA8ItemCost;
 }
 
 struct A8Walk {
@@ -427,18 +431,19 @@ struct A8Walk {
                 r = attn_request(p, b);
                 continue;
             }
-            const int nt = attn_tiles(p, r, it), wt = a8_weight(p, r, it), all = wt * nt + kAttnItemCost;
+            const int nt = attn_tiles(p, r, it), wt = a8_weight(p, r, it), all = wt * nt + kA8ItemCost;
             const int take = min(units, all - pos);
             const int t0 = min(nt, (pos + wt - 1) / wt), t1 = min(nt, (pos + take + wt - 1) / wt);
             if (t1 > t0) {
-                const int tok0 = it * 2 * p.tpt, left = r.n - tok0;
+                const int tok0 = it * 2 * p.tpt, here = min(r.n - tok0, 2 * p.tpt), tok1 = wt == 2 ? (here + 1) / 2 : here;
                 s[kSegJobs] = t1 - t0;
                 s[kSegPaired] = wt == 2; s[kSegT0] = t0; s[kSegT1] = t1; s[kSegTiles] = nt;
                 s[kSegKeys] = r.kv; s[kSegLimit] = r.kv - r.n + tok0;
                 s[kSegRow] = r.q0 + tok0; s[kSegHead] = kvh; s[kSegReq] = b;
                 s[kSegLeft] = units + pos;       // (from the item's first unit to the end of the range)
-                s[kSegRows0] = min(left, p.tpt) * p.group;
-                s[kSegRows1] = wt == 2 ? min(left - p.tpt, p.tpt) * p.group : 0;
+                s[kSegRows0] = tok1 * p.group;
+                s[kSegRows1] = (here - tok1) * p.group;
+                s[kA8Tok1] = tok1;
             }
             units -= take;
             pos += take;
@@ -625,9 +630,9 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
     const int slot = w.slot, col0 = w.half * C, ts = w.half * 128 + w.row;
     const bool paired = sg[kSegPaired];
     const int nt = sg[kSegT1] - sg[kSegT0], keys = sg[kSegKeys];
-    const int limit = sg[kSegLimit] + (paired && slot ? p.tpt : 0);  // last key that the tile's first token sees
+    const int limit = sg[kSegLimit] + (paired && slot ? sg[kA8Tok1] : 0);  // last key that the tile's first token sees
     const int rows = paired && slot ? sg[kSegRows1] : sg[kSegRows0];
-    const int tok0 = sg[kSegRow] + (paired && slot ? p.tpt : 0);
+    const int tok0 = sg[kSegRow] + (paired && slot ? sg[kA8Tok1] : 0);
     const uint32_t aS = w.tmem + static_cast<uint32_t>(slot) * 256 + w.lane_off, aO = aS + a8_o_at<E>();
     const float* const rs = sm->rs[slot] + col0;
     float* const m = sm->m[slot];
@@ -1014,7 +1019,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                 const bool some = walk.next(p, s);
                 const int qi = item & (kSegQueue - 1);
                 if (some) {
-                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1; s[kSegOdd] = 0; s[kSegShift] = 16 * half;
+                    s[kSegFirst] = static_cast<int>(me); s[kSegParts] = 1; s[kSegShift] = 16 * half;
                     if (s[kSegT0] > 0 || s[kSegT1] < s[kSegTiles]) {                 // shared: whose ranges does the item reach?
                         auto block_of = [&](unsigned u) {
                             return u < more * (share + 1) ? u / (share + 1) : more + (u - more * (share + 1)) / share;
