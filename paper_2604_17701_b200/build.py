@@ -12,7 +12,7 @@ SOURCES = [os.path.join(CSRC, "wisv_api.cu"), os.path.join(CSRC, "wisv_static.cu
            os.path.join(CSRC, "wisv_link.cu"), os.path.join(CSRC, "wisv_paged.cu"),
            os.path.join(CSRC, "wisv_q8.cu"), os.path.join(CSRC, "wisv_residual.cu")]
 DEPS = SOURCES + [os.path.join(CSRC, n) for n in ("wisv_gemm.cuh", "wisv_gemm2.cuh", "wisv_aux.cuh", "wisv_ptx.cuh",
-                                                  "wisv_pages.cuh", "wisv_attn.cuh", "wisv_attn8.cuh", "wisv_cache.cuh",
+                                                  "wisv_pages.cuh", "wisv_attn.cuh", "wisv_attn8.cuh", "wisv_attn8r.cuh", "wisv_cache.cuh",
                                                   "wisv_q8.cuh")] + \
     [os.path.join(os.path.dirname(_HERE), "include", "wisv.h")]
 

@@ -55,7 +55,8 @@ struct Attn8Params : AttnParams {
     const void* q; int64_t qt, qh;               // in elements
     const float *ks, *vs;                        // scales: tokens of a page and head side by side
     int64_t ksp, ksh, vsp, vsh;                  // strides of pages and heads, in floats
-    int32_t cols;                                // 16, 32 or 64: no tile has more
+    int32_t rows;                                // query rows are rows of the products (wisv_attn8r.cuh)
+    int32_t cols;                                // 16, 32, 48 or 64: no tile has more
     int32_t k_stages, v_stages;                  // even
     uint32_t q_bytes, p_bytes;                   // of a tile's queries, of a slot's P
 };
@@ -410,8 +411,8 @@ __host__ __device__ __forceinline__ int a8_cols(int rows) { return rows <= 16 ? 
 
 constexpr float kA8None = -3.402823466e38f;      // the reference of a column that has seen no key
 
-// ---- the work: as in the 16-bit kernel, with tiles of paired items weighing two units, since their two slots have a product each.  A paired item's
-// tokens are halved, so that neither tile has columns to spare.
+// ---- the work: as in the 16-bit kernel, with tiles of paired items weighing two units, since their two slots have a product each.  Where
+// rows are columns a paired item's tokens are halved, so that neither tile has columns to spare.
 __device__ __forceinline__ int a8_weight(const Attn8Params& p, const AttnReq& r, int it) { return r.n - it * 2 * p.tpt > p.tpt ? 2 : 1; }
 __device__ __forceinline__ unsigned a8_units(const Attn8Params& p, const AttnReq& r, int it)
 {
@@ -435,7 +436,7 @@ struct A8Walk {
             const int take = min(units, all - pos);
             const int t0 = min(nt, (pos + wt - 1) / wt), t1 = min(nt, (pos + take + wt - 1) / wt);
             if (t1 > t0) {
-                const int tok0 = it * 2 * p.tpt, here = min(r.n - tok0, 2 * p.tpt), tok1 = wt == 2 ? (here + 1) / 2 : here;
+                const int tok0 = it * 2 * p.tpt, here = min(r.n - tok0, 2 * p.tpt), tok1 = wt != 2 ? here : p.rows ? p.tpt : (here + 1) / 2;
                 s[kSegJobs] = t1 - t0;
                 s[kSegPaired] = wt == 2; s[kSegT0] = t0; s[kSegT1] = t1; s[kSegTiles] = nt;
                 s[kSegKeys] = r.kv; s[kSegLimit] = r.kv - r.n + tok0;
@@ -525,7 +526,8 @@ __device__ __forceinline__ void a8_range(const Attn8Params& p, unsigned me, int 
 
 // The scales of key tiles t0 .. t1 - 1 into their ring, by one warp, four tokens to a lane: copied four tiles ahead, then turned in place into
 // a, log2 b and 1 / b.  A lane works on what it has copied itself.
-__device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int head, int t0, int t1, int keys, uint32_t ring, A8Small* sm, uint32_t flag,
+template <typename Small>
+__device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int head, int t0, int t1, int keys, uint32_t ring, Small* sm, uint32_t flag,
                                           int lane, A8Ring& at, A8Ring& done)
 {
     constexpr int kAhead = 4;

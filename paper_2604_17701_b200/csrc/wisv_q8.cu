@@ -7,6 +7,7 @@
 
 #include "../../include/wisv.h"
 #include "wisv_cache.cuh"
+#include "wisv_attn8r.cuh"
 #include "wisv_q8.cuh"
 
 namespace wisv {
@@ -14,9 +15,13 @@ namespace wisv {
 bool q8_prepare()
 {
     return cudaFuncSetAttribute(attn8_kernel<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(attn8_rows_kernel<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
            cudaFuncSetAttribute(attn8_kernel<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(attn8_rows_kernel<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
            cudaFuncSetAttribute(attn8_kernel<__half, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
+           cudaFuncSetAttribute(attn8_rows_kernel<__half, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(attn8_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
+           cudaFuncSetAttribute(attn8_rows_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
 }
 
 }  // namespace wisv
@@ -66,6 +71,9 @@ int encode_codes(const wisv_cache* c, CUtensorMap* out, const void* base, int64_
     return r == CUDA_SUCCESS ? WISV_OK : WISV_EINVAL;
 }
 
+// Rows of a key head from which a window's rows are rows of the products, not columns.
+constexpr int kRowsFrom = 65;
+
 // Programmatic dependent launch: the block set-up (barriers, TMEM) runs while the kernel before it in the stream ends.
 template <typename E, int D>
 int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap& tmV, Attn8Params& p, cudaStream_t st)
@@ -90,7 +98,12 @@ int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap&
     cfg.gridDim = dim3((unsigned)c->sm_count);
     cfg.blockDim = dim3(kA8Threads);
     cfg.dynamicSmemBytes = kAttnSmem;
-    WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
+    if (p.rows) {
+        cfg.blockDim = dim3(kAttnThreads);
+        WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_rows_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
+    } else {
+        WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
+    }
     return WISV_OK;
 }
 
@@ -193,7 +206,9 @@ int wisv_cache_attend_q8(wisv_cache* c, const wisv_q8_pages* pages, const wisv_q
     const int group = c->cfg.n_heads / c->cfg.n_kv_heads, D = c->cfg.head_dim;
     Attn8Params p;
     memset(&p, 0, sizeof p);
-    p.tpt = kA8Cols / group < a->max_new ? kA8Cols / group : a->max_new;
+    p.rows = (int64_t)a->max_new * group >= kRowsFrom;
+    const int tile = (p.rows ? kAttnTile : kA8Cols) / group;
+    p.tpt = tile < a->max_new ? tile : a->max_new;
     // every key tile of every item has to count in 31 bits, whatever the lengths on the device say
     const int64_t items = (a->T + p.tpt - 1) / p.tpt + a->B, tiles = ((int64_t)a->max_blocks << c->page_shift) / kAttnTile + 2;
     if (items * tiles > 0x7ffe0000LL / c->cfg.n_kv_heads) return WISV_ESHAPE;
