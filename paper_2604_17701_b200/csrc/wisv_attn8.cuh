@@ -56,7 +56,6 @@ struct Attn8Params : AttnParams {
     const float *ks, *vs;                        // scales: tokens of a page and head side by side
     int64_t ksp, ksh, vsp, vsh;                  // strides of pages and heads, in floats
     int32_t rows;                                // query rows are rows of the products (wisv_attn8r.cuh)
-    int32_t cols;                                // 16, 32, 48 or 64: no tile has more
     int32_t k_stages, v_stages;                  // even
     uint32_t q_bytes, p_bytes;                   // of a tile's queries, of a slot's P
 };
@@ -406,7 +405,8 @@ __device__ __forceinline__ void a8_merge(const Attn8Params& p, const int* sg, in
     }
 }
 
-// columns that a tile of so many rows is computed with
+// Columns that tiles of up to so many rows are computed with, all tiles of a call alike.  (Sixteen warps that change from one width's instructions to
+// another's fetch them anew: windows of 8 or of 9 rows of 4 heads 121 and 141 us, mixed with a width for each 163, with one 141.)
 __host__ __device__ __forceinline__ int a8_cols(int rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 ? 48 : kA8Cols; }
 
 constexpr float kA8None = -3.402823466e38f;      // the reference of a column that has seen no key
@@ -622,7 +622,7 @@ template <int W> __device__ __forceinline__ void a8_tmem_ld(uint32_t at, uint32_
 template <> __device__ __forceinline__ void a8_tmem_ld<8>(uint32_t at, uint32_t (&r)[8]) { tmem_ld8(at, r); }
 template <> __device__ __forceinline__ void a8_tmem_ld<16>(uint32_t at, uint32_t (&r)[16]) { tmem_ld16(at, r); }
 
-// A stretch of an item's tiles with at most 2 C columns, up to and including its outputs or partials.  false: a wait ran out.
+// A stretch of an item's tiles with 2 C columns, up to and including its outputs or partials.  false: a wait ran out.
 template <typename E, int D, int C>
 __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8Soft& w, const int* sg, uint32_t item)
 {
@@ -938,7 +938,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
     return true;
 }
 
-template <typename E, int D>
+template <typename E, int D, int N>
 __global__ void __launch_bounds__(kA8Threads, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const Attn8Params p)
 {
@@ -1065,10 +1065,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                 } else {
                     // ------------------------------------------------ MMA: a warp per slot and product
                     const bool second = warp > 4;
-                    const int cols = __shfl_sync(0xffffffffu, a8_cols(paired && slot ? sg[kSegRows1] : sg[kSegRows0]), 0);
-                    const int stages = second ? p.v_stages : p.k_stages, s_parts = a8_s_stacked<E>(cols) ? 1 : NP;
+                    const int stages = second ? p.v_stages : p.k_stages;
+                    constexpr int kSParts = a8_s_stacked<E>(N) ? 1 : NP;             // products of S
                     const uint32_t sS = tmem + slot * 256, sO = sS + a8_o_at<E>();
-                    const uint32_t idesc = second ? a8_idesc(D, NP * cols, true) : a8_idesc(kAttnTile, s_parts == 1 ? NP * cols : cols, false);
+                    const uint32_t idesc = second ? a8_idesc(D, NP * N, true) : a8_idesc(kAttnTile, kSParts == 1 ? NP * N : N, false);
                     ok = second ? item == 0 || attn_wait_warp(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
                                 : attn_wait_warp(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
                     const int i0 = paired ? 0 : static_cast<int>((tiles ^ static_cast<uint32_t>(slot)) & 1u), step = paired ? 1 : 2;
@@ -1082,9 +1082,10 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                             tc_fence_after();
                             if (elect_one()) {
                                 const uint64_t a0 = a8_desc(ring_k + r.s * kTile, D, 16), b0 = a8_desc(q_buf + slot * p.q_bytes, D, 16);
-                                for (int q = 0; q < s_parts; ++q) {
 #pragma unroll
-                                    for (int k = 0; k < D / 32; ++k) umma_f8(sS, a0 + 2 * k, b0 + 2 * k + q * (cols * D / 16), idesc, q != 0 || k != 0);
+                                for (int q = 0; q < kSParts; ++q) {
+#pragma unroll
+                                    for (int k = 0; k < D / 32; ++k) umma_f8(sS, a0 + 2 * k, b0 + 2 * k + q * (N * D / 16), idesc, q != 0 || k != 0);
                                 }
                                 umma_commit(bar(sm->s_full[slot]));
                                 umma_commit(bar(sm->k_empty[r.s]));
@@ -1132,12 +1133,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             const int* const sg = sm->queue[qi];
             if (!attn_wait_warp(bar(sm->seg_full[qi]), (item / kSegQueue) & 1u, flag)) break;
             if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;
-            const int cols = __shfl_sync(0xffffffffu, a8_cols(sg[kSegPaired] && w.slot ? sg[kSegRows1] : sg[kSegRows0]), 0);
-            bool ok;
-            if (cols == 16) ok = a8_stretch<E, D, 8>(p, sm, w, sg, item);
-            else if (cols == 32) ok = a8_stretch<E, D, 16>(p, sm, w, sg, item);
-            else if (cols == 48) ok = a8_stretch<E, D, 24>(p, sm, w, sg, item);
-            else ok = a8_stretch<E, D, 32>(p, sm, w, sg, item);
+            const bool ok = a8_stretch<E, D, N / 2>(p, sm, w, sg, item);
             if (!ok) break;
             tc_fence_before();
             __syncwarp();

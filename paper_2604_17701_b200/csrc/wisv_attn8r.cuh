@@ -17,6 +17,7 @@
 
 namespace wisv {
 
+constexpr int kR8Poly = 0;                       // pairs of every 8 whose exponentials are polynomials
 constexpr int kR8Small = 8 * 1024;
 constexpr int kR8Fixed = kA8Slack + kR8Small + kA8Scales * kA8ScaleBytes;            // shared memory beside queries and tiles
 
@@ -101,6 +102,16 @@ __device__ __forceinline__ void r8_cut_queries(const Attn8Params& p, int row0, i
     const int c = lane % L;
 #pragma unroll 1
     for (int r0 = 32 * w; r0 < 32 * w + 32; r0 += 4 * R) {
+        if (r0 >= rows) {                        // no such rows: zeros
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                for (int q = 0; q < NP; ++q)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(dst + q * (kAttnTile * D) + (r0 + u * R) * D + lane * 16), "r"(0) : "memory");
+                if (c == 0) rs[r0 + u * R + lane / L] = 0.0f;
+            }
+            continue;
+        }
         uint4 v[4][2];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -423,7 +434,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const uint64_t x = add2(pair(s[c + 2 * i], s[c + 2 * i + 1]), base2);
-                            y[i] = pair(attn_ex2(low(x)), attn_ex2(high(x)));
+                            y[i] = (c / 2 + i & 7) < kR8Poly ? exp2_poly2(x) : pair(attn_ex2(low(x)), attn_ex2(high(x)));
                             sum[i] = fma2(y[i], lds_pair(sc + 1024 + (c + 2 * i) * 4), sum[i]);
                         }
                         uint32_t e[NP];

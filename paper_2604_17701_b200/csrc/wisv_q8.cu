@@ -12,16 +12,21 @@
 
 namespace wisv {
 
+namespace {
+
+template <typename E, int D>
+bool prepare()
+{
+    auto set = [](const void* kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess; };
+    return set((const void*)attn8_kernel<E, D, 16>) && set((const void*)attn8_kernel<E, D, 32>) && set((const void*)attn8_kernel<E, D, 48>) &&
+           set((const void*)attn8_kernel<E, D, 64>) && set((const void*)attn8_rows_kernel<E, D>);
+}
+
+}  // namespace
+
 bool q8_prepare()
 {
-    return cudaFuncSetAttribute(attn8_kernel<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_rows_kernel<__nv_bfloat16, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_kernel<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_rows_kernel<__nv_bfloat16, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_kernel<__half, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_rows_kernel<__half, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess &&
-           cudaFuncSetAttribute(attn8_rows_kernel<__half, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAttnSmem) == cudaSuccess;
+    return prepare<__nv_bfloat16, 128>() && prepare<__nv_bfloat16, 64>() && prepare<__half, 128>() && prepare<__half, 64>();
 }
 
 }  // namespace wisv
@@ -71,22 +76,10 @@ int encode_codes(const wisv_cache* c, CUtensorMap* out, const void* base, int64_
     return r == CUDA_SUCCESS ? WISV_OK : WISV_EINVAL;
 }
 
-// Rows of a key head from which a window's rows are rows of the products, not columns.
-constexpr int kRowsFrom = 65;
-
 // Programmatic dependent launch: the block set-up (barriers, TMEM) runs while the kernel before it in the stream ends.
 template <typename E, int D>
 int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap& tmV, Attn8Params& p, cudaStream_t st)
 {
-    const int rows = p.tpt * p.group;
-    p.cols = a8_cols(rows);
-    p.q_bytes = (uint32_t)(a8_parts<E>::n * p.cols * D);
-    p.p_bytes = (uint32_t)a8_p_bytes<E>(p.cols);
-    // what is left of shared memory: stages of keys and values in even numbers; a value stage is held longer (behind the exponentials)
-    const int left = kAttnSmem - kA8Slack - kA8Small - kA8Scales * kA8ScaleBytes - 2 * (int)(p.q_bytes + p.p_bytes);
-    const int stages = left / (int)a8_tile_bytes<D>(), v = (stages + 2) / 4 * 2, k = (stages - (v < kA8Stages ? v : kA8Stages)) / 2 * 2;
-    p.v_stages = v < kA8Stages ? v : kA8Stages;
-    p.k_stages = k < kA8Stages ? k : kA8Stages;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -96,14 +89,26 @@ int launch_attn8(const wisv_cache* c, const CUtensorMap& tmK, const CUtensorMap&
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     cfg.gridDim = dim3((unsigned)c->sm_count);
-    cfg.blockDim = dim3(kA8Threads);
     cfg.dynamicSmemBytes = kAttnSmem;
+    const Attn8Params& q = p;
     if (p.rows) {
         cfg.blockDim = dim3(kAttnThreads);
-        WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_rows_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
-    } else {
-        WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_kernel<E, D>, tmK, tmV, (const Attn8Params&)p));
+        WISV_TRY_CUDA(cudaLaunchKernelEx(&cfg, attn8_rows_kernel<E, D>, tmK, tmV, q));
+        return WISV_OK;
     }
+    const int cols = a8_cols(p.tpt * p.group);
+    p.q_bytes = (uint32_t)(a8_parts<E>::n * cols * D);
+    p.p_bytes = (uint32_t)a8_p_bytes<E>(cols);
+    // what is left of shared memory: stages of keys and values in even numbers; a value stage is held longer (behind the exponentials)
+    const int left = kAttnSmem - kA8Slack - kA8Small - kA8Scales * kA8ScaleBytes - 2 * (int)(p.q_bytes + p.p_bytes);
+    const int stages = left / (int)a8_tile_bytes<D>(), v = (stages + 2) / 4 * 2, k = (stages - (v < kA8Stages ? v : kA8Stages)) / 2 * 2;
+    p.v_stages = v < kA8Stages ? v : kA8Stages;
+    p.k_stages = k < kA8Stages ? k : kA8Stages;
+    cfg.blockDim = dim3(kA8Threads);
+    WISV_TRY_CUDA(cols == 16   ? cudaLaunchKernelEx(&cfg, attn8_kernel<E, D, 16>, tmK, tmV, q)
+                  : cols == 32 ? cudaLaunchKernelEx(&cfg, attn8_kernel<E, D, 32>, tmK, tmV, q)
+                  : cols == 48 ? cudaLaunchKernelEx(&cfg, attn8_kernel<E, D, 48>, tmK, tmV, q)
+                               : cudaLaunchKernelEx(&cfg, attn8_kernel<E, D, 64>, tmK, tmV, q));
     return WISV_OK;
 }
 
@@ -206,7 +211,7 @@ int wisv_cache_attend_q8(wisv_cache* c, const wisv_q8_pages* pages, const wisv_q
     const int group = c->cfg.n_heads / c->cfg.n_kv_heads, D = c->cfg.head_dim;
     Attn8Params p;
     memset(&p, 0, sizeof p);
-    p.rows = (int64_t)a->max_new * group >= kRowsFrom;
+    p.rows = (int64_t)a->T * group > (int64_t)kA8Cols * a->B;
     const int tile = (p.rows ? kAttnTile : kA8Cols) / group;
     p.tpt = tile < a->max_new ? tile : a->max_new;
     // every key tile of every item has to count in 31 bits, whatever the lengths on the device say
