@@ -61,7 +61,8 @@ Q8Pages pools_of(const wisv_cache* c, const wisv_q8_pages* g)
 }
 
 // A pool of codes as (element, token of the page, key head, page): one box is one page (or 128 tokens of a larger one) of one head, a row per
-// token with the swizzle of its width.
+// token with the swizzle of its width.  (Fetched by 128 bytes: with 256 a pool with heads side by side gives twice what is asked for, one row each
+// of 64 requests over 270 k keys 152 instead of 116 us.)
 int encode_codes(const wisv_cache* c, CUtensorMap* out, const void* base, int64_t page, int64_t token, int64_t head)
 {
     const cuuint64_t D = (cuuint64_t)c->cfg.head_dim;
@@ -72,7 +73,7 @@ int encode_codes(const wisv_cache* c, CUtensorMap* out, const void* base, int64_
     const cuuint32_t one[4] = {1, 1, 1, 1};
     const CUresult r = c->encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, one,
                                  CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                                 CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? WISV_OK : WISV_EINVAL;
 }
 

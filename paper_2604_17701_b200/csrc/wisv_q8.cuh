@@ -15,7 +15,7 @@
 
 namespace wisv {
 
-constexpr int kQ8Threads = 256;
+constexpr int kQ8Threads = 128;
 
 struct Q8Pages {                                  // strides in 16-byte pieces of codes, in floats of scales
     uint4 *k, *v;
@@ -39,37 +39,43 @@ template <typename E, int L>
 __device__ __forceinline__ float q8_codes(const uint4 (&w)[2], uint4& out)
 {
     const uint32_t* v = reinterpret_cast<const uint32_t*>(w);
-    float x[16];
-    uint32_t top = 0;
+    // the largest magnitude: 16-bit numbers without their sign order as whole numbers, infinity and NaN last
+    uint32_t two = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        unpack2<E>(v[i], x[2 * i], x[2 * i + 1]);
-        top = max(top, max(__float_as_uint(x[2 * i]) & 0x7fffffffu, __float_as_uint(x[2 * i + 1]) & 0x7fffffffu));
-    }
+    for (int i = 0; i < 8; ++i) two = __vmaxu2(two, v[i] & 0x7fff7fffu);
+    uint32_t top = max(two >> 16, two & 0xffffu);
 #pragma unroll
     for (int o = 1; o < L; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const bool fine = top < 0x7f800000u;
-    const float t = __uint_as_float(top);
-    // (below 2^-100 both are scaled by 2^64, which is exact, so that the reciprocal stays finite)
-    const float up = top < 0x0d800000u ? 1.8446744e19f : 1.0f;
-    const float inv = fine && top ? __fdiv_rn(448.0f, t * up) : 0.0f;
-    uint32_t c[4];
+    const bool fine = top < (is_bf16<E>::value ? 0x7f80u : 0x7c00u);
+    float t, none;
+    unpack2<E>(top, t, none);
+    out = make_uint4(0, 0, 0, 0);
+    if (fine && top != 0) {
+        // (below 2^-100 both are scaled by 2^64, which is exact, so that the reciprocal stays finite)
+        const bool tiny = t < 7.888609e-31f;
+        const float inv = __fdiv_rn(448.0f, tiny ? t * 1.8446744e19f : t);
+        uint32_t c[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint16_t e[2];
+        for (int i = 0; i < 4; ++i) {
+            float x[4];
+            unpack2<E>(v[2 * i], x[0], x[1]);
+            unpack2<E>(v[2 * i + 1], x[2], x[3]);
+            if (tiny) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float y[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint32_t b = __float_as_uint(x[4 * i + 2 * h + k] * up * inv);
-                y[k] = fine ? __uint_as_float((b + 4u) & ~7u) : 0.0f;
+                for (int k = 0; k < 4; ++k) x[k] *= 1.8446744e19f;
             }
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(e[h]) : "f"(y[1]), "f"(y[0]));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] = __uint_as_float((__float_as_uint(x[k] * inv) + 4u) & ~7u);
+            asm("{\n\t"
+                ".reg .b16 e0, e1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f32 e0, %2, %1;\n\t"
+                "cvt.rn.satfinite.e4m3x2.f32 e1, %4, %3;\n\t"
+                "mov.b32 %0, {e0, e1};\n\t"
+                "}"
+                : "=r"(c[i]) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]));
         }
-        c[i] = static_cast<uint32_t>(e[0]) | static_cast<uint32_t>(e[1]) << 16;
+        out = make_uint4(c[0], c[1], c[2], c[3]);
     }
-    out = make_uint4(c[0], c[1], c[2], c[3]);
     return fine ? __fdiv_rn(t, 448.0f) : CUDART_NAN_F;
 }
 
@@ -84,11 +90,11 @@ __global__ void __launch_bounds__(kQ8Threads) append_q8_kernel(const Q8AppendPar
     griddep_wait();
     griddep_launch_dependents();
     const int x = static_cast<int>(i - t * p.vecs), h = x / L, e = x % L;
-    const int64_t slot = t < p.T ? p.slot_map[t] : -1;
-    const bool in = slot >= 0 && slot < p.pg.n_slots;             // (the same for the lanes of a head)
+    int64_t slot = -1;
     uint4 k[2], v[2];
     k[0] = k[1] = v[0] = v[1] = make_uint4(0, 0, 0, 0);
-    if (in) {
+    if (t < p.T) {                                                // (the rows are read whatever the slot, which comes beside them)
+        slot = p.slot_map[t];
         const uint4* a = p.k + t * p.kt + h * p.kh + 2 * e;
         const uint4* b = p.v + t * p.vt + h * p.vh + 2 * e;
         k[0] = a[0]; k[1] = a[1];
@@ -96,7 +102,7 @@ __global__ void __launch_bounds__(kQ8Threads) append_q8_kernel(const Q8AppendPar
     }
     uint4 kc, vc;
     const float ks = q8_codes<E, L>(k, kc), vs = q8_codes<E, L>(v, vc);
-    if (!in) return;
+    if (slot < 0 || slot >= p.pg.n_slots) return;
     const int64_t pg = slot >> p.pg.page_shift, o = slot & ((1 << p.pg.page_shift) - 1);
     p.pg.k[pg * p.pg.kp + o * p.pg.kt + h * p.pg.kh + e] = kc;
     p.pg.v[pg * p.pg.vp + o * p.pg.vt + h * p.pg.vh + e] = vc;
