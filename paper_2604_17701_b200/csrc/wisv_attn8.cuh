@@ -671,7 +671,10 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lb) : "r"(at + 512) : "memory");
             asm volatile("ld.shared.f32 %0, [%1];" : "=f"(rb) : "r"(at + 1024) : "memory");
         }
-        if (kCommon) ka *= common;
+        if (kCommon) {
+            ka *= common;
+            if (ka > 3.402823466e38f) ka = 3.402823466e38f;          // (times a column of zeros it must stay 0)
+        }
         const uint64_t ka2 = pair(ka, ka), lb2 = pair(lb, lb);
         const bool masked = key0 + kAttnTile - 1 > limit;
         if (!a8_wait<A8_AT(s_full)>(w.bars, w.jobs & 1u, w.flag)) return false;
