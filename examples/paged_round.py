@@ -11,9 +11,10 @@ sends K drafted tokens per round and the drafter's distribution; one round is
     PagedCache.commit          the kept lengths; pages of rejected drafts go back to the pool (a request that the pool had no
                                pages for keeps its old length)
 
-Lengths, verdicts and pages stay on the device; the host sees tokens only when it prints them.
+Lengths, verdicts and pages stay on the device; the host sees tokens only when it prints them.  With --cache-bits 8 keys and values are
+kept as e4m3 codes with a scale for each token and head (append_q8, attend_q8).
 
-    python examples/paged_round.py [--requests 4] [--rounds 6] [--drafts 5]
+    python examples/paged_round.py [--requests 4] [--rounds 6] [--drafts 5] [--cache-bits 16]
 """
 import argparse
 import os
@@ -59,7 +60,8 @@ class ToyTarget:
 class Server:
     """The target with its paged cache and the verifier; every method only enqueues work."""
 
-    def __init__(self, model, *, requests, drafts, page_size=16, max_tokens=256, drafter_hidden=64, seed=1):
+    def __init__(self, model, *, requests, drafts, page_size=16, max_tokens=256, drafter_hidden=64, seed=1,
+                 cache_bits=16):
         dev = model.device
         g = torch.Generator(device=dev)
         g.manual_seed(seed)
@@ -69,8 +71,11 @@ class Server:
                                      page_size=page_size, n_pages=requests * blocks, max_requests=requests,
                                      max_blocks=blocks, device=dev)
         shape = (requests * blocks, page_size, model.kv_heads, model.head_dim)
-        self.pools = [(torch.empty(shape, dtype=torch.bfloat16, device=dev), torch.empty(shape, dtype=torch.bfloat16, device=dev))
-                      for _ in model.qkv]
+        if cache_bits == 8:
+            self.pools = [self.cache.quant_pages() for _ in model.qkv]
+        else:
+            self.pools = [(torch.empty(shape, dtype=torch.bfloat16, device=dev), torch.empty(shape, dtype=torch.bfloat16, device=dev))
+                          for _ in model.qkv]
         vocab, hidden = model.lm_head.shape
         d_j, d_c = 128, 2
         w1 = (torch.randn((d_j, drafter_hidden + hidden + d_c), generator=g, device=dev) * 0.05).bfloat16()
@@ -81,6 +86,9 @@ class Server:
     def forward(self, tokens, layout, max_new):
         """The new tokens through all layers: their keys and values cached, their hidden states returned."""
         def attention(i, q, k, v):
+            if isinstance(self.pools[i], wisv.QuantPages):
+                self.cache.append_q8(k, v, self.pools[i], layout.slot_map)
+                return self.cache.attend_q8(q, self.pools[i], layout.kv_len, B=self.B, max_new=max_new, q_off=layout.q_off)
             k_pages, v_pages = self.pools[i]
             self.cache.append(k, v, k_pages, v_pages, layout.slot_map)
             return self.cache.attend(q, k_pages, v_pages, layout.kv_len, B=self.B, max_new=max_new, q_off=layout.q_off)
@@ -123,12 +131,12 @@ class Server:
         self.cache.close()
 
 
-def serve(requests=4, rounds=6, drafts=5, seed=0, semantic=True, device="cuda:0"):
+def serve(requests=4, rounds=6, drafts=5, seed=0, semantic=True, device="cuda:0", cache_bits=16):
     """Runs the rounds and returns (server, the tokens of each request, tokens accepted per round)."""
     g = torch.Generator(device=device)
     g.manual_seed(seed)
     model = ToyTarget(device=device)
-    server = Server(model, requests=requests, drafts=drafts)
+    server = Server(model, requests=requests, drafts=drafts, cache_bits=cache_bits)
     vocab = model.embed.shape[0]
     lengths = [7 + 9 * b for b in range(requests)]
     text = [torch.randint(0, vocab, (n,), generator=g, device=device, dtype=torch.int32) for n in lengths]
@@ -156,8 +164,9 @@ def main():
     ap.add_argument("--requests", type=int, default=4)
     ap.add_argument("--rounds", type=int, default=6)
     ap.add_argument("--drafts", type=int, default=5)
+    ap.add_argument("--cache-bits", type=int, default=16, choices=(16, 8))
     a = ap.parse_args()
-    server, text, accepted = serve(a.requests, a.rounds, a.drafts)
+    server, text, accepted = serve(a.requests, a.rounds, a.drafts, cache_bits=a.cache_bits)
     print("accepted drafts per round (rows) and request (columns; -1: no pages):\n%s" % accepted.cpu())
     print("kept tokens %s, free pages %d of %d" % (server.cache.seq_len.tolist(), server.cache.n_free.item(),
                                                    server.cache.n_pages))

@@ -193,7 +193,8 @@ def _owned_array(i):
 
 
 class PagedCache:
-    """wisv_cache_* on torch CUDA tensors: the paged key/value cache of a target model.
+    """wisv_cache_* on torch CUDA tensors: the paged key/value cache of a target model, in 16 bits (append, attend) or, with pools of
+    quant_pages, in 8 (append_q8, attend_q8, read_q8).
 
     The bookkeeping tensors (``free_list``, ``n_free``, ``block_table``, ``n_blocks``, ``seq_len``) are ordinary int32
     tensors of this object, with every page free at the start, to be written in place, not replaced.  The page pools of each
@@ -422,9 +423,14 @@ class PagedCache:
         made = out is None
         if made:
             both = _empty(self._torch, stream, (2, T, kv, self.head_dim), self.dtype, self.device)
-            out = tuple(both.unbind(0))
-        kp, kt, kh, _ = self._rows("out[0]", out[0], kv, T)
-        vp, vt, vh, _ = self._rows("out[1]", out[1], kv, T)
+            out = both.unbind(0)
+            kt = vt = kv * self.head_dim
+            kh = vh = self.head_dim
+            kp = both.data_ptr()
+            vp = kp + 2 * T * kt
+        else:
+            kp, kt, kh, _ = self._rows("out[0]", out[0], kv, T)
+            vp, vt, vh, _ = self._rows("out[1]", out[1], kv, T)
         table, step, blocks = self._table(block_table, B)
         self._call("wisv_cache_read_q8", stream, self._q8(pages),
                    _pack_q8_read(B, T, 0 if n is None else n, 0 if off is None else _array("off", off, i32, B + 1, dev),
