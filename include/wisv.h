@@ -603,11 +603,13 @@ int wisv_cache_read_q8(wisv_cache* cache, const wisv_q8_pages* pages, const wisv
 
 /*
  * wisv_cache_attend over 8-bit pools: the same rows, masks, lse, rows without a key, rows of no window and work hint.  The codes are operands of
- * the matrix products as they are and scales enter in fp32; queries and probabilities enter with the precision of the cache's
- * type, down to 2^-18 of a query's (2^-16 of the probabilities') largest element.  A score of +inf or NaN makes its row and lse NaN, and so does a token
- * whose scale is NaN, in the rows that see it.  Codes of the tokens that rows see are numbers (wisv_cache_append_q8 writes no other): the code of
- * NaN in a window may reach each of its rows.  Codes and scales past kv_len[b], and pages that the table does not reach, may
- * hold anything.  Scales of values count as at least 2^-100, and as 2^-40 of the largest among the 32 tokens around them.
+ * the matrix products as they are and scales enter in fp32.  Queries enter with the precision of the cache's type down to 2^-17 of the largest
+ * element among the queries of a request and key head; probabilities are rounded to that type, down to 2^-14 of the largest product of a
+ * row's probabilities and their tokens' value scales.  A score of +inf or NaN makes its row and lse NaN, and so does a token whose scale
+ * is NaN (a value scale: or negative), in the rows that see it.  Codes of the tokens that rows see are numbers (wisv_cache_append_q8 writes no other): the code
+ * of NaN in a window may reach each of its rows.  Codes and scales past kv_len[b], and pages that the table does not reach, may hold
+ * anything; tokens whose table entry lies outside the pool count as zeros.  Value scales count as at least 2^-100, and as 2^-40 of the largest
+ * among the 128 tokens of a tile.
  */
 typedef struct {
     int32_t B;

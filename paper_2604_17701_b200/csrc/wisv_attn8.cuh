@@ -10,14 +10,17 @@
 //
 // 8-bit operands without a loss.  The codes are operands of the products as they are.  The other operand is cut into e4m3 parts: a number's
 // nearest e4m3 number, the nearest to what is left, and so on; each part takes 4 bits and the sign of the rest one more, so two parts carry
-// the 8 bits of a bf16 and three the 11 of an fp16 number, above a floor.  Queries are scaled by a power of two to a largest element in
-// [128, 256); a last part's half step of 2^-10 is 2^-17 of a row's largest element at most.  Each further part of P is scaled up by 16 (its
-// sums are kept apart until the end), so that with a largest P of 4 or more the half step is 2^-16 of it, 2^-20 with three parts.  The
-// products are exact, sums are fp32.  (P is rounded to fp16 on the way, then to 9 bits where queries are bf16: half the error of a bf16 P.)  The
-// parts lie side by side as columns, [part][column], so that a tile of K or V is read once for all of them.
+// the 8 bits of a bf16 and three the 11 of an fp16 number, above a floor: the last part's half step, 2^-10.  The parts lie side by side as columns,
+// [part][column], so that a tile of K or V is read once for all of them, and each further part is scaled up by 16, since its sums are
+// kept apart until they are read.  Queries share a power of two that brings the tile's largest element to [128, 256): the floor is 2^-21 of that element.  (Where
+// three parts of S do not fit TMEM side by side they are added in one accumulator, unscaled: then every row has its own power of two, and the
+// floor is 2^-17 of the row's largest element.)  P is rounded to fp16 on the way, then to 9 bits where queries are bf16, half the error of a bf16 P;
+// its floor is 2^-14 (three parts: 2^-17) of its largest.  The products are exact, sums are fp32.
 //
-// References.  m grows only when a column's x passes 8.75 (P must stay below 448, the largest e4m3 number), then to the column's largest
-// minus 2; l and O are scaled with it.  One vote of a slot's warps per tile says whether any column has to.
+// References.  m grows only when a column's x passes 8.75 (P must stay below 448, the largest e4m3 number), then to the column's largest (one more
+// where there are three parts, whose floor leaves room); l and O are scaled with it.  One vote of a slot's warps per tile says whether any
+// column has to, and columns that have doubled follow.  (With 2^2 below the largest instead, half of the tiles of a prompt chunk grew some
+// column: 1267 us instead of 1077.)
 //
 // What does not reach a column.  Masked keys have x = -inf and P = 0 exactly.  V behind the last key of a request is cleared in shared memory,
 // since 0 times a code of NaN is NaN.  A scale of NaN (a token with infinite or NaN elements) makes x, and so the columns that see
@@ -30,6 +33,15 @@
 // work item is "paired" - two tiles of columns of the same (request, key head), one per slot, sharing every tile of keys - or, where one
 // tile of columns is left, "split": the slots take the key tiles in turn and are put together at the end.  The line of key tiles, its cut
 // over the blocks and the joining of shared items are those of the 16-bit cache (wisv_attn.cuh).
+//
+// What bounds it.  A tile of 128 keys has 2 * 128 D bytes, some 1400 clocks at a 148th of the measured copy rate (D = 128), and with keys as the
+// rows its products take 32 + columns / 4 clocks per 32 of the inner dimension, what their operands take through shared memory: 320 clocks at
+// 16 query rows, 1030 at 64.  One row per request is bound by HBM; from some 32 rows on by the instructions of the softmax warps (some 540 for 32 columns
+// of a tile, half of them for waits, votes and addresses).
+//
+// Measured (8B shape: 32 query heads, 8 key heads, D = 128, pools with heads first; short runs): 64 requests of one row over 514 k keys
+// 172 us, 6.3 TB/s, 0.96 of the copy rate; of 4, 8, 9 and 16 rows over 270 k keys 102, 114, 131 and 153 us (5.6 to 3.8 TB/s); one
+// row over 131 k keys 54 us; one request of 9 rows over 709 keys 14.2 us, of which 3 us are the walk's first lookups, 1.5 the queries and 2 the merge.
 #pragma once
 
 #include <stddef.h>
@@ -46,8 +58,10 @@ constexpr int kA8Small = 9 * 1024;               // barriers, queue, tables of c
 constexpr int kA8Slack = 1024;
 constexpr int kA8SoftWarps = 16;                 // eight per slot
 constexpr int kA8Threads = 256 + 32 * kA8SoftWarps;
-constexpr int kA8ItemCost = 8;                   // (see kAttnItemCost) key tiles that starting and finishing an item is worth
-constexpr float kA8Grow = 8.75f;
+// Key tiles that starting and finishing an item is worth.  (With 1, 5, 8, 12: decoding 64 requests over 514 k keys 212, 173, 173, 176 us; windows
+// of 5 to 17 rows over 270 k keys -, 175, 167, 171.)
+constexpr int kA8ItemCost = 8;
+constexpr float kA8Grow = 8.75f;                 // log2 of 430
 template <typename E> __host__ __device__ constexpr float a8_room() { return is_bf16<E>::value ? 0.0f : -1.0f; }
 constexpr float kA8Step = 16.0f;                 // from one part to the next
 
@@ -62,8 +76,8 @@ struct Attn8Params : AttnParams {
 
 template <typename E> struct a8_parts { static constexpr int n = is_bf16<E>::value ? 2 : 3; };
 
-// TMEM: 256 columns a slot, O behind S.  O has columns for each part, so that V is read once for all of them (a product whose operand has to be
-// turned takes 73 clocks whatever its columns, 16 to 64) and that the parts can have scales of their own; S too where that fits.
+// TMEM: 256 columns a slot, O behind S.  O has columns for each part, so that V is read once for all of them and that the parts can have scales of
+// their own; S too where that fits.
 template <typename E> __host__ __device__ constexpr int a8_o_at() { return 256 - kA8Cols * a8_parts<E>::n; }
 template <typename E> __host__ __device__ constexpr bool a8_s_stacked(int cols) { return a8_parts<E>::n * cols <= a8_o_at<E>(); }
 // bytes of a slot's P: 64 columns of 128 keys in a piece
@@ -565,7 +579,7 @@ __device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int hea
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float be = fmaxf(b[i], least);
-            lb[i] = b[i] == b[i] ? attn_lg2(be) : CUDART_NAN_F;
+            lb[i] = b[i] >= 0.0f ? attn_lg2(be) : CUDART_NAN_F;
             b[i] = attn_rcp(be);
         }
         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(src), "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]) : "memory");
@@ -733,13 +747,8 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                 continue;
             }
             // ---- the references grow
-            float keep = 0.0f;
 #pragma unroll
-            for (int n = 0; n < C; ++n) {
-                const float r = warp_max_nan(x[n]);
-                if (n == w.lane) keep = r;
-            }
-            if (w.lane < C) sm->mx[slot][w.quad][col0 + w.lane] = keep;
+            for (int n = 0; n < C; ++n) sm->mx[slot][w.quad][col0 + n] = warp_max_nan(x[n]);
             if (!vote()) return false;
             if (ts < N) {
                 const float (&mx)[4][kA8Cols] = sm->mx[slot];

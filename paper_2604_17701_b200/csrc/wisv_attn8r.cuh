@@ -8,16 +8,20 @@
 // largest element of a query row in [128, 256) two parts are exact for bf16 and three for fp16 down to 2^-24 of it; a P, whose largest is
 // 1 or more, is rounded to fp16 and then to 8 bits (bf16) or not at all (fp16), down to 2^-17.
 //
-// Measured against the kernel with keys as rows: it needs a thread per row whether the row exists or not, but no meeting of warps, no
-// tables of columns and half of the instructions per element.  The roles are those of wisv_attn8.cuh, the slots, the work line and the
-// merge those of wisv_attn.cuh.
+// Against the kernel with keys as rows it needs a thread per row whether the row exists or not, but no meeting of warps, no tables of columns and half
+// of the instructions per element: 64 requests of 16, 17 and 24 rows of 4 heads over 270 k keys take 217, 223 and 223 us here and 153,
+// 354 and 244 there, where 17 tokens are two tiles.  Hence the rule: more than 64 rows to a request on the average.  The roles are
+// those of wisv_attn8.cuh, slots and merge those of wisv_attn.cuh.
+//
+// Measured (8B shape, D = 128, short runs): 2 x 2048 rows over 8 k keys 698 us, 0.78 PFLOP/s of the formula's (each product is done twice, a
+// part at a time); 8 requests of 65 rows of 7 heads over 120 k keys 175 us.  What bounds it: two softmax warps on each scheduler, which issue half of the
+// time (exponentials and cutting 1240 of 2760 clocks per 64 keys, scores 660, the rest waits); the tensor pipe is active 36 %.
 #pragma once
 
 #include "wisv_attn8.cuh"
 
 namespace wisv {
 
-constexpr int kR8Poly = 0;                       // pairs of every 8 whose exponentials are polynomials
 constexpr int kR8Small = 8 * 1024;
 constexpr int kR8Fixed = kA8Slack + kR8Small + kA8Scales * kA8ScaleBytes;            // shared memory beside queries and tiles
 
@@ -434,7 +438,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             const uint64_t x = add2(pair(s[c + 2 * i], s[c + 2 * i + 1]), base2);
-                            y[i] = (c / 2 + i & 7) < kR8Poly ? exp2_poly2(x) : pair(attn_ex2(low(x)), attn_ex2(high(x)));
+                            y[i] = pair(attn_ex2(low(x)), attn_ex2(high(x)));
                             sum[i] = fma2(y[i], lds_pair(sc + 1024 + (c + 2 * i) * 4), sum[i]);
                         }
                         uint32_t e[NP];

@@ -212,11 +212,12 @@ int wisv_cache_attend_q8(wisv_cache* c, const wisv_q8_pages* pages, const wisv_q
     const int group = c->cfg.n_heads / c->cfg.n_kv_heads, D = c->cfg.head_dim;
     Attn8Params p;
     memset(&p, 0, sizeof p);
+    // rows of a request as rows of the products where they are more than a tile's columns on the average (wisv_attn8r.cuh has both sides' figures)
     p.rows = (int64_t)a->T * group > (int64_t)kA8Cols * a->B;
     const int tile = (p.rows ? kAttnTile : kA8Cols) / group;
     p.tpt = tile < a->max_new ? tile : a->max_new;
-    // every key tile of every item has to count in 31 bits, whatever the lengths on the device say
-    const int64_t items = (a->T + p.tpt - 1) / p.tpt + a->B, tiles = ((int64_t)a->max_blocks << c->page_shift) / kAttnTile + 2;
+    // every unit of every item has to count in 31 bits, whatever the lengths on the device say
+    const int64_t items = (a->T + p.tpt - 1) / p.tpt + a->B, tiles = ((int64_t)a->max_blocks << c->page_shift) / kAttnTile + 2 + kA8ItemCost;
     if (items * tiles > 0x7ffe0000LL / c->cfg.n_kv_heads) return WISV_ESHAPE;
     p.B = a->B; p.T = a->T; p.n_kv = c->cfg.n_kv_heads; p.group = group;
     p.page_shift = c->page_shift; p.n_pages = c->cfg.n_pages; p.max_blocks = a->max_blocks;
