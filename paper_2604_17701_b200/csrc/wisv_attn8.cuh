@@ -204,6 +204,52 @@ template <typename E> __device__ __forceinline__ E a8_round(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 a8_round<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half a8_round<__half>(float x) { return __float2half_rn(x); }
 
+// Waits and arrivals of whole warps, on a barrier OFF bytes behind `base`.  A wait for a barrier that is complete is a try, a vote and a branch
+// that the warp takes as one; an arrival is one predicated instruction.  (As calls of attn_wait they were two fifths of a tile's
+// instructions, and their loops, one to each place, a twentieth of the time: 24 warps in eight roles share the caches of instructions.)
+// `flag`: see attn_wait.
+template <int OFF>
+__device__ __forceinline__ bool a8_try(uint32_t base, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1 + %3], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "}\n"
+        : "=r"(ok) : "r"(base), "r"(parity), "n"(OFF) : "memory");
+    return __all_sync(0xffffffffu, ok);
+}
+template <int OFF>
+__device__ __forceinline__ bool a8_wait(uint32_t base, uint32_t parity, uint32_t flag)
+{
+    if (a8_try<OFF>(base, parity)) return true;
+    const uint32_t t0 = static_cast<uint32_t>(clock64() >> 10);
+#pragma unroll 1
+    for (;;) {
+        if (a8_try<OFF>(base, parity)) return true;
+        uint32_t stop, limit;
+        asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(stop) : "r"(flag) : "memory");
+        asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(limit) : "r"(flag + 12u) : "memory");
+        if (static_cast<uint32_t>(clock64() >> 10) - t0 > limit) {
+            asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(flag), "r"(1) : "memory");
+            stop = 1;
+        }
+        if (__any_sync(0xffffffffu, stop)) return false;
+    }
+}
+template <int OFF>
+__device__ __forceinline__ void a8_arrive(uint32_t base, int lane)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.eq.s32 p, %1, 0;\n\t"
+        "@p mbarrier.arrive.shared::cta.b64 _, [%0 + %2];\n\t"
+        "}\n"
+        ::"r"(base), "r"(lane), "n"(OFF) : "memory");
+}
 // A ring of `n` stages (n even), walked one or two entries at a time.  Slots of a split item take the tiles by the parity of their number, so
 // the fill before the one that a warp waits for is of a tile that the same warp has seen: a barrier's one phase bit is enough.
 struct A8Ring {
@@ -261,7 +307,7 @@ __device__ __forceinline__ bool a8_load_tiles(const Attn8Params& p, const CUtens
         const int at = (tok0 + lane * box_tok) & ((1 << p.page_shift) - 1);
         const int g = pg >= 0 && pg < p.n_pages ? pg : p.n_pages;                                   // out of range: zeros
         pg = attn_page(p, req, t + 1, t1, keys, lane);
-        if (!attn_wait_warp(empty + 8u * rg.s, rg.ph ^ 1u, flag)) return false;
+        if (!a8_wait<0>(empty + 8u * rg.s, rg.ph ^ 1u, flag)) return false;
         const uint32_t dst = ring + rg.s * a8_tile_bytes<D>(), bar = full + 8u * rg.s;
         if (elect_one()) mbar_expect_tx(bar, static_cast<uint32_t>(pages) * box_bytes);
         __syncwarp();
@@ -556,7 +602,7 @@ __device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int hea
             const bool in = pg >= 0 && pg < p.n_pages;
             const int o = in ? (t * kAttnTile + 4 * lane) & mask : 0, from = in ? pg : 0;
             pg = page(t + 1);
-            if (!attn_wait_warp(smem_u32(&sm->sc_empty[at.s]), at.ph ^ 1u, flag)) return false;
+            if (!a8_wait<0>(smem_u32(&sm->sc_empty[at.s]), at.ph ^ 1u, flag)) return false;
             const uint32_t dst = ring + at.s * kA8ScaleBytes + lane * 16;
             cp_async16(dst, p.ks + from * p.ksp + head * p.ksh + o, in ? 16 : 0);
             cp_async16(dst + 512, p.vs + from * p.vsp + head * p.vsh + o, in ? 16 : 0);
@@ -592,33 +638,6 @@ __device__ __forceinline__ bool a8_scales(const Attn8Params& p, int req, int hea
     return true;
 }
 
-// Waits and arrivals of the softmax warps, on a barrier OFF bytes behind `base`.  A wait for a barrier that is complete is a try, a vote and a branch
-// that the warp takes as one; an arrival is one predicated instruction.  (They were two fifths of a tile's instructions as calls of the general forms.)
-template <int OFF>
-__device__ __forceinline__ bool a8_wait(uint32_t base, uint32_t parity, uint32_t flag)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1 + %3], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t"
-        "}\n"
-        : "=r"(ok) : "r"(base), "r"(parity), "n"(OFF) : "memory");
-    if (__all_sync(0xffffffffu, ok)) return true;
-    return __all_sync(0xffffffffu, attn_wait_slow(base + OFF, parity, flag));
-}
-template <int OFF>
-__device__ __forceinline__ void a8_arrive(uint32_t base, int lane)
-{
-    asm volatile(
-        "{\n\t"
-        ".reg .pred p;\n\t"
-        "setp.eq.s32 p, %1, 0;\n\t"
-        "@p mbarrier.arrive.shared::cta.b64 _, [%0 + %2];\n\t"
-        "}\n"
-        ::"r"(base), "r"(lane), "n"(OFF) : "memory");
-}
 #define A8_AT(member) static_cast<int>(offsetof(A8Small, member))
 
 // What a softmax warp carries from stretch to stretch
@@ -1043,7 +1062,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                         s[kSegFirst] = first; s[kSegParts] = last - first + 1;
                     }
                 }
-                ok = attn_wait_warp(bar(sm->seg_empty[qi]), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
+                ok = a8_wait<0>(bar(sm->seg_empty[qi]), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
                 if (!ok) break;
                 if (lane == 0) {
 #pragma unroll
@@ -1062,7 +1081,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             bool ok = warp != 7 || static_cast<int>(me) != p.stalled;
             for (int item = 0; ok; ++item) {
                 const int qi = item & (kSegQueue - 1);
-                ok = attn_wait_warp(bar(sm->seg_full[qi]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+                ok = a8_wait<0>(bar(sm->seg_full[qi]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
                 if (!ok) break;
                 const int* const sg = sm->queue[qi];
                 if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;           // (the compiler then knows it uniform)
@@ -1081,15 +1100,15 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                     constexpr int kSParts = a8_s_stacked<E>(N) ? 1 : NP;             // products of S
                     const uint32_t sS = tmem + slot * 256, sO = sS + a8_o_at<E>();
                     const uint32_t idesc = second ? a8_idesc(D, NP * N, true) : a8_idesc(kAttnTile, kSParts == 1 ? NP * N : N, false);
-                    ok = second ? item == 0 || attn_wait_warp(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
-                                : attn_wait_warp(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
+                    ok = second ? item == 0 || a8_wait<0>(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
+                                : a8_wait<0>(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
                     const int i0 = paired ? 0 : static_cast<int>((tiles ^ static_cast<uint32_t>(slot)) & 1u), step = paired ? 1 : 2;
                     A8Ring r = rg;
                     if (i0) r.step(stages, 1);
                     for (int i = i0; ok && i < nt; i += step, ++jobs) {
                         if (!second) {
-                            ok = attn_wait_warp(bar(sm->s_free[slot]), (jobs & 1u) ^ 1u, flag);
-                            if (ok) ok = attn_wait_warp(bar(sm->k_full[r.s]), r.ph, flag);
+                            ok = a8_wait<0>(bar(sm->s_free[slot]), (jobs & 1u) ^ 1u, flag);
+                            if (ok) ok = a8_wait<0>(bar(sm->k_full[r.s]), r.ph, flag);
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
@@ -1104,8 +1123,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                                 if (!paired) umma_commit(bar(sm->k_empty[r.s]));
                             }
                         } else {
-                            ok = attn_wait_warp(bar(sm->v_full[r.s]), r.ph, flag);
-                            if (ok) ok = attn_wait_warp(bar(sm->p_full[slot]), jobs & 1u, flag);
+                            ok = a8_wait<0>(bar(sm->v_full[r.s]), r.ph, flag);
+                            if (ok) ok = a8_wait<0>(bar(sm->p_full[slot]), jobs & 1u, flag);
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
@@ -1143,7 +1162,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         for (uint32_t item = 0; ; ++item) {
             const int qi = item & (kSegQueue - 1);
             const int* const sg = sm->queue[qi];
-            if (!attn_wait_warp(bar(sm->seg_full[qi]), (item / kSegQueue) & 1u, flag)) break;
+            if (!a8_wait<0>(bar(sm->seg_full[qi]), (item / kSegQueue) & 1u, flag)) break;
             if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;
             const bool ok = a8_stretch<E, D, N / 2>(p, sm, w, sg, item);
             if (!ok) break;
@@ -1156,7 +1175,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                 const int first_block = sg[kSegFirst], parts = sg[kSegParts];
                 if (lane == 0) mbar_arrive(bar(sm->part_full));
                 if (warp == 8) {
-                    if (!attn_wait_warp(bar(sm->part_full), splits & 1u, flag)) break;
+                    if (!a8_wait<0>(bar(sm->part_full), splits & 1u, flag)) break;
                     if (lane == 0) {
                         const int shift = sg[kSegShift];
                         __threadfence();
@@ -1168,7 +1187,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                     }
                     __syncwarp();
                 }
-                if (!attn_wait_warp(bar(sm->last_full), splits & 1u, flag)) break;
+                if (!a8_wait<0>(bar(sm->last_full), splits & 1u, flag)) break;
                 ++splits;
                 if (__shfl_sync(0xffffffffu, *const_cast<volatile int32_t*>(&sm->came_last), 0)) a8_merge<E, D>(p, sg, warp - 8, lane);
             }

@@ -249,7 +249,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                         s[kSegFirst] = first; s[kSegParts] = last - first + 1;
                     }
                 }
-                ok = attn_wait_warp(bar(sm->seg_empty[qi]), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
+                ok = a8_wait<0>(bar(sm->seg_empty[qi]), (static_cast<uint32_t>(item / kSegQueue) & 1u) ^ 1u, flag);
                 if (!ok) break;
                 if (lane == 0) {
 #pragma unroll
@@ -268,7 +268,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             bool ok = warp != 7 || static_cast<int>(me) != p.stalled;
             for (int item = 0; ok; ++item) {
                 const int qi = item & (kSegQueue - 1);
-                ok = attn_wait_warp(bar(sm->seg_full[qi]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+                ok = a8_wait<0>(bar(sm->seg_full[qi]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
                 if (!ok) break;
                 const int* const sg = sm->queue[qi];
                 const int tiles = __shfl_sync(0xffffffffu, sg[kSegJobs], 0);         // (the compiler then knows it uniform)
@@ -286,15 +286,15 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                     const bool second = warp > 4;
                     const uint32_t sS = tS + slot * 128, sO = tO + slot * 128;
                     const int J = paired ? 2 * tiles : tiles;
-                    ok = second ? item == 0 || attn_wait_warp(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
-                                : attn_wait_warp(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
+                    ok = second ? item == 0 || a8_wait<0>(bar(sm->o_empty), static_cast<uint32_t>(item - 1) & 1u, flag)      // the previous O has been read
+                                : a8_wait<0>(bar(sm->q_full[slot]), static_cast<uint32_t>(item) & 1u, flag);
                     for (int n = 0; ok && n < J; ++n, ++used) {
                         const uint32_t h = used & 1u, ph = (used >> 1) & 1u;
                         const bool first_use = !paired || (n & 1) == 0, last_use = !paired || (n & 1) == 1;
                         const uint32_t keys_at = (paired ? (n & 1) : slot) * (kAttnSub * D);
                         if (!second) {
-                            ok = attn_wait_warp(bar(sm->s_free[2 * h + slot]), ph ^ 1u, flag);
-                            if (ok && first_use) ok = attn_wait_warp(bar(sm->k_full[rg.s]), rg.ph, flag);
+                            ok = a8_wait<0>(bar(sm->s_free[2 * h + slot]), ph ^ 1u, flag);
+                            if (ok && first_use) ok = a8_wait<0>(bar(sm->k_full[rg.s]), rg.ph, flag);
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
@@ -309,8 +309,8 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                                 if (last_use) umma_commit(bar(sm->k_empty[rg.s]));
                             }
                         } else {
-                            if (first_use) ok = attn_wait_warp(bar(sm->v_full[rg.s]), rg.ph, flag);
-                            if (ok) ok = attn_wait_warp(bar(sm->p_full[2 * h + slot]), ph, flag);
+                            if (first_use) ok = a8_wait<0>(bar(sm->v_full[rg.s]), rg.ph, flag);
+                            if (ok) ok = a8_wait<0>(bar(sm->p_full[2 * h + slot]), ph, flag);
                             if (!ok) break;
                             tc_fence_after();
                             if (elect_one()) {
@@ -349,7 +349,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         bool ok = true;
         for (int item = 0; ok; ++item) {
             const int* const sg = sm->queue[item & (kSegQueue - 1)];
-            ok = attn_wait_warp(bar(sm->seg_full[item & (kSegQueue - 1)]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
+            ok = a8_wait<0>(bar(sm->seg_full[item & (kSegQueue - 1)]), static_cast<uint32_t>(item / kSegQueue) & 1u, flag);
             if (!ok) break;
             if (__shfl_sync(0xffffffffu, sg[kSegJobs], 0) == 0) break;
             const bool paired = sg[kSegPaired];
@@ -374,10 +374,10 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 const int sub = paired ? n & 1 : slot;
                 const bool first_use = !paired || sub == 0, last_use = !paired || sub == 1;
                 if (first_use) {
-                    ok = attn_wait_warp(bar(sm->sc_full[rsc.s]), rsc.ph, flag);
+                    ok = a8_wait<0>(bar(sm->sc_full[rsc.s]), rsc.ph, flag);
                     if (!ok) break;
                 }
-                ok = attn_wait_warp(bar(sm->s_full[2 * h + slot]), (used >> 1) & 1u, flag);
+                ok = a8_wait<0>(bar(sm->s_full[2 * h + slot]), (used >> 1) & 1u, flag);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t aS = aS0 + h * kAttnSub, sc = ring_sc + rsc.s * kA8ScaleBytes + sub * (kAttnSub * 4);
@@ -414,7 +414,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                         m = m_new;
                         if (n > 0) {
                             // O holds the jobs up to the last but one for certain; its rescaling waits for that one too
-                            ok = attn_wait_warp(bar(sm->s_free[2 * (h ^ 1u) + slot]), ((used - 1) >> 1) & 1u, flag);
+                            ok = a8_wait<0>(bar(sm->s_free[2 * (h ^ 1u) + slot]), ((used - 1) >> 1) & 1u, flag);
                             if (!ok) break;
                             tc_fence_after();
 #pragma unroll
@@ -455,7 +455,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 if (have < kAttnSub) {
                     // V behind the last key is cleared.  (Both slots of a paired item do: whoever comes second writes zeros over zeros.  The
                     // stage cannot be recycled before this job's second product.)
-                    ok = attn_wait_warp(bar(sm->v_full[rv.s]), rv.ph, flag);
+                    ok = a8_wait<0>(bar(sm->v_full[rv.s]), rv.ph, flag);
                     if (!ok) break;
                     for (int i = row + max(have, 0) * (D / 16); i < kAttnSub * (D / 16); i += 128)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring_v + rv.s * kTile + sub * (kAttnSub * D) + i * 16), "r"(0) : "memory");
@@ -477,14 +477,14 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             // ---- the item (or its stretch) is done once O is complete (which also says that nobody reads the previous
             // stretch's m and l any more).  The slots' (m, l) are exchanged: a split item is put together here from both
             // accumulators, each slot taking half of the columns.
-            ok = attn_wait_warp(bar(sm->o_full), static_cast<uint32_t>(item) & 1u, flag);
+            ok = a8_wait<0>(bar(sm->o_full), static_cast<uint32_t>(item) & 1u, flag);
             if (!ok) break;
             tc_fence_after();
             if (m == -CUDART_INF_F && l == l) l = 0.0f;                              // the row has seen no key (and no NaN)
             sm->ml[slot][row] = make_float2(m, l);
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(sm->ml_full));
-            ok = attn_wait_warp(bar(sm->ml_full), static_cast<uint32_t>(item) & 1u, flag);
+            ok = a8_wait<0>(bar(sm->ml_full), static_cast<uint32_t>(item) & 1u, flag);
             if (!ok) break;
             if (warp_has_rows) {
                 float wa = 1.0f, wb = 0.0f;      // weights of this slot's accumulator and of the other one's
@@ -546,7 +546,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 const int first_block = sg[kSegFirst], parts = sg[kSegParts];
                 if (lane == 0) mbar_arrive(bar(sm->part_full));
                 if (warp == 8) {
-                    ok = attn_wait_warp(bar(sm->part_full), splits & 1u, flag);
+                    ok = a8_wait<0>(bar(sm->part_full), splits & 1u, flag);
                     if (!ok) break;
                     if (lane == 0) {
                         const int shift = sg[kSegShift];
@@ -559,7 +559,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                     }
                     __syncwarp();
                 }
-                ok = attn_wait_warp(bar(sm->last_full), splits & 1u, flag);
+                ok = a8_wait<0>(bar(sm->last_full), splits & 1u, flag);
                 if (!ok) break;
                 ++splits;
                 if (__shfl_sync(0xffffffffu, *const_cast<volatile int32_t*>(&sm->came_last), 0)) attn_merge<E, D>(p, sg, warp - 8, lane);

@@ -240,6 +240,8 @@ SHAPES = {
     "chunk fp16": ([515], [777], 8, 1, 128, 128, "fp16", False),
     "chunk of few keys": ([300], [120], 8, 2, 64, 16, "bf16", True),
     "batch": ([1] * 70, list(range(0, 1400, 20)), 16, 4, 128, 16, "bf16", True),
+    "a long window among single tokens": ([1] * 40 + [300, 0, 90] + [1] * 50, [30 + 7 * i for i in range(40)] + [1000, 5, 90] + [200] * 50, 8, 2, 128, 16, "bf16", True),
+    "a thousand requests": ([1] * 1000, [1 + i % 150 for i in range(1000)], 2, 1, 64, 16, "fp16", True),
     "large batch": ([2] * 300, [64 + i for i in range(300)], 4, 2, 64, 32, "fp16", True),
 }
 
