@@ -30,6 +30,7 @@ struct R8Small {
     uint64_t sc_full[kA8Scales], sc_empty[kA8Scales];
     uint64_t q_full[2], s_full[4], p_full[4], s_free[4];             // slots; 2 half + slot
     uint64_t seg_full[kSegQueue], seg_empty[kSegQueue];
+    uint64_t turn[2][4];                         // at the exponentials: of slots, for the two warps of a scheduler
     uint64_t o_full, o_empty, ml_full, part_full, last_full, drain[4];
     uint32_t tmem;
     uint32_t abort[2];                           // [1] is for the waits after a time-out
@@ -196,6 +197,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         for (int s = 0; s < kSegQueue; ++s) { mbar_init(bar(sm->seg_full[s]), 1); mbar_init(bar(sm->seg_empty[s]), 14); }
         mbar_init(bar(sm->o_full), 2); mbar_init(bar(sm->o_empty), 8); mbar_init(bar(sm->ml_full), 8); mbar_init(bar(sm->part_full), 8); mbar_init(bar(sm->last_full), 1);
         for (int s = 0; s < 4; ++s) mbar_init(bar(sm->drain[s]), 1);
+        for (int s = 0; s < 8; ++s) mbar_init(bar(sm->turn[s >> 2][s & 3]), 1);
         sm->abort[0] = 0; sm->abort[1] = 0;
         sm->limit[0] = sm->limit[1] = p.wait_limit;
         fence_barrier_init();
@@ -429,6 +431,10 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                         }
                     }
                     base_m = !valid ? -CUDART_INF_F : m == -CUDART_INF_F ? 0.0f : -m;
+                    // The slots' warps on a scheduler take turns at the exponentials (both have the same number of jobs): together they would queue for
+                    // the special-function unit and leave it idle together.  (2 x 2048 rows 668 -> 612 us, 65 rows 168 -> 155.)
+                    ok = a8_wait<0>(bar(sm->turn[slot][quad]), (used & 1u) ^ (slot ? 0u : 1u), flag);
+                    if (!ok) break;
                     const uint64_t base2 = pair(base_m, base_m);
                     uint64_t sum[2] = {0, 0};
                     uint32_t pk[NP][16];
@@ -446,11 +452,19 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
                         for (int q = 0; q < NP; ++q) pk[q][c / 4] = e[q];
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(sm->turn[slot ^ 1][quad]));
 #pragma unroll
                     for (int q = 0; q < NP; ++q) tmem_st16(aS + q * 16, pk[q]);
                     const uint64_t both = add2(sum[0], sum[1]);
                     l += low(both) + high(both);
                     tmem_wait_st();
+                }
+                if (!warp_has_rows) {
+                    ok = a8_wait<0>(bar(sm->turn[slot][quad]), (used & 1u) ^ (slot ? 0u : 1u), flag);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(bar(sm->turn[slot ^ 1][quad]));
+                    __syncwarp();
                 }
                 if (have < kAttnSub) {
                     // V behind the last key is cleared.  (Both slots of a paired item do: whoever comes second writes zeros over zeros.  The
@@ -463,10 +477,8 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(bar(sm->p_full[2 * h + slot]));
-                    if (last_use) mbar_arrive(bar(sm->sc_empty[rsc.s]));
-                }
+                a8_arrive<0>(bar(sm->p_full[2 * h + slot]), lane);
+                if (last_use) a8_arrive<0>(bar(sm->sc_empty[rsc.s]), lane);
                 if (last_use) { rsc.step(kA8Scales, 1); rv.step(kV, 1); }
                 cut -= step;
                 have -= step;
