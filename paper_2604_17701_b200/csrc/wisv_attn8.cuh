@@ -14,8 +14,8 @@
 // [part][column], so that a tile of K or V is read once for all of them, and each further part is scaled up by 16, since its sums are
 // kept apart until they are read.  Queries share a power of two that brings the tile's largest element to [128, 256): the floor is 2^-21 of that element.  (Where
 // three parts of S do not fit TMEM side by side they are added in one accumulator, unscaled: then every row has its own power of two, and the
-// floor is 2^-17 of the row's largest element.)  P is rounded to fp16 on the way, then to 9 bits where queries are bf16, half the error of a bf16 P;
-// its floor is 2^-14 (three parts: 2^-17) of its largest.  The products are exact, sums are fp32.
+// floor is 2^-17 of the row's largest element.)  Of P two parts keep 9 bits (and fp16's 11 on the way), half the error of a bf16 P, and three 14; its
+// floor is 2^-14 (three parts: 2^-17) of its largest.  The products are exact, sums are fp32.
 //
 // References.  m grows only when a column's x passes 8.75 (P must stay below 448, the largest e4m3 number), then to the column's largest (one more
 // where there are three parts, whose floor leaves room); l and O are scaled with it.  One vote of a slot's warps per tile says whether any
@@ -40,7 +40,7 @@
 // of a tile, half of them for waits, votes and addresses).
 //
 // Measured (8B shape: 32 query heads, 8 key heads, D = 128, pools with heads first; short runs): 64 requests of one row over 514 k keys
-// 172 us, 6.3 TB/s, 0.96 of the copy rate; of 4, 8, 9 and 16 rows over 270 k keys 102, 114, 131 and 153 us (5.6 to 3.8 TB/s); one
+// 174 us, 6.2 TB/s, 0.95 of the copy rate; of 4, 8, 9 and 16 rows over 270 k keys 101, 111, 130 and 146 us (5.7 to 4.0 TB/s); one
 // row over 131 k keys 54 us; one request of 9 rows over 709 keys 14.2 us, of which 3 us are the walk's first lookups, 1.5 the queries and 2 the merge.
 #pragma once
 
@@ -149,16 +149,51 @@ __device__ __forceinline__ float warp_max_nan(float x)
     asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
     return r;
 }
+// The e4m3 codes of four numbers (a word, the first in the low byte), and what is left of them, in fp16: 11 bits of the rest, where rounding the numbers
+// themselves to fp16 would leave it 7.
+__device__ __forceinline__ uint32_t a8_first(float x0, float x1, float x2, float x3, uint32_t& h0, uint32_t& h1)
+{
+    uint32_t c;
+    float r0, r1, r2, r3;
+    asm("{\n\t"
+        ".reg .b16 e0, e1, b0, b1, b2, b3, one;\n\t"
+        ".reg .b32 f0, f1;\n\t"
+        "mov.b16 one, 0xbc00;\n\t"                                 // -1
+        "cvt.rn.satfinite.e4m3x2.f32 e0, %6, %5;\n\t"
+        "cvt.rn.satfinite.e4m3x2.f32 e1, %8, %7;\n\t"
+        "mov.b32 %0, {e0, e1};\n\t"
+        "cvt.rn.f16x2.e4m3x2 f0, e0;\n\t"
+        "cvt.rn.f16x2.e4m3x2 f1, e1;\n\t"
+        "mov.b32 {b0, b1}, f0;\n\t"
+        "mov.b32 {b2, b3}, f1;\n\t"
+        "fma.rn.f32.f16 %1, b0, one, %5;\n\t"
+        "fma.rn.f32.f16 %2, b1, one, %6;\n\t"
+        "fma.rn.f32.f16 %3, b2, one, %7;\n\t"
+        "fma.rn.f32.f16 %4, b3, one, %8;\n\t"
+        "}"
+        : "=r"(c), "=f"(r0), "=f"(r1), "=f"(r2), "=f"(r3) : "f"(x0), "f"(x1), "f"(x2), "f"(x3));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(r1), "f"(r0));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(r3), "f"(r2));
+    return c;
+}
 // Four numbers below 448 in NP e4m3 parts each, largest first, each further part 16 times what is left where `kScaled`: a word of four codes,
 // the first number in the low byte, for each part
-template <int NP, bool kScaled>
+template <int NP, bool kScaled, bool kLong>
 __device__ __forceinline__ void a8_cut(float x0, float x1, float x2, float x3, uint32_t (&c)[NP])
 {
     uint32_t h0, h1;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(x1), "f"(x0));
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(x3), "f"(x2));
+    if (kLong) {
+        c[0] = a8_first(x0, x1, x2, x3, h0, h1);
+        if (kScaled) {
+            asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h0) : "r"(0x4c004c00u));               // 16
+            asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(h1) : "r"(0x4c004c00u));
+        }
+    } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(x1), "f"(x0));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(x3), "f"(x2));
+    }
 #pragma unroll
-    for (int p = 0; p < NP; ++p) {
+    for (int p = kLong ? 1 : 0; p < NP; ++p) {
         if (p + 1 < NP) {
             uint32_t b0, b1;
             asm("{\n\t"
@@ -386,7 +421,7 @@ __device__ __forceinline__ bool a8_cut_queries(const Attn8Params& p, A8Small* sm
 #pragma unroll
             for (int k = 0; k < 4; ++k) x[k] = fine ? x[k] * up : 0.0f;
             uint32_t f[NP];
-            a8_cut<NP, kCommon>(x[0], x[1], x[2], x[3], f);
+            a8_cut<NP, kCommon, false>(x[0], x[1], x[2], x[3], f);
 #pragma unroll
             for (int q = 0; q < NP; ++q) out[q][i] = f[q];
         }
@@ -838,7 +873,7 @@ __device__ __forceinline__ bool a8_stretch(const Attn8Params& p, A8Small* sm, A8
                     l[k / 2] = fma2(y[h], rb2, l[k / 2]);
                 }
                 uint32_t e[NP];
-                a8_cut<NP, true>(low(y[0]), high(y[0]), low(y[1]), high(y[1]), e);
+                a8_cut<NP, true, NP == 3>(low(y[0]), high(y[0]), low(y[1]), high(y[1]), e);
 #pragma unroll
                 for (int q = 0; q < NP; ++q) out[q][j] = e[q];
             }

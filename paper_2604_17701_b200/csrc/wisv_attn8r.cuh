@@ -6,16 +6,16 @@
 //
 // Parts.  Both operands' parts are added in one accumulator, so they are not scaled.  The last one is e5m2, whose steps go down to 2^-16: with a
 // largest element of a query row in [128, 256) two parts are exact for bf16 and three for fp16 down to 2^-24 of it; a P, whose largest is
-// 1 or more, is rounded to fp16 and then to 8 bits (bf16) or not at all (fp16), down to 2^-17.
+// 1 or more, is rounded to 8 bits (bf16, fp16's 11 on the way) or 13 (fp16), down to 2^-17.
 //
 // Against the kernel with keys as rows it needs a thread per row whether the row exists or not, but no meeting of warps, no tables of columns and half
-// of the instructions per element: 64 requests of 16, 17 and 24 rows of 4 heads over 270 k keys take 217, 223 and 223 us here and 153,
-// 354 and 244 there, where 17 tokens are two tiles.  Hence the rule: more than 64 rows to a request on the average.  The roles are
-// those of wisv_attn8.cuh, slots and merge those of wisv_attn.cuh.
+// of the instructions per element: 64 requests of 12, 16, 17 and 24 rows of 4 heads over 270 k keys take 200, 203, 208 and 211 us here and
+// 132, 147, 235 and 243 there, where 17 tokens are two tiles.  Hence the rule: more than 64 rows to a request on the average.  The roles
+// are those of wisv_attn8.cuh, slots and merge those of wisv_attn.cuh.
 //
-// Measured (8B shape, D = 128, short runs): 2 x 2048 rows over 8 k keys 698 us, 0.78 PFLOP/s of the formula's (each product is done twice, a
-// part at a time); 8 requests of 65 rows of 7 heads over 120 k keys 175 us.  What bounds it: two softmax warps on each scheduler, which issue half of the
-// time (exponentials and cutting 1240 of 2760 clocks per 64 keys, scores 660, the rest waits); the tensor pipe is active 36 %.
+// Measured (8B shape, D = 128, short runs): 2 x 2048 rows over 8 k keys 612 us, 0.89 PFLOP/s of the formula's (each product is done twice, a
+// part at a time); 8 requests of 65 rows of 7 heads over 120 k keys 155 us.  What bounds it: two softmax warps on each scheduler, which issue half of the
+// time; the tensor pipe is active 39 %.
 #pragma once
 
 #include "wisv_attn8.cuh"
@@ -46,14 +46,18 @@ static_assert(sizeof(R8Small) <= kR8Small, "shared memory");
 static_assert(offsetof(R8Small, limit) - offsetof(R8Small, abort) == 12, "attn_wait");
 
 // Four numbers below 448 in NP parts each, the last e5m2, the others e4m3 (see a8_cut)
-template <int NP>
+template <int NP, bool kLong>
 __device__ __forceinline__ void r8_cut(float x0, float x1, float x2, float x3, uint32_t (&c)[NP])
 {
     uint32_t h0, h1;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(x1), "f"(x0));
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(x3), "f"(x2));
+    if (kLong) {
+        c[0] = a8_first(x0, x1, x2, x3, h0, h1);
+    } else {
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h0) : "f"(x1), "f"(x0));
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(h1) : "f"(x3), "f"(x2));
+    }
 #pragma unroll
-    for (int p = 0; p + 1 < NP; ++p) {
+    for (int p = kLong ? 1 : 0; p + 1 < NP; ++p) {
         uint32_t b0, b1;
         asm("{\n\t"
             ".reg .b16 e0, e1;\n\t"
@@ -149,7 +153,7 @@ __device__ __forceinline__ void r8_cut_queries(const Attn8Params& p, int row0, i
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t f[NP];
-                r8_cut<NP>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, f);
+                r8_cut<NP, false>(fine ? x[4 * i] * up : 0.0f, fine ? x[4 * i + 1] * up : 0.0f, fine ? x[4 * i + 2] * up : 0.0f, fine ? x[4 * i + 3] * up : 0.0f, f);
 #pragma unroll
                 for (int q = 0; q < NP; ++q) out[q][i] = f[q];
             }
@@ -448,7 +452,7 @@ attn8_rows_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
                             sum[i] = fma2(y[i], lds_pair(sc + 1024 + (c + 2 * i) * 4), sum[i]);
                         }
                         uint32_t e[NP];
-                        r8_cut<NP>(low(y[0]), high(y[0]), low(y[1]), high(y[1]), e);
+                        r8_cut<NP, NP == 3>(low(y[0]), high(y[0]), low(y[1]), high(y[1]), e);
 #pragma unroll
                         for (int q = 0; q < NP; ++q) pk[q][c / 4] = e[q];
                     }

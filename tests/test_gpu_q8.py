@@ -4,8 +4,8 @@ Codes.  x and the largest |x| of its head, t, have at most 11 bits, so 448 x / t
 it is one exactly, and rounding it is the definition: codes must be equal.  Scales are one division in fp32 (2^-24, relative, or half a step of
 2^-149 where the result is subnormal).
 
-Attention.  With p the softmax, c and b the codes and scales of the values, v = c b.  A numerator P of p, times b, is rounded to fp16 (2^-11,
-relative) and then cut into parts that are added up again: two parts leave a bf16 cache at most 2^-8 of it, three an fp16 one 2^-13.  Below that is
+Attention.  With p the softmax, c and b the codes and scales of the values, v = c b.  A numerator P of p, times b, is cut into parts that are added
+up again (by way of fp16, 2^-11 at most): two parts leave a bf16 cache at most 2^-8 of it, three an fp16 one 2^-13.  Below that is
 the last part's half step, 2^-14 at most in units in which a column's largest P b is 1 or more; it meets every code.  Queries lose at
 most 2^-17 of the largest element A of their tile in each element, which enters a score as scale 2^-17 A sum_d |k_d|; sums are fp32, 2e-4
 covers them as in the 16-bit test.  The result is rounded once.  With h = 2^-11 + 2^-8 (2^-13 for fp16) and r = eps / 2:
